@@ -23,12 +23,16 @@
 
 #include <mutex>
 
+#include "bounded_wait.cuh"
 #include "sdvg_internal.h"
 #include "sm100_ptx.cuh"
+#include "tensor_map.h"
 
 namespace {
 
 using namespace sm100;
+using sdvg::encode_tiled_fn;
+using sdvg::EncodeTiledFn;
 
 constexpr int kTileM = 128;            // query rows per tile
 constexpr int kTileN = 128;            // keys per tile
@@ -81,73 +85,9 @@ __device__ __forceinline__ float fmax3(float a, float b, float c) {
   return y;
 }
 
-// Every wait on an mbarrier ends at an absolute deadline taken at kernel start.
-struct Deadline {
-  uint64_t t_ns;                       // globaltimer value after which waits give up
-  unsigned int* status;                // global status word
-};
-
-// Slow path of the bounded wait: poll until the phase completes or the deadline passes.  Kept out
-// of line of the first attempt so that the timer read never sits on the fast path.  Waiting threads
-// that poll less often (a suspend-time hint on the try_wait, the timer read once per 256 polls) or that
-// never suspend (test_wait) were measured 2-5% slower: how soon a waiter notices counts for more than the
-// issue slots its polling takes.
-__device__ __forceinline__ bool wait_bar_slow(uint32_t bar_addr, uint32_t parity, uint64_t deadline_ns,
-                                           unsigned int* status) {
-  uint32_t ok;
-  asm volatile(
-      "{\n\t"
-      ".reg .pred p, q;\n\t"
-      ".reg .u64 t;\n\t"
-      "SDVG_WAIT:\n\t"
-      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
-      "@p bra SDVG_DONE;\n\t"
-      "mov.u64 t, %%globaltimer;\n\t"
-      "setp.lt.u64 q, t, %3;\n\t"
-      "@q bra SDVG_WAIT;\n\t"
-      "SDVG_DONE:\n\t"
-      "selp.u32 %0, 1, 0, p;\n\t"
-      "}"
-      : "=r"(ok)
-      : "r"(bar_addr), "r"(parity), "l"(deadline_ns)
-      : "memory");
-  if (!ok) atomicMax(status, (unsigned)SDVG_ERR_TIMEOUT);      // sticky: only a reset clears it
-  return ok != 0;
-}
-
-// Bounded mbarrier wait.  One try_wait (which itself suspends the thread for a hardware-chosen
-// time) settles almost every wait; only if it fails does the thread enter the timed poll loop.
-// Returns false (and records SDVG_ERR_TIMEOUT) once the deadline has passed.
-__device__ __forceinline__ bool wait_bar(uint64_t* bar, uint32_t parity, const Deadline& d) {
-  if (mbar_try_wait(bar, parity)) return true;
-  return wait_bar_slow(smem_u32(bar), parity, d.t_ns, d.status);
-}
-
-// The same wait made by all 32 lanes of a warp, with a warp-uniform result.
-__device__ __forceinline__ bool wait_warp(uint64_t* bar, uint32_t parity, const Deadline& d) {
-  return __all_sync(0xffffffffu, wait_bar(bar, parity, d));
-}
-
 #include "attn_fwd_ws.cuh"
 
 // ---- host side -------------------------------------------------------------------------------
-
-typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
-                                  const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
-                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-EncodeTiledFn encode_tiled_fn() {
-  // looked up once; the initialisation of a function-local static is thread-safe
-  static const EncodeTiledFn fn = [] {
-    void* ptr = nullptr;
-    cudaDriverEntryPointQueryResult qres;
-    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &ptr, cudaEnableDefault, &qres) == cudaSuccess &&
-        qres == cudaDriverEntryPointSuccess)
-      return reinterpret_cast<EncodeTiledFn>(ptr);
-    return (EncodeTiledFn) nullptr;
-  }();
-  return fn;
-}
 
 // bf16 (elem_bytes 2) or byte (1) matrix seen as (dim, rows, heads) with arbitrary row and head strides;
 // box = 128 bytes x 128 rows x 1, 128-byte swizzle, rows beyond `rows` read as zero.

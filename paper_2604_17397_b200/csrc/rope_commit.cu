@@ -9,10 +9,14 @@
 // bytes per (token, head) row.
 #include <cuda_bf16.h>
 
+#include "rope_args.h"
 #include "sdvg_internal.h"
 #include "sm100_ptx.cuh"
 
 namespace {
+
+using sdvg::fill_rope;
+using sdvg::RopeArgs;
 
 constexpr int kMaxJobs = 3;
 constexpr int kHeadGroup = 8;     // heads walked by one thread
@@ -286,31 +290,6 @@ void tile_commit_jobs(TileQuantParams& p, int& n, const sdvg_cache* c, int slot,
                             (long long)c->slots * tiles, rope_k};
   p.job[n++] = TileQuantJob{(const uint4*)v, vslot, 16, head_stride, c->v_tile_scale + (size_t)slot * tiles,
                             (long long)c->slots * tiles, 0};
-}
-
-struct RopeArgs {
-  int frames, grid_h, grid_w, frame_offset, tab_frames;
-  const float* tab;
-};
-
-int fill_rope(RopeCommitParams& p, int head_dim, int tokens, const RopeArgs& r) {
-  if (r.frames <= 0 || r.grid_h <= 0 || r.grid_w <= 0) return SDVG_ERR_BAD_SHAPE;
-  if ((long long)r.frames * r.grid_h * r.grid_w != tokens) return SDVG_ERR_BAD_SHAPE;
-  if (!r.tab) return SDVG_ERR_INVALID_ARG;
-  if (!sdvg::aligned16(r.tab)) return SDVG_ERR_MISALIGNED;
-  if (r.tab_frames <= 0) return SDVG_ERR_BAD_SHAPE;
-  if (r.frame_offset < 0 || (long long)r.frame_offset + r.frames > r.tab_frames) return SDVG_ERR_BAD_STATE;
-  int pf, ph, pw;
-  sdvg_rope3d_pairs(head_dim, &pf, &ph, &pw);
-  p.grid_hw = r.grid_h * r.grid_w;
-  p.grid_w = r.grid_w;
-  p.frame_offset = r.frame_offset;
-  p.pairs_f = pf;
-  p.pairs_h = ph;
-  p.tab_h_off = r.tab_frames * pf;                 // in (cos, sin) pairs
-  p.tab_w_off = p.tab_h_off + r.grid_h * ph;
-  p.tab = reinterpret_cast<const float2*>(r.tab);
-  return SDVG_OK;
 }
 
 int launch(RopeCommitParams& p, int head_dim, cudaStream_t stream, bool q8 = false) {
