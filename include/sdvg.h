@@ -539,6 +539,103 @@ int sdvg_block_steps_e4m3_tiled(int steps, sdvg_cache* cache, const void* const*
                                 const float* cos_sin_tab, int tab_frames, int64_t block_index, float scale,
                                 void* workspace, size_t workspace_bytes, void* stream);
 
+/* ---- dense operators around the attention -------------------------------------- */
+/*
+ * What a transformer layer of the drafter or the target computes before and after the block attention
+ * (Sec. 4.1 "Models": both models share one attention backbone; the paper gives no layer formula, the forms
+ * below are the usual ones of a diffusion transformer whose modulation vectors change from frame to frame).
+ * Rows are tokens.  Matrices are row-major with unit column stride and a row stride `ld_*` counted in elements.
+ * Element types are SDVG_BF16, SDVG_F16 or SDVG_F32.  VECTORS (bias, gate, scale, shift, norm weights) are always
+ * fp32.  A vector that changes along the rows is a matrix with one row per GROUP of consecutive rows:
+ * row r uses group r / group_rows, and ceil(rows / group_rows) groups must be there.
+ * Arithmetic is fp32 with one rounding into each output.  Infinities and NaN travel as in the formulas.
+ */
+#define SDVG_BF16 0
+#define SDVG_F16  1
+#define SDVG_F32  2
+
+#define SDVG_ACT_NONE      0
+#define SDVG_ACT_SILU      1   /* v / (1 + e^-v) */
+#define SDVG_ACT_GELU_TANH 2   /* v / (1 + e^(-2u)), u = sqrt(2/pi) (v + 0.044715 v^3) */
+#define SDVG_ACT_GELU      3   /* v erfc(-v / sqrt 2) / 2 */
+
+/*
+ * out[r, j] = residual[r, j] + gate[r / gate_rows, j] * act( sum_k x[r, k] w[j, k] + bias[j] )
+ *   x         device, in_type (SDVG_BF16 or SDVG_F16) [rows, inner], row stride ld_x
+ *   w         device, the same type [cols, inner], row stride ld_w: the layout of a stored weight matrix
+ *   bias      device fp32 [cols], or NULL
+ *   gate      device fp32 [ceil(rows / gate_rows), cols], row stride ld_gate, or NULL (no factor; gate_rows unused)
+ *   residual  device, out_type [rows, cols], row stride ld_residual (0: one row for all), or NULL (no addend); may be `out`
+ *             itself (same pointer and stride), otherwise it must not overlap out
+ *   out       device, out_type [rows, cols], row stride ld_out >= cols; must not overlap x, w, bias or gate
+ * Products of the 16-bit operands on the tensor cores, fp32 accumulation over `inner`, fp32 epilogue.  The order of the sum
+ * depends on the three sizes alone: equal calls give equal bits.
+ * Strides and alignment: x and w are fetched by TMA, so their base addresses must be 16-byte aligned and ld_x, ld_w
+ * multiples of 8 and >= inner (a single row's stride is not read); rows longer than `inner` are padding that is not read
+ * into the result.  out, residual, bias and gate need the alignment of their element type only.
+ * rows == 0 or cols == 0 is a call with nothing to do.  inner >= 1.
+ * workspace: as for sdvg_block_attn_fwd (the same buffer may serve both): its status word reports a bounded wait that
+ * gave up (sdvg_block_attn_status), the call keeps nothing else in it.
+ * Errors: INVALID_ARG (NULL, unknown type or activation, workspace too small, gate_rows < 1), BAD_SHAPE (negative sizes,
+ * strides too small, more than 2^31 tiles), MISALIGNED, UNSUPPORTED_ARCH, CUDA.
+ */
+int sdvg_linear(const void* x, int64_t ld_x, const void* w, int64_t ld_w, const float* bias, int act,
+                const float* gate, int64_t ld_gate, int gate_rows, const void* residual, int64_t ld_residual,
+                void* out, int64_t ld_out, int rows, int cols, int inner, int in_type, int out_type,
+                void* workspace, size_t workspace_bytes, void* stream);
+
+#define SDVG_NORM_NONE  0
+#define SDVG_NORM_RMS   1   /* v / sqrt(mean(v^2) + eps) */
+#define SDVG_NORM_LAYER 2   /* (v - mean(v)) / sqrt(mean((v - mean(v))^2) + eps) */
+
+/*
+ * The residual add of one sublayer and the norm that opens the next, one pass over the rows:
+ *   s   = x + gate[r / gate_rows] * (post(y) * post_weight)
+ *   out = (norm(s) * weight + bias) * (1 + scale[r / mod_rows]) + shift[r / mod_rows]
+ *   x           device, x_type [rows, cols]
+ *   y           device, y_type [rows, cols], or NULL (s = x; then post must be SDVG_NORM_NONE and gate, post_weight NULL)
+ *   post_norm   norm of y's rows; post_weight fp32 [cols] or NULL (1)
+ *   gate        fp32 [groups, cols], row stride ld_gate, or NULL (1)
+ *   x_out       device, x_type: s rounded; NULL if not wanted.  May be x or y itself (same pointer, stride and type)
+ *   norm        norm of s's rows (of the unrounded sum); weight, bias fp32 [cols] or NULL (1 and 0)
+ *   scale/shift fp32 [groups, cols], both with row stride ld_mod; either may be NULL (0)
+ *   out         device, out_type; NULL if only x_out is wanted.  May be x or y itself (same pointer, stride and type)
+ * x_out and out must not overlap each other; nothing else may overlap them.  Strides are >= cols (a single row's is not
+ * read).  Each pointer needs the alignment of its element type; rows whose addresses are all multiples of 16 bytes with
+ * cols a multiple of 8 are moved in whole vectors, others element by element.
+ * Means and variances are fp32, the variance from the centred values.  eps >= 0 and finite.
+ * rows == 0 is a call with nothing to do.  cols >= 1.
+ * Errors: INVALID_ARG, BAD_SHAPE, MISALIGNED, UNSUPPORTED_ARCH, CUDA.
+ */
+int sdvg_gated_norm(const void* x, int64_t ld_x, int x_type, const void* y, int64_t ld_y, int y_type,
+                    int post_norm, const float* post_weight, const float* gate, int64_t ld_gate, int gate_rows,
+                    void* x_out, int64_t ld_x_out, int norm, const float* weight, const float* bias,
+                    const float* scale, const float* shift, int64_t ld_mod, int mod_rows, float eps,
+                    void* out, int64_t ld_out, int out_type, int rows, int cols, void* stream);
+
+#define SDVG_SCOPE_ROW  0   /* one norm over all heads of a token */
+#define SDVG_SCOPE_HEAD 1   /* one norm per head */
+
+/*
+ * sdvg_rope3d_qk_commit for a model that normalises q and k first: q_out = rope(rms(q) * q_weight), and
+ * rope(rms(k) * k_weight) and v go into the ring slot of block_index (and k' into k_out, if given), in one pass.
+ *   q, k, v   device bf16 [block_tokens, heads, head_dim] whose TOKEN strides ld_q, ld_k, ld_v (elements, multiples of 8,
+ *             >= heads * head_dim) may be larger than a token, e.g. column ranges of one fused QKV product
+ *   q_weight, k_weight   device fp32, 16-byte aligned: [heads * head_dim] with SDVG_SCOPE_ROW, [head_dim] with
+ *             SDVG_SCOPE_HEAD; NULL = 1
+ *   q_out, k_out   device bf16 [block_tokens, heads, head_dim], contiguous; q/q_out NULL/NULL for none, k_out optional;
+ *             q_out may be q and k_out may be k where those are contiguous
+ * Norm and rotation are fp32 with one rounding to bf16 at the end (no rounding between the two; v is copied).  Other
+ * arguments, ring semantics and errors as sdvg_rope3d_qk_commit; INVALID_ARG also for an unknown scope or a negative or
+ * non-finite eps; BAD_SHAPE also for strides that are too small, more than 16384 elements per token, or an 8-bit ring;
+ * MISALIGNED also for strides that are no multiple of 8.
+ */
+int sdvg_qk_norm_rope3d_commit(sdvg_cache* cache, const void* q, int64_t ld_q, const void* k, int64_t ld_k,
+                               const void* v, int64_t ld_v, const float* q_weight, const float* k_weight, int scope,
+                               float eps, void* q_out, void* k_out, int frames, int grid_h, int grid_w,
+                               int frame_offset, const float* cos_sin_tab, int tab_frames, int64_t block_index,
+                               int flags, int64_t* evicted_block, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

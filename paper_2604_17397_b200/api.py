@@ -30,6 +30,10 @@ SDVG_AGG_MIN = 0
 SDVG_AGG_MEAN = 1
 SDVG_SIGNAL_REWARD = 0
 SDVG_SIGNAL_RANDOM = 1
+SDVG_BF16, SDVG_F16, SDVG_F32 = 0, 1, 2
+SDVG_ACT_NONE, SDVG_ACT_SILU, SDVG_ACT_GELU_TANH, SDVG_ACT_GELU = 0, 1, 2, 3
+SDVG_NORM_NONE, SDVG_NORM_RMS, SDVG_NORM_LAYER = 0, 1, 2
+SDVG_SCOPE_ROW, SDVG_SCOPE_HEAD = 0, 1
 
 # name -> (restype, argtypes); the list of everything include/sdvg.h declares
 _VP, _I, _I64, _SZ, _F = C.c_void_p, C.c_int, C.c_int64, C.c_size_t, C.c_float
@@ -82,6 +86,12 @@ SIGNATURES = {
     "sdvg_block_steps": (_I, [_I, _VP, _VP, _VP, _VP, _VP, _VP, _I, _I, _I, _I, _VP, _I, _I64, _F, _VP, _SZ, _VP]),
     "sdvg_block_steps_e4m3": (_I, [_I, _VP, _VP, _VP, _VP, _VP, _VP, _VP, _VP, _VP, _VP, _VP, _I, _I, _I, _I, _VP, _I,
                                    _I64, _F, _VP, _SZ, _VP]),
+    "sdvg_linear": (_I, [_VP, _I64, _VP, _I64, _VP, _I, _VP, _I64, _I, _VP, _I64, _VP, _I64, _I, _I, _I, _I, _I,
+                         _VP, _SZ, _VP]),
+    "sdvg_gated_norm": (_I, [_VP, _I64, _I, _VP, _I64, _I, _I, _VP, _VP, _I64, _I, _VP, _I64, _I, _VP, _VP, _VP, _VP,
+                             _I64, _I, _F, _VP, _I64, _I, _I, _I, _VP]),
+    "sdvg_qk_norm_rope3d_commit": (_I, [_VP, _VP, _I64, _VP, _I64, _VP, _I64, _VP, _VP, _I, _F, _VP, _VP, _I, _I, _I, _I,
+                                        _VP, _I, _I64, _I, C.POINTER(_I64), _VP]),
 }
 
 _lib = None
@@ -604,3 +614,132 @@ def sdvg_block_attn_fwd_e4m3_batched(q8s, k_self8s, v_self8s, caches, block_indi
     st = lib().sdvg_block_attn_fwd_e4m3_batched(n, *[C.cast(a, _VP) if a is not None else None for a in keep], scale,
                                                 workspace.data_ptr(), workspace.numel(), _stream(stream))
     _check(st, "sdvg_block_attn_fwd_e4m3_batched")
+
+
+# ---------------------------------------------------------------- dense operators around the attention
+
+_ELEM_TYPES = {torch.bfloat16: SDVG_BF16, torch.float16: SDVG_F16, torch.float32: SDVG_F32}
+
+
+def _matrix(t: Optional[torch.Tensor], like: torch.Tensor, rows: int, cols: int, dtype: torch.dtype, what: str):
+    """(pointer, row stride) of a [rows, cols] tensor with unit column stride on `like`'s device; (None, 0) for None."""
+    if t is None:
+        return None, 0
+    if t.dtype != dtype or t.device != like.device or t.shape != (rows, cols):
+        raise ValueError(f"{what}: expected {dtype} [{rows}, {cols}] on {like.device}, got {t.dtype} "
+                         f"{list(t.shape)} on {t.device}")
+    ld, step = t.stride()
+    if step != 1 and cols > 1:
+        raise ValueError(f"{what}: columns must be contiguous")
+    return t.data_ptr(), ld
+
+
+def _vector(t: Optional[torch.Tensor], like: torch.Tensor, n: int, what: str):
+    if t is None:
+        return None
+    if t.dtype != torch.float32 or t.device != like.device or t.shape != (n,) or (t.stride(0) != 1 and n > 1):
+        raise ValueError(f"{what}: expected contiguous float32 [{n}] on {like.device}")
+    return t.data_ptr()
+
+
+def _groups(t: Optional[torch.Tensor], like: torch.Tensor, rows: int, cols: int, group_rows: int, what: str):
+    """Vectors that change with the row group: one row per `group_rows` rows."""
+    if t is None:
+        return None, 0
+    if group_rows < 1:
+        raise ValueError(f"{what}: rows per group must be given")
+    return _matrix(t, like, -(-rows // group_rows), cols, torch.float32, what)
+
+
+def _call_on(t: torch.Tensor, name: str, *args) -> None:
+    """Calls an entry point whose last argument is the stream, with `t`'s device current (streams and launches are the
+    current device's); the last of `args` is the caller's stream or None."""
+    if not t.is_cuda:
+        raise ValueError("expected CUDA tensors")
+    fn = getattr(lib(), name)
+    if t.device.index == torch.cuda.current_device():
+        _check(fn(*args[:-1], _stream(args[-1])), name)
+    else:
+        with torch.cuda.device(t.device):
+            _check(fn(*args[:-1], _stream(args[-1])), name)
+
+
+def sdvg_linear(x, w, out, workspace, bias=None, act: int = SDVG_ACT_NONE, residual=None, gate=None, gate_rows: int = 0,
+                stream=None) -> None:
+    """out = residual + gate[row // gate_rows] * act(x @ w.T + bias): x [rows, inner] and w [cols, inner] bf16 or fp16,
+    out and residual [rows, cols] of one type, bias fp32 [cols], gate fp32 [groups, cols].  Row strides are free
+    (x and w: multiples of 8; residual may be one expanded row); residual may be `out`."""
+    rows, inner = x.shape
+    cols = w.shape[0]
+    if x.dtype not in (torch.bfloat16, torch.float16) or out.dtype not in _ELEM_TYPES:
+        raise ValueError("x must be bfloat16 or float16, out also float32")
+    xp, ld_x = _matrix(x, x, rows, inner, x.dtype, "x")
+    wp, ld_w = _matrix(w, x, cols, inner, x.dtype, "w")
+    op, ld_out = _matrix(out, x, rows, cols, out.dtype, "out")
+    rp, ld_res = _matrix(residual, x, rows, cols, out.dtype, "residual")
+    gp, ld_gate = _groups(gate, x, rows, cols, gate_rows, "gate")
+    if workspace.device != x.device:
+        raise ValueError("workspace must be on the tensors' device")
+    _call_on(x, "sdvg_linear", xp, ld_x, wp, ld_w, _vector(bias, x, cols, "bias"), act, gp, ld_gate, gate_rows, rp, ld_res,
+             op, ld_out, rows, cols, inner, _ELEM_TYPES[x.dtype], _ELEM_TYPES[out.dtype], workspace.data_ptr(),
+             workspace.numel(), stream)
+
+
+def sdvg_gated_norm(x, out, y=None, gate=None, gate_rows: int = 0, post_norm: int = SDVG_NORM_NONE, post_weight=None,
+                    x_out=None, norm: int = SDVG_NORM_LAYER, weight=None, bias=None, scale=None, shift=None,
+                    modulate_rows: int = 0, eps: float = 1e-6, stream=None) -> None:
+    """s = x + gate[row // gate_rows] * (post_norm(y) * post_weight); x_out = s;
+    out = (norm(s) * weight + bias) * (1 + scale[row // modulate_rows]) + shift[row // modulate_rows].
+    x, y, x_out, out: [rows, cols] of bf16, fp16 or fp32 (x_out has x's type; out may be None when x_out is given);
+    vectors fp32 [cols], gate / scale / shift fp32 [groups, cols]."""
+    rows, cols = x.shape
+    for t in (x, y, out):
+        if t is not None and t.dtype not in _ELEM_TYPES:
+            raise ValueError("expected bfloat16, float16 or float32 tensors")
+    xp, ld_x = _matrix(x, x, rows, cols, x.dtype, "x")
+    yp, ld_y = (None, 0) if y is None else _matrix(y, x, rows, cols, y.dtype, "y")
+    xo, ld_xo = _matrix(x_out, x, rows, cols, x.dtype, "x_out")
+    op, ld_out = (None, 0) if out is None else _matrix(out, x, rows, cols, out.dtype, "out")
+    gp, ld_gate = _groups(gate, x, rows, cols, gate_rows, "gate")
+    sp, ld_mod = _groups(scale, x, rows, cols, modulate_rows, "scale")
+    hp, ld_shift = _groups(shift, x, rows, cols, modulate_rows, "shift")
+    if sp is not None and hp is not None and ld_mod != ld_shift and rows > modulate_rows:
+        raise ValueError("scale and shift must have the same row stride")
+    _call_on(x, "sdvg_gated_norm", xp, ld_x, _ELEM_TYPES[x.dtype], yp, ld_y, 0 if y is None else _ELEM_TYPES[y.dtype],
+             post_norm, _vector(post_weight, x, cols, "post_weight"), gp, ld_gate, gate_rows, xo, ld_xo, norm,
+             _vector(weight, x, cols, "weight"), _vector(bias, x, cols, "bias"), sp, hp, ld_mod if sp is not None else ld_shift,
+             modulate_rows, eps, op, ld_out, 0 if out is None else _ELEM_TYPES[out.dtype], rows, cols, stream)
+
+
+def _tokens(t: Optional[torch.Tensor], cache: Cache, what: str):
+    """(pointer, token stride) of a bf16 [block_tokens, heads, head_dim] tensor that is contiguous within a token."""
+    if t is None:
+        return None, 0
+    shape = (cache.block_tokens, cache.heads, cache.head_dim)
+    if t.dtype != torch.bfloat16 or t.shape != shape or t.device != cache._k_raw.device:
+        raise ValueError(f"{what}: expected bfloat16 {list(shape)} on {cache._k_raw.device}")
+    ld, head, step = t.stride()
+    if step != 1 or (head != cache.head_dim and cache.heads > 1):
+        raise ValueError(f"{what}: the heads of a token must be contiguous")
+    return t.data_ptr(), ld if cache.block_tokens > 1 else cache.heads * cache.head_dim
+
+
+def sdvg_qk_norm_rope3d_commit(cache: Cache, q, k, v, q_weight, k_weight, scope: int, eps: float, q_out, k_out, grid,
+                               frame_offset: int, table, tab_frames: int, block_index: int, flags: int, stream=None) -> int:
+    """sdvg_rope3d_qk_commit with an RMS norm of q and k first; q, k, v may be column ranges of a wider QKV product
+    viewed as [tokens, heads, head_dim].  Returns the evicted block."""
+    width = cache.heads * cache.head_dim if scope == SDVG_SCOPE_ROW else cache.head_dim
+    dev = cache._k_raw
+    (qp, ld_q), (kp, ld_k), (vp, ld_v) = _tokens(q, cache, "q"), _tokens(k, cache, "k"), _tokens(v, cache, "v")
+    outs = []
+    for t, what in ((q_out, "q_out"), (k_out, "k_out")):
+        p, ld = _tokens(t, cache, what)
+        if t is not None and ld != cache.heads * cache.head_dim:
+            raise ValueError(f"{what} must be contiguous")
+        outs.append(p)
+    frames, grid_h, grid_w = grid
+    ev = _I64(-1)
+    _call_on(dev, "sdvg_qk_norm_rope3d_commit", cache.handle, qp, ld_q, kp, ld_k, vp, ld_v,
+             _vector(q_weight, dev, width, "q_weight"), _vector(k_weight, dev, width, "k_weight"), scope, eps, outs[0],
+             outs[1], frames, grid_h, grid_w, frame_offset, _ptr(table), tab_frames, block_index, flags, C.byref(ev), stream)
+    return ev.value

@@ -70,6 +70,14 @@ __device__ __forceinline__ uint64_t globaltimer_ns() {
 __device__ __forceinline__ void prefetch_tmap(const CUtensorMap* m) {
   asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(m)) : "memory");
 }
+// 2-D tiled load global -> shared, completion counted in bytes on `bar`.
+__device__ __forceinline__ void tma_load_2d(void* smem_dst, const CUtensorMap* m, uint64_t* bar, int c0, int c1) {
+  asm volatile(
+      "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
+      " [%0], [%1, {%3, %4}], [%2];" ::"r"(smem_u32(smem_dst)),
+      "l"(reinterpret_cast<uint64_t>(m)), "r"(smem_u32(bar)), "r"(c0), "r"(c1)
+      : "memory");
+}
 // 3-D tiled load global -> shared, completion counted in bytes on `bar`.
 __device__ __forceinline__ void tma_load_3d(void* smem_dst, const CUtensorMap* m, uint64_t* bar, int c0,
                                             int c1, int c2) {
@@ -224,6 +232,15 @@ __host__ __device__ constexpr uint32_t idesc_bf16_f32(int m, int n, bool b_mn_ma
          | (1u << 7)                     // A is bf16
          | (1u << 10)                    // B is bf16
          | ((b_mn_major ? 1u : 0u) << 16)
+         | ((uint32_t)(n >> 3) << 17)
+         | ((uint32_t)(m >> 4) << 24);
+}
+
+// Instruction descriptor: 16-bit x 16-bit -> fp32 with both operands K-major and of the same type (bf16, or fp16).
+__host__ __device__ constexpr uint32_t idesc_16bit_f32(int m, int n, bool bf16) {
+  return (1u << 4)                       // D is fp32
+         | ((bf16 ? 1u : 0u) << 7)       // A
+         | ((bf16 ? 1u : 0u) << 10)      // B
          | ((uint32_t)(n >> 3) << 17)
          | ((uint32_t)(m >> 4) << 24);
 }
