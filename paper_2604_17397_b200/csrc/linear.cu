@@ -13,6 +13,7 @@
 #include <cuda.h>
 #include <math.h>
 
+#include <algorithm>
 #include <mutex>
 
 #include "bounded_wait.cuh"
@@ -29,6 +30,7 @@ constexpr int kTileF = 128;                          // features per tile: the i
 constexpr int kTileK = 64;                           // elements of `inner` per stage: one 128-byte swizzled row
 constexpr int kMaxTileT = 256;                       // tokens per tile: the instruction's N, a multiple of 16
 constexpr uint64_t kWaitLimitNs = 2000000000ull;     // 2 s per wait
+constexpr int kMaxStages = 8;
 constexpr int kWorkspaceBytes = 256;
 constexpr int kMaxDevices = 64;
 
@@ -43,7 +45,9 @@ struct alignas(64) LinearParams {
   int gate_rows;
   int rows, cols;
   int act;
-  int tile_t, tiles_f, k_iters, stages;
+  int tile_t, tiles_f, tiles_t, k_iters, stages;
+  int group;                                         // feature tiles of a group of the tile order (pairs)
+  long long tiles;
   uint32_t idesc;
   unsigned int* status;
 };
@@ -65,66 +69,144 @@ template <> struct OutElem<SDVG_F32> {
   static __device__ __forceinline__ T put(float v) { return v; }
 };
 
-// Both exponential forms keep their relative accuracy where the value vanishes: v / (1 + e^-z) tends to -0 for z -> -inf
-// (the exponential overflows to infinity), and GELU uses erfc, which has no 1 + erf cancellation.
-__device__ __forceinline__ float activate(float v, int act) {
-  if (act == SDVG_ACT_SILU) return __fdividef(v, 1.f + __expf(-v));
-  if (act == SDVG_ACT_GELU_TANH) return __fdividef(v, 1.f + __expf(-1.5957691216057308f * fmaf(0.044715f * v * v, v, v)));
-  if (act == SDVG_ACT_GELU) return 0.5f * v * erfcf(-0.70710678118654752f * v);
-  return v;
+// The exponential forms keep their relative accuracy where the value vanishes: v / (1 + e^-z) tends to -0 for z -> -inf
+// (the exponential overflows to infinity).
+//
+// GELU: v Phi(v) with the lower tail h = erfc(z) / 2, z = |v| / sqrt 2, taken directly, without the cancellation of 1 + erf:
+// erfc(z) e^(z^2) / t with t = 1 / (1 + 0.45 z) is smooth on 0 < t <= 1, and a polynomial of degree 9 in t, fitted by
+// least squares with weights driven towards an even relative error, is within 3.3e-8 of it (relative, in exact arithmetic;
+// 6.2e-7 in fp32 for |v| < 3, 4.1e-6 at |v| = 12, where the rounding of v^2 counts).  The library's erfcf, 16 at a time,
+// took so many registers that others spilled.
+__device__ __forceinline__ float gelu_erf(float v) {
+  const float z = fabsf(v);
+  const float t = __fdividef(1.f, fmaf(0.31819805f, z, 1.f));
+  float q = -0.02069617911700f;
+  q = fmaf(q, t, 0.09534660188561f);
+  q = fmaf(q, t, -0.15029583590903f);
+  q = fmaf(q, t, 0.07120466716636f);
+  q = fmaf(q, t, -0.01118113013510f);
+  q = fmaf(q, t, 0.05997585263270f);
+  q = fmaf(q, t, 0.08762596187607f);
+  q = fmaf(q, t, 0.11413582878705f);
+  q = fmaf(q, t, 0.12694158118874f);
+  q = fmaf(q, t, 0.12694266037636f);
+  const float h = q * t * __expf(-0.5f * v * v);
+  return v > 0.f ? fmaf(-v, h, v) : v * h;
 }
 
-// Epilogue of 32 tokens m0 .. of one feature n: `acc` holds the sums; tokens from `m_end` on are not touched.
+// The choice is made once for the 16 values, and the epilogue is instantiated once per kernel: unrolled over a tile with
+// the choice inside, its code outgrew the instruction caches and the fetches took ten times the arithmetic.
+__device__ __forceinline__ void activate16(float (&v)[16], int act) {
+  if (act == SDVG_ACT_SILU) {
+#pragma unroll
+    for (int j = 0; j < 16; ++j) v[j] = __fdividef(v[j], 1.f + __expf(-v[j]));
+  } else if (act == SDVG_ACT_GELU_TANH) {
+#pragma unroll
+    for (int j = 0; j < 16; ++j)
+      v[j] = __fdividef(v[j], 1.f + __expf(-1.5957691216057308f * fmaf(0.044715f * v[j] * v[j], v[j], v[j])));
+  } else if (act == SDVG_ACT_GELU) {
+#pragma unroll
+    for (int j = 0; j < 16; ++j) v[j] = gelu_erf(v[j]);
+  }
+}
+
+// A row stride whose multiples the compiler must form where they are used: hoisted out of the epilogue's loop, 16 of them
+// for each of two matrices cost 64 registers and spilled others into its loop.
+__device__ __forceinline__ long long stride_here(long long ld) {
+  asm volatile("" : "+l"(ld));
+  return ld;
+}
+
+// Residual of 16 tokens m0 .. of one feature n, requested a block ahead of its use: the epilogue would otherwise spend
+// most of its time waiting for these loads.
 template <int OutType>
-__device__ __forceinline__ void epilogue32(const LinearParams& p, const uint32_t (&acc)[32], int n, int m0, int m_end) {
+__device__ __forceinline__ void load_residual16(const LinearParams& p, typename OutElem<OutType>::T (&res)[16], int n,
+                                                int m0, int m_end) {
+  using T = typename OutElem<OutType>::T;
+  if (!p.residual || n >= p.cols) return;
+  const long long ld = stride_here(p.ld_res);
+  const T* r = static_cast<const T*>(p.residual) + m0 * ld + n;
+  if (m0 + 16 <= m_end) {
+#pragma unroll
+    for (int j = 0; j < 16; ++j, r += ld) res[j] = *r;
+  } else {
+#pragma unroll
+    for (int j = 0; j < 16; ++j, r += ld)
+      if (m0 + j < m_end) res[j] = *r;
+  }
+}
+
+// Epilogue of these tokens: `acc` holds the sums; tokens from `m_end` on are not touched.
+template <int OutType>
+__device__ __forceinline__ void epilogue16(const LinearParams& p, float (&acc)[16], typename OutElem<OutType>::T (&res)[16],
+                                           int n, int m0, int m_end, float b) {
   using E = OutElem<OutType>;
   using T = typename E::T;
   if (n >= p.cols || m0 >= m_end) return;
-  const int count = min(32, m_end - m0);
-  T res[32];
-  if (p.residual) {
-    const T* r = static_cast<const T*>(p.residual) + (long long)m0 * p.ld_res + n;
+  const int count = min(16, m_end - m0);
+  const long long ld = stride_here(p.ld_out);
+  T* o = static_cast<T*>(p.out) + m0 * ld + n;
 #pragma unroll
-    for (int j = 0; j < 32; ++j)
-      if (j < count) res[j] = r[j * p.ld_res];
-  }
-  float g[32];
+  for (int j = 0; j < 16; ++j) acc[j] += b;
+  activate16(acc, p.act);
+  int group = 0, last_group = 0;
   if (p.gate) {
-    const int g0 = m0 / p.gate_rows, g1 = (m0 + count - 1) / p.gate_rows;
-    const float* gp = p.gate + g0 * p.ld_gate + n;
-    const float first = gp[0];
-    if (g0 == g1) {
+    group = m0 / p.gate_rows;
+    last_group = (m0 + count - 1) / p.gate_rows;
+  }
+  if (count == 16 && group == last_group) {
+    // whole block, one gate: about ten instructions per value
+    const float g = p.gate ? p.gate[group * p.ld_gate + n] : 1.f;
+    if (p.residual) {
 #pragma unroll
-      for (int j = 0; j < 32; ++j) g[j] = first;
-    } else {
-      long long next = (long long)(g0 + 1) * p.gate_rows;
+      for (int j = 0; j < 16; ++j) acc[j] = fmaf(acc[j], g, E::get(res[j]));
+    } else if (p.gate) {
 #pragma unroll
-      for (int j = 0; j < 32; ++j) {
-        if (j < count) {
+      for (int j = 0; j < 16; ++j) acc[j] *= g;
+    }
+#pragma unroll
+    for (int j = 0; j < 16; ++j, o += ld) *o = E::put(acc[j]);
+  } else {
+    const float* gp = p.gate ? p.gate + group * p.ld_gate + n : nullptr;
+    long long next = (long long)(group + 1) * p.gate_rows;
+#pragma unroll
+    for (int j = 0; j < 16; ++j, o += ld) {
+      if (j < count) {
+        float v = acc[j];
+        if (p.gate) {
           if (m0 + j == next) {
             gp += p.ld_gate;
             next += p.gate_rows;
           }
-          g[j] = gp[0];
+          v *= *gp;
         }
+        if (p.residual) v += E::get(res[j]);
+        *o = E::put(v);
       }
-    }
-  }
-  const float b = p.bias ? p.bias[n] : 0.f;
-  T* o = static_cast<T*>(p.out) + (long long)m0 * p.ld_out + n;
-#pragma unroll
-  for (int j = 0; j < 32; ++j) {
-    if (j < count) {
-      float v = activate(__uint_as_float(acc[j]) + b, p.act);
-      if (p.gate) v *= g[j];
-      if (p.residual) v += E::get(res[j]);
-      o[j * p.ld_out] = E::put(v);
     }
   }
 }
 
+// Position in the ring of operand stages: the stage and the parity of its current use.
+struct RingPos {
+  int stage = 0;
+  uint32_t phase = 0;
+  __device__ __forceinline__ void next(int stages) {
+    if (++stage == stages) {
+      stage = 0;
+      phase ^= 1;
+    }
+  }
+  __device__ __forceinline__ void back(int stages) {
+    if (--stage < 0) {
+      stage = stages - 1;
+      phase ^= 1;
+    }
+  }
+};
+
 struct TileSmem {
-  uint64_t full[8], empty[8], done;
+  uint64_t full[kMaxStages], empty[kMaxStages], done;
   uint32_t tmem;
 };
 
@@ -163,24 +245,28 @@ __global__ void __launch_bounds__(128) linear_tile_kernel(const __grid_constant_
   if (warp == 0) {
     if (elect_one()) {
       int i = 0;
-      for (; i < p.k_iters; ++i) {
-        const int s = i % p.stages;
-        if (!wait_for(&sm.empty[s], ((i / p.stages) & 1) ^ 1, p.status, kWaitLimitNs)) break;
+      RingPos r;
+      for (; i < p.k_iters; ++i, r.next(p.stages)) {
+        const int s = r.stage;
+        if (!wait_for(&sm.empty[s], r.phase ^ 1, p.status, kWaitLimitNs)) break;
         uint8_t* st = buf + s * stage_bytes;
         mbar_expect_tx(&sm.full[s], stage_bytes);
         tma_load_2d(st, &p.w_map, &sm.full[s], i * kTileK, n0);
         tma_load_2d(st + w_bytes, &p.x_map, &sm.full[s], i * kTileK, m0);
       }
       if (i < p.k_iters)                             // gave up: see the copies in flight land before the CTA may leave
-        for (int j = max(0, i - p.stages); j < i; ++j)
-          wait_for(&sm.full[j % p.stages], (j / p.stages) & 1, p.status, kWaitLimitNs);
+        for (int j = min(i, p.stages); j > 0; --j) {
+          r.back(p.stages);
+          wait_for(&sm.full[r.stage], r.phase, p.status, kWaitLimitNs);
+        }
     }
   } else if (warp == 1) {
     if (elect_one()) {
       bool ok = true;
-      for (int i = 0; i < p.k_iters; ++i) {
-        const int s = i % p.stages;
-        if (!(ok = wait_for(&sm.full[s], (i / p.stages) & 1, p.status, kWaitLimitNs))) break;
+      RingPos r;
+      for (int i = 0; i < p.k_iters; ++i, r.next(p.stages)) {
+        const int s = r.stage;
+        if (!(ok = wait_for(&sm.full[s], r.phase, p.status, kWaitLimitNs))) break;
         tc_fence_after();
         const uint32_t st = smem_u32(buf + s * stage_bytes);
         const uint64_t a = smem_desc_sw128(st, 16, 1024), b = smem_desc_sw128(st + w_bytes, 16, 1024);
@@ -195,17 +281,236 @@ __global__ void __launch_bounds__(128) linear_tile_kernel(const __grid_constant_
   if (__all_sync(0xffffffffu, wait_for(&sm.done, 0, p.status, kWaitLimitNs))) {
     tc_fence_after();
     const int m_end = min(p.rows, m0 + p.tile_t);
-    for (int c = 0; m0 + c < m_end; c += 32) {
-      uint32_t acc[32];
-      tmem_ld32(tmem + ((uint32_t)(warp * 32) << 16) + c, acc);
+    const int n = n0 + warp * 32 + lane;
+    const float b = p.bias && n < p.cols ? p.bias[n] : 0.f;
+#pragma unroll 1
+    for (int c = 0; m0 + c < m_end; c += 16) {
+      float acc[16];
+      typename OutElem<OutType>::T res[16];
+      load_residual16<OutType>(p, res, n, m0 + c, m_end);
+      tmem_ld16(tmem + ((uint32_t)(warp * 32) << 16) + c, reinterpret_cast<uint32_t(&)[16]>(acc));
       tmem_wait_ld();
-      epilogue32<OutType>(p, acc, n0 + warp * 32 + lane, m0 + c, m_end);
+      epilogue16<OutType>(p, acc, res, n, m0 + c, m_end, b);
     }
   }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   if (warp == 0) tmem_dealloc(tmem, tmem_cols);
+}
+
+// ---- many tokens: CTA pairs, persistent ---------------------------------------------------------
+//
+// A pair of CTAs (two SMs) works on one tile of 256 features x tile_t tokens: each CTA holds 128 of the features (its
+// accumulator lanes) and fetches half of the token tile, and one tcgen05.mma of the even CTA reads both halves, so that a
+// token tile crosses into shared memory once per pair.  Accumulators are double-buffered in tensor memory (2 x 256
+// columns): the epilogue of one tile runs under the products of the next.
+//
+// fp32 outputs: the tensor core adds a product to the accumulator by truncation, so a sum over `inner` drifts in one
+// direction by about 2^-26 of its magnitude per 16 products (measured 3.7e-6 relative for inner = 5120, fp32's own
+// rounding giving 1e-7).  That is far below the rounding of a 16-bit output but not of an fp32 one, so there the sum is
+// cut into chunks of kChunkK: each chunk gets a fresh accumulator, and the epilogue warps add the chunks with round-to-nearest.
+constexpr int kEpiWarps = 8;
+constexpr int kPairThreads = 32 * (kEpiWarps + 2);
+constexpr int kPairSmem = 227 * 1024 - 512;          // dynamic shared memory of a CTA; the barriers are static
+constexpr int kChunkK = 1024;
+// Tensor memory columns of the two accumulators; a chunked sum keeps its running total in a third set.  (Held in registers
+// between chunks, 2 or 3 blocks of 32 totals a thread spilled others into the epilogue's loop: up to 2x the time.)
+constexpr int kMaxTileChunked = 160;
+template <int OutType>
+constexpr int kAccStride = OutType == SDVG_F32 ? kMaxTileChunked : kMaxTileT;
+
+struct PairSmem {
+  uint64_t full[kMaxStages], empty[kMaxStages], acc_full[2], acc_empty[2];
+  uint32_t tmem;
+};
+
+// Tile t of the list: groups of `group` neighbouring feature tiles, token tiles within a group, features innermost, so
+// that the pairs that run at the same time share operand tiles in L2 on both sides.
+__device__ __forceinline__ void tile_of(const LinearParams& p, long long t, int* f, int* tok) {
+  const long long per_group = (long long)p.group * p.tiles_t;
+  const int g = (int)(t / per_group);
+  const int r = (int)(t - g * per_group);
+  const int width = min(p.group, p.tiles_f - g * p.group);
+  *tok = r / width;
+  *f = g * p.group + r % width;
+}
+
+template <int OutType>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
+    linear_pair_kernel(const __grid_constant__ LinearParams p) {
+  constexpr bool kChunked = OutType == SDVG_F32;
+  using T = typename OutElem<OutType>::T;
+  extern __shared__ uint8_t raw[];
+  __shared__ PairSmem sm;
+  uint8_t* buf = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  const uint32_t rank = cluster_ctarank();
+  const int pair = blockIdx.x / 2, pairs = gridDim.x / 2;
+  const int w_bytes = kTileF * 128, stage_bytes = w_bytes + p.tile_t * 64;
+  const int chunks = kChunked ? (p.k_iters + kChunkK / kTileK - 1) / (kChunkK / kTileK) : 1;
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < p.stages; ++s) {
+      mbar_init(&sm.full[s], 1);                     // the even CTA's counts the bytes of both
+      mbar_init(&sm.empty[s], 1);
+    }
+    for (int b = 0; b < 2; ++b) {
+      mbar_init(&sm.acc_full[b], 1);
+      mbar_init(&sm.acc_empty[b], 2 * kEpiWarps);    // the even CTA's: the epilogue warps of both
+    }
+    fence_mbar_init();
+    prefetch_tmap(&p.w_map);
+    prefetch_tmap(&p.x_map);
+  }
+  if (warp == 0) {
+    tmem_alloc_pair(&sm.tmem, 512);
+    tmem_relinquish_pair();
+  }
+  tc_fence_before();
+  __syncthreads();
+  cluster_arrive();
+  cluster_wait();                                    // the other CTA's barriers are initialised as well
+  tc_fence_after();
+  const uint32_t tmem = sm.tmem;
+
+  if (warp == kEpiWarps) {
+    // ================= producer: this CTA's features and its half of the token tile =================
+    if (elect_one()) {
+      RingPos r;
+      int issued = 0;                                // up to the number of stages
+      bool ok = true;
+      for (long long t = pair; ok && t < p.tiles; t += pairs) {
+        int ft, tt;
+        tile_of(p, t, &ft, &tt);
+        const int n0 = (2 * ft + (int)rank) * kTileF, m0 = tt * p.tile_t + (int)rank * (p.tile_t / 2);
+        for (int i = 0; i < p.k_iters; ++i, r.next(p.stages)) {
+          const int s = r.stage;
+          if (!(ok = wait_for(&sm.empty[s], r.phase ^ 1, p.status, kWaitLimitNs))) break;
+          issued = min(issued + 1, p.stages);
+          uint8_t* st = buf + s * stage_bytes;
+          const uint32_t full = map_to_rank(smem_u32(&sm.full[s]), 0);
+          if (rank == 0) mbar_expect_tx(&sm.full[s], 2 * stage_bytes);
+          tma_load_2d_pair(st, &p.w_map, full, i * kTileK, n0);
+          tma_load_2d_pair(st + w_bytes, &p.x_map, full, i * kTileK, m0);
+        }
+      }
+      // every stage is read (on a give-up: landed, as far as this CTA can tell) before the CTA may leave
+      for (; issued > 0; --issued) {
+        r.back(p.stages);
+        if (ok) ok = wait_for(&sm.empty[r.stage], r.phase, p.status, kWaitLimitNs);
+        else if (rank == 0) wait_for(&sm.full[r.stage], r.phase, p.status, kWaitLimitNs);
+      }
+    }
+  } else if (warp == kEpiWarps + 1) {
+    // ================= issuer: the even CTA, for both ==============================================
+    if (rank == 0 && elect_one()) {
+      RingPos r, acc;
+      bool ok = true;
+      for (long long t = pair; ok && t < p.tiles; t += pairs) {
+        for (int c = 0; ok && c < chunks; ++c, acc.next(2)) {
+          const int b = acc.stage;
+          if (!(ok = wait_for(&sm.acc_empty[b], acc.phase ^ 1, p.status, kWaitLimitNs))) break;
+          tc_fence_after();
+          const int i0 = c * (kChunkK / kTileK);
+          const int i1 = kChunked ? min(p.k_iters, i0 + kChunkK / kTileK) : p.k_iters;
+          for (int i = i0; i < i1; ++i, r.next(p.stages)) {
+            const int s = r.stage;
+            if (!(ok = wait_for(&sm.full[s], r.phase, p.status, kWaitLimitNs))) break;
+            tc_fence_after();
+            const uint32_t st = smem_u32(buf + s * stage_bytes);
+            const uint64_t da = smem_desc_sw128(st, 16, 1024), db = smem_desc_sw128(st + w_bytes, 16, 1024);
+#pragma unroll
+            for (int kk = 0; kk < 4; ++kk)
+              mma_ss_pair(tmem + b * kAccStride<OutType>, da + 2 * kk, db + 2 * kk, p.idesc, i > i0 || kk > 0);
+            mma_commit_pair(&sm.empty[s]);
+          }
+          if (ok) mma_commit_pair(&sm.acc_full[b]);
+        }
+      }
+    }
+  } else if (warp < kEpiWarps) {
+    // ================= epilogue: warps w and w + 4 share 32 features and take 32-token column blocks in turn ==========
+    const int quad = warp % 4, half = warp / 4;
+    const uint32_t lanes = tmem + ((uint32_t)(quad * 32) << 16);
+    const uint32_t empty0 = map_to_rank(smem_u32(&sm.acc_empty[0]), 0), empty1 = map_to_rank(smem_u32(&sm.acc_empty[1]), 0);
+    RingPos r;
+    bool ok = true;
+    for (long long t = pair; ok && t < p.tiles; t += pairs) {
+      int ft, tt;
+      tile_of(p, t, &ft, &tt);
+      const int n = (2 * ft + (int)rank) * kTileF + quad * 32 + lane;
+      const int m0 = tt * p.tile_t, m_end = min(p.rows, m0 + p.tile_t);
+      const float bias = p.bias && n < p.cols ? p.bias[n] : 0.f;
+      // this warp's columns: blocks of 32 from 32 half on, 64 apart, handled as two halves of 16
+      T ahead0[16], ahead1[16];
+      load_residual16<OutType>(p, ahead0, n, m0 + half * 32, m_end);
+      load_residual16<OutType>(p, ahead1, n, m0 + half * 32 + 16, m_end);
+      if constexpr (kChunked) {
+        for (int c = 0; c < chunks - 1; ++c) {       // all but the last chunk: add to the total, which stays in tensor memory
+          ok = __all_sync(0xffffffffu, wait_for(&sm.acc_full[r.stage], r.phase, p.status, kWaitLimitNs));
+          if (!ok) break;
+          tc_fence_after();
+          const uint32_t part = lanes + r.stage * kAccStride<OutType>, total = lanes + 2 * kAccStride<OutType>;
+#pragma unroll 1
+          for (int col = half * 32; m0 + col < m_end; col += 64) {
+            float v[32], sum[32];
+            tmem_ld32(part + col, reinterpret_cast<uint32_t(&)[32]>(v));
+            if (c > 0) tmem_ld32(total + col, reinterpret_cast<uint32_t(&)[32]>(sum));
+            tmem_wait_ld();
+            if (c > 0) {
+#pragma unroll
+              for (int j = 0; j < 32; ++j) v[j] += sum[j];
+            }
+            tmem_st32(total + col, reinterpret_cast<uint32_t(&)[32]>(v));
+          }
+          tmem_wait_st();
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive_cluster(r.stage ? empty1 : empty0);
+          r.next(2);
+        }
+        if (!ok) break;
+      }
+      ok = __all_sync(0xffffffffu, wait_for(&sm.acc_full[r.stage], r.phase, p.status, kWaitLimitNs));
+      if (!ok) break;
+      tc_fence_after();
+      const uint32_t cols = lanes + r.stage * kAccStride<OutType>;
+#pragma unroll 1
+      for (int col = half * 32; m0 + col < m_end; col += 64) {
+        float acc0[16], acc1[16];
+        tmem_ld16(cols + col, reinterpret_cast<uint32_t(&)[16]>(acc0));
+        tmem_ld16(cols + col + 16, reinterpret_cast<uint32_t(&)[16]>(acc1));
+        if (kChunked && chunks > 1) {
+          float sum0[16], sum1[16];
+          const uint32_t total = lanes + 2 * kAccStride<OutType> + col;
+          tmem_ld16(total, reinterpret_cast<uint32_t(&)[16]>(sum0));
+          tmem_ld16(total + 16, reinterpret_cast<uint32_t(&)[16]>(sum1));
+          tmem_wait_ld();
+#pragma unroll
+          for (int j = 0; j < 16; ++j) {
+            acc0[j] += sum0[j];
+            acc1[j] += sum1[j];
+          }
+        }
+        tmem_wait_ld();
+        epilogue16<OutType>(p, acc0, ahead0, n, m0 + col, m_end, bias);
+        load_residual16<OutType>(p, ahead0, n, m0 + col + 64, m_end);
+        epilogue16<OutType>(p, acc1, ahead1, n, m0 + col + 16, m_end, bias);
+        load_residual16<OutType>(p, ahead1, n, m0 + col + 80, m_end);
+      }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive_cluster(r.stage ? empty1 : empty0);
+      r.next(2);
+    }
+  }
+  __syncwarp();
+  tc_fence_before();
+  __syncthreads();
+  cluster_arrive();
+  cluster_wait();                                    // neither CTA leaves while the other may still reach into it
+  tc_fence_after();
+  if (warp == 0) tmem_dealloc_pair(tmem, 512);
 }
 
 // ---- host side -------------------------------------------------------------------------------
@@ -228,25 +533,90 @@ int make_map(CUtensorMap* m, const void* base, int type, int inner, int rows, in
 
 std::mutex g_setup_mu;
 
+constexpr int kPairRows = 256;                       // more tokens than this go to the pairs
+
+// Tokens per tile of the pairs: the size whose waves of tiles cost least.  A tile's time grows linearly with its tokens on
+// top of a part that does not depend on them (the features' operand tiles come in whatever the token count), worth about
+// kFixedTokens: at 4680 x 5120 x 15360 a wave of tiles took 13.9, 18.9, 24.8 and 32.3 us for 64, 128, 192 and 256 tokens.
+// Small tiles lose to that part, large ones to the last, partly filled wave (5120 features: 6 waves either way, 179 us at
+// 224 tokens and 190 us at 256; 194 us in 10 full waves of 128).
+constexpr int kFixedTokens = 80;
+int pair_tile(int rows, int tiles_f, int pairs, int largest) {
+  int best = largest;
+  long long best_cost = 0;
+  for (int nt = largest; nt >= 64; nt -= 16) {
+    const long long tiles = (long long)tiles_f * ((rows + nt - 1) / nt);
+    const long long cost = (tiles + pairs - 1) / pairs * (nt + kFixedTokens);
+    if (!best_cost || cost < best_cost) {
+      best = nt;
+      best_cost = cost;
+    }
+  }
+  return best;
+}
+
 constexpr int kTileDynamic = 4 * (kTileF + kMaxTileT) * 128 + 1024;
 
+// One-time set-up per device and output type: the opt-in to the kernels' dynamic shared memory, and how many CTA pairs
+// the device runs at once.
 template <int OutType>
-int launch_tile(const LinearParams& p, long long tiles, cudaStream_t stream) {
-  static bool ready[kMaxDevices] = {};
+int set_up(int* pairs) {
+  static int pairs_of_device[kMaxDevices] = {};
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return sdvg::cuda_status(e);
   if (dev < 0 || dev >= kMaxDevices) return SDVG_ERR_INVALID_ARG;
-  {
-    std::lock_guard<std::mutex> lock(g_setup_mu);
-    if (!ready[dev]) {
-      e = cudaFuncSetAttribute(linear_tile_kernel<OutType>, cudaFuncAttributeMaxDynamicSharedMemorySize, kTileDynamic);
-      if (e != cudaSuccess) return sdvg::cuda_status(e);
-      ready[dev] = true;
-    }
+  std::lock_guard<std::mutex> lock(g_setup_mu);
+  if (!pairs_of_device[dev]) {
+    e = cudaFuncSetAttribute(linear_tile_kernel<OutType>, cudaFuncAttributeMaxDynamicSharedMemorySize, kTileDynamic);
+    if (e != cudaSuccess) return sdvg::cuda_status(e);
+    e = cudaFuncSetAttribute(linear_pair_kernel<OutType>, cudaFuncAttributeMaxDynamicSharedMemorySize, kPairSmem);
+    if (e != cudaSuccess) return sdvg::cuda_status(e);
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(2);
+    cfg.blockDim = dim3(kPairThreads);
+    cfg.dynamicSmemBytes = kPairSmem;
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = 2;
+    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    int n = 0;
+    e = cudaOccupancyMaxActiveClusters(&n, linear_pair_kernel<OutType>, &cfg);
+    if (e != cudaSuccess || n < 1) return sdvg::cuda_status(e != cudaSuccess ? e : cudaErrorUnknown);
+    pairs_of_device[dev] = n;
   }
-  const int dynamic = p.stages * (kTileF + p.tile_t) * 128 + 1024;
-  linear_tile_kernel<OutType><<<(unsigned)tiles, 128, dynamic, stream>>>(p);
+  *pairs = pairs_of_device[dev];
+  return SDVG_OK;
+}
+
+template <int OutType>
+int launch(LinearParams& p, const void* x, int64_t ld_x, const void* w, int64_t ld_w, int inner, int in_type,
+           cudaStream_t stream) {
+  int pairs = 0;
+  int st = set_up<OutType>(&pairs);
+  if (st != SDVG_OK) return st;
+  const bool by_pair = p.rows > kPairRows;
+  const int feature_tile = by_pair ? 2 * kTileF : kTileF;
+  p.tiles_f = (p.cols + feature_tile - 1) / feature_tile;
+  p.tile_t = p.rows >= kMaxTileT ? kMaxTileT : (p.rows + 15) / 16 * 16;
+  if (by_pair) p.tile_t = pair_tile(p.rows, p.tiles_f, pairs, OutType == SDVG_F32 ? kMaxTileChunked : kMaxTileT);
+  p.tiles_t = (p.rows + p.tile_t - 1) / p.tile_t;
+  p.tiles = (long long)p.tiles_f * p.tiles_t;
+  if (p.tiles >= 1ll << 31) return SDVG_ERR_BAD_SHAPE;
+  p.idesc = idesc_16bit_f32(feature_tile, p.tile_t, in_type == SDVG_BF16);
+  if ((st = make_map(&p.w_map, w, in_type, inner, p.cols, ld_w, kTileF)) != SDVG_OK) return st;
+  if ((st = make_map(&p.x_map, x, in_type, inner, p.rows, ld_x, by_pair ? p.tile_t / 2 : p.tile_t)) != SDVG_OK) return st;
+  if (by_pair) {
+    p.group = 8;
+    p.stages = std::min(kMaxStages, (kPairSmem - 1024) / (kTileF * 128 + p.tile_t * 64));
+    const int grid = 2 * (int)std::min((long long)pairs, p.tiles);
+    linear_pair_kernel<OutType><<<grid, kPairThreads, kPairSmem, stream>>>(p);
+  } else {
+    p.stages = 4;
+    linear_tile_kernel<OutType><<<(unsigned)p.tiles, 128, p.stages * (kTileF + p.tile_t) * 128 + 1024, stream>>>(p);
+  }
   return sdvg::cuda_status(cudaGetLastError());
 }
 
@@ -292,19 +662,12 @@ int sdvg_linear(const void* x, int64_t ld_x, const void* w, int64_t ld_w, const 
   p.rows = rows;
   p.cols = cols;
   p.act = act;
-  p.tile_t = rows >= kMaxTileT ? kMaxTileT : (rows + 15) / 16 * 16;
-  p.tiles_f = (cols + kTileF - 1) / kTileF;
   p.k_iters = (inner + kTileK - 1) / kTileK;
-  p.stages = 4;
-  p.idesc = idesc_16bit_f32(kTileF, p.tile_t, in_type == SDVG_BF16);
   p.status = (unsigned int*)workspace + 1;
-  const long long tiles = (long long)p.tiles_f * ((rows + p.tile_t - 1) / p.tile_t);
-  if (tiles >= 1ll << 31) return SDVG_ERR_BAD_SHAPE;
-  if ((st = make_map(&p.w_map, w, in_type, inner, cols, ld_w, kTileF)) != SDVG_OK) return st;
-  if ((st = make_map(&p.x_map, x, in_type, inner, rows, ld_x, p.tile_t)) != SDVG_OK) return st;
-  if (out_type == SDVG_F32) return launch_tile<SDVG_F32>(p, tiles, (cudaStream_t)stream);
-  if (out_type == SDVG_F16) return launch_tile<SDVG_F16>(p, tiles, (cudaStream_t)stream);
-  return launch_tile<SDVG_BF16>(p, tiles, (cudaStream_t)stream);
+  const cudaStream_t s = (cudaStream_t)stream;
+  if (out_type == SDVG_F32) return launch<SDVG_F32>(p, x, ld_x, w, ld_w, inner, in_type, s);
+  if (out_type == SDVG_F16) return launch<SDVG_F16>(p, x, ld_x, w, ld_w, inner, in_type, s);
+  return launch<SDVG_BF16>(p, x, ld_x, w, ld_w, inner, in_type, s);
 }
 
 }  // extern "C"
