@@ -1,6 +1,17 @@
 // Residual add of a sublayer's output (with its own norm and gate) and the modulated norm that opens the next sublayer,
 // one pass over the rows.
+//
+// Bound by HBM: every row of x and y is read once and every row of x_out and out written once.  A row is split over a team
+// (a CTA, or one warp where a warp can hold the row) and stays in registers between its statistics and its outputs.
+// A thread keeps the same columns for all rows it walks, and with them the vectors, combined to three:
+//   s = x + G * post(y),  out = norm(s) * A + B,   G = gate * post_weight,  A = weight * (1 + scale),  B = bias * (1 + scale) + shift
+// which change only with the row group; read per row instead, they were 60 KB through L1 for 40 KB of row (5120 columns).
+// The next rows are on their way into shared memory meanwhile (cp.async, every thread fetching just what it will read
+// itself, so that no barrier is needed): held in registers they cost the occupancy that hides the reductions.
+// The arithmetic is in packed pairs (fma.rn.f32x2).
 #include <math.h>
+
+#include <algorithm>
 
 #include "elem_types.cuh"
 #include "sdvg_internal.h"
@@ -29,22 +40,441 @@ struct NormParams {
   float eps, inv_cols;
 };
 
-constexpr int kThreads = 256;
+// Sum and centred sum of squares of a part of a row: parts combine without the cancellation of a difference of squares.
+struct Moments {
+  float sum, m2;
+};
 
-// Sum over the CTA; every thread gets it.
-__device__ __forceinline__ float block_sum(float v, float* buf) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-  __syncthreads();                                   // the last sum's readers are done with buf
-  if ((threadIdx.x & 31) == 0) buf[threadIdx.x >> 5] = v;
-  __syncthreads();
-  v = threadIdx.x % 32 < kThreads / 32 ? buf[threadIdx.x % 32] : 0.f;
+__device__ __forceinline__ float warp_sum(float v) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
   return v;
 }
 
-// One CTA per row.  `value(c)` gives the row's column c; the mean is subtracted for a layer norm, and the variance is
+__device__ __forceinline__ float bf16_lo(uint32_t u) { return __uint_as_float(u << 16); }
+__device__ __forceinline__ float bf16_hi(uint32_t u) { return __uint_as_float(u & 0xffff0000u); }
+
+// Eight columns as four packed pairs of fp32.
+typedef unsigned long long Pair;
+struct Vec8 {
+  Pair p[4];
+};
+__device__ __forceinline__ Pair pair_of(float lo, float hi) {
+  Pair r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+  return r;
+}
+__device__ __forceinline__ float2 floats_of(Pair a) {
+  float2 f;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(f.x), "=f"(f.y) : "l"(a));
+  return f;
+}
+__device__ __forceinline__ Pair add2(Pair a, Pair b) {
+  Pair r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ Pair fma2(Pair a, Pair b, Pair c) {
+  Pair r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+
+__device__ __forceinline__ void unpack8(const uint4& a, int type, Vec8& v) {
+  const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+  if (type == SDVG_BF16) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v.p[j] = pair_of(bf16_lo(w[j]), bf16_hi(w[j]));
+  } else {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[j]));
+      v.p[j] = pair_of(f.x, f.y);
+    }
+  }
+}
+
+__device__ __forceinline__ void store8(char* at, int type, const Vec8& v) {
+  float2 f[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) f[j] = floats_of(v.p[j]);
+  if (type == SDVG_F32) {
+    float4* o = reinterpret_cast<float4*>(at);
+    __stcs(o, make_float4(f[0].x, f[0].y, f[1].x, f[1].y));
+    __stcs(o + 1, make_float4(f[2].x, f[2].y, f[3].x, f[3].y));
+    return;
+  }
+  uint32_t w[4];
+  if (type == SDVG_BF16) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const __nv_bfloat162 h = __floats2bfloat162_rn(f[j].x, f[j].y);
+      w[j] = *reinterpret_cast<const uint32_t*>(&h);
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const __half2 h = __floats2half2_rn(f[j].x, f[j].y);
+      w[j] = *reinterpret_cast<const uint32_t*>(&h);
+    }
+  }
+  __stcs(reinterpret_cast<uint4*>(at), make_uint4(w[0], w[1], w[2], w[3]));
+}
+
+__device__ __forceinline__ void copy16(void* smem, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(smem)), "l"(src)
+               : "memory");
+}
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+// A thread's pieces of a tensor's next rows, W bytes per element (0: no such tensor): piece i of ring slot s is W / 2
+// vectors of 16 bytes, the warp's 32 threads side by side.
+template <int W, int NI>
+struct Ring {
+  static constexpr int kVecs = W / 2;
+  static constexpr int kBytes = NI * kVecs * 16;       // per thread and slot
+  uint4* mine;                                         // this thread's first vector
+  __device__ __forceinline__ uint4* at(int slot, int i, int h) const { return mine + ((slot * NI + i) * kVecs + h) * 32; }
+  __device__ __forceinline__ void request(int slot, int i, const char* row) const {
+#pragma unroll
+    for (int h = 0; h < kVecs; ++h) copy16(at(slot, i, h), row + (i * 256 * W + 16 * h));
+  }
+  __device__ __forceinline__ void values(int slot, int i, int type, Vec8& v) const {
+    if constexpr (W == 2) {
+      unpack8(*at(slot, i, 0), type, v);
+    } else if constexpr (W == 4) {
+      const float4 a = *reinterpret_cast<const float4*>(at(slot, i, 0)), b = *reinterpret_cast<const float4*>(at(slot, i, 1));
+      v.p[0] = pair_of(a.x, a.y);
+      v.p[1] = pair_of(a.z, a.w);
+      v.p[2] = pair_of(b.x, b.y);
+      v.p[3] = pair_of(b.z, b.w);
+    }
+  }
+};
+
+constexpr int kSlots = 2;                              // rows on their way per team
+constexpr int kTeamThreads = 640;                      // most threads of a CTA team; leaves a thread 96 registers
+
+__device__ __forceinline__ void load_vector(const float* p, float (&v)[8]) {
+  const float4 a = __ldg(reinterpret_cast<const float4*>(p)), b = __ldg(reinterpret_cast<const float4*>(p) + 1);
+  v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+}
+
+// Joins the warps' moments of a row to its mean and 1 / deviation: warp w has the sum and the centred sum of squares of
+// counts[w] columns.  With one warp per row there is nothing to join.
+template <bool WARP>
+struct Team {
+  Moments (*part)[32];                                 // two exchange buffers
+  const float* counts;
+  int turn = 0;
+
+  __device__ __forceinline__ void join(const NormParams& p, int kind, Moments m, float* mean, float* rstd) {
+    if (!WARP) {
+      // a buffer is written again only two exchanges later, after a barrier that its readers have reached
+      const int lane = threadIdx.x % 32;
+      if (lane == 0) part[turn][threadIdx.x / 32] = m;
+      __syncthreads();
+      const bool mine = lane < blockDim.x / 32;
+      const Moments other = mine ? part[turn][lane] : Moments{0.f, 0.f};
+      if (kind == SDVG_NORM_LAYER) {
+        m.sum = warp_sum(other.sum);
+        const float n = mine ? counts[lane] : 0.f;
+        const float off = n > 0.f ? __fdividef(other.sum, n) - m.sum * p.inv_cols : 0.f;
+        m.m2 = warp_sum(fmaf(n * off, off, other.m2));
+      } else {
+        m.m2 = warp_sum(other.m2);
+      }
+      turn ^= 1;
+    }
+    *mean = m.sum * p.inv_cols;
+    *rstd = rsqrtf(fmaf(m.m2, p.inv_cols, p.eps));
+  }
+};
+
+// This warp's moments of a row of vectors held in v.
+template <int NI, class Valid>
+__device__ __forceinline__ Moments warp_moments(const Vec8 (&v)[NI], int kind, float inv_count, Valid valid) {
+  Moments m{0.f, 0.f};
+  if (kind == SDVG_NORM_LAYER) {
+    Pair a = 0, b = 0;                                 // 0.0f pairs
+#pragma unroll
+    for (int i = 0; i < NI; ++i)
+      if (valid(i)) {
+        a = add2(a, add2(v[i].p[0], v[i].p[1]));
+        b = add2(b, add2(v[i].p[2], v[i].p[3]));
+      }
+    const float2 f = floats_of(add2(a, b));
+    m.sum = warp_sum(f.x + f.y);
+  }
+  const float mid = -m.sum * inv_count;
+  const Pair mid2 = pair_of(mid, mid);
+  Pair a = 0, b = 0;
+#pragma unroll
+  for (int i = 0; i < NI; ++i)
+    if (valid(i)) {
+#pragma unroll
+      for (int j = 0; j < 4; j += 2) {
+        const Pair d = add2(v[i].p[j], mid2), e = add2(v[i].p[j + 1], mid2);
+        a = fma2(d, d, a);
+        b = fma2(e, e, b);
+      }
+    }
+  const float2 f = floats_of(add2(a, b));
+  m.m2 = warp_sum(f.x + f.y);
+  return m;
+}
+
+// (v - mean) * rstd
+template <int NI>
+__device__ __forceinline__ void apply_norm(Vec8 (&v)[NI], float mean, float rstd) {
+  const Pair r = pair_of(rstd, rstd), c = pair_of(-mean, -mean);
+  const Pair zero = pair_of(-0.f, -0.f);               // x * r + -0 is x * r to the bit
+#pragma unroll
+  for (int i = 0; i < NI; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[i].p[j] = fma2(add2(v[i].p[j], c), r, zero);
+}
+
+// Rows of aligned vectors.  XW and YW: bytes of x's and y's elements (YW = 0: no y).  A thread holds NI pieces of 8 columns; the
+// pieces of a warp are 32 vectors apart, so that they are a constant distance from one address per row, which moves on by the
+// row stride.  FULL: the team's pieces are all inside the row.
+template <int XW, int YW, int NI, bool WARP, bool FULL>
+__global__ void __launch_bounds__(WARP ? 128 : kTeamThreads) gated_norm_kernel(const NormParams p) {
+  extern __shared__ uint4 s_ring[];
+  __shared__ Moments s_part[2][32];
+  __shared__ float s_count[32];
+  const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+  const int c0 = ((WARP ? 0 : warp * 32 * NI) + lane) * 8;             // first piece; piece i: c0 + 256 i
+  auto valid = [&](int i) { return FULL || c0 + 256 * i < p.cols; };
+  // neighbouring rows per team: they share their group's vectors
+  const int teams = WARP ? gridDim.x * (blockDim.x / 32) : gridDim.x, me = WARP ? blockIdx.x * (blockDim.x / 32) + warp : blockIdx.x;
+  const int share = p.rows / teams, rest = p.rows % teams;
+  const long long begin = (long long)me * share + min(me, rest), end = begin + share + (me < rest ? 1 : 0);
+  float own = 0.f;
+#pragma unroll
+  for (int i = 0; i < NI; ++i) own += valid(i) ? 8.f : 0.f;
+  const float count = warp_sum(own), inv_count = count > 0.f ? 1.f / count : 0.f;
+  if (!WARP && lane == 0) s_count[warp] = count;
+  Team<WARP> team{s_part, s_count};
+
+  uint4* ring = s_ring + warp * 32 * (kSlots * (Ring<XW, NI>::kBytes + Ring<YW, NI>::kBytes) / 16) + lane;
+  const Ring<XW, NI> rx{ring};
+  const Ring<YW, NI> ry{ring + kSlots * Ring<XW, NI>::kBytes / 16 * 32};
+  const int out_bytes = p.out_type == SDVG_F32 ? 4 : 2;
+  const char* x = static_cast<const char*>(p.x) + (begin * p.ld_x + c0) * XW;
+  const char* y = static_cast<const char*>(p.y) + (begin * p.ld_y + c0) * YW;
+  char* x_out = static_cast<char*>(p.x_out) + (begin * p.ld_x_out + c0) * XW;
+  char* out = static_cast<char*>(p.out) + (begin * p.ld_out + c0) * out_bytes;
+  const long long step_x = p.ld_x * XW, step_y = p.ld_y * YW, step_x_out = p.ld_x_out * XW, step_out = p.ld_out * out_bytes;
+  int asked = 0;                                       // rows requested so far; x and y point at the next one
+  const int total = (int)(end - begin);
+  auto request = [&](int slot) {
+    if (asked < total) {
+#pragma unroll
+      for (int i = 0; i < NI; ++i)
+        if (valid(i)) {
+          rx.request(slot, i, x);
+          if (YW) ry.request(slot, i, y);
+        }
+    }
+    copy_commit();                                     // an empty group where there is no such row
+    ++asked;
+    x += step_x;
+    y += step_y;
+  };
+#pragma unroll
+  for (int k = 0; k < kSlots; ++k) request(k);
+
+  Vec8 G[YW ? NI : 1], A[NI], B[NI];
+  long long new_gate = begin, new_mod = begin;         // rows at which the vectors change
+  int slot = 0;
+  for (long long r = begin; r < end; ++r, slot = slot + 1 == kSlots ? 0 : slot + 1) {      // uniform over the team
+    if (YW && r == new_gate) {
+      const unsigned group = p.gate ? (unsigned)r / (unsigned)p.gate_rows : 0;
+      new_gate = p.gate ? (long long)(group + 1) * p.gate_rows : end;
+#pragma unroll
+      for (int i = 0; i < NI; ++i) {
+        float g[8] = {1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f}, w[8];
+        if (valid(i)) {
+          if (p.gate) load_vector(p.gate + group * p.ld_gate + c0 + 256 * i, g);
+          if (p.post_weight) {
+            load_vector(p.post_weight + c0 + 256 * i, w);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) g[j] *= w[j];
+          }
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) G[i].p[j] = pair_of(g[2 * j], g[2 * j + 1]);
+      }
+    }
+    if (p.out && r == new_mod) {
+      const bool mod = p.scale || p.shift;
+      const unsigned group = mod ? (unsigned)r / (unsigned)p.mod_rows : 0;
+      new_mod = mod ? (long long)(group + 1) * p.mod_rows : end;
+#pragma unroll
+      for (int i = 0; i < NI; ++i) {
+        float a[8] = {1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f}, b[8] = {}, f[8];
+        if (valid(i)) {
+          const int c = c0 + 256 * i;
+          if (p.weight) load_vector(p.weight + c, a);
+          if (p.bias) load_vector(p.bias + c, b);
+          if (p.scale) {
+            load_vector(p.scale + group * p.ld_mod + c, f);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+              a[j] = fmaf(a[j], f[j], a[j]);
+              b[j] = fmaf(b[j], f[j], b[j]);
+            }
+          }
+          if (p.shift) {
+            load_vector(p.shift + group * p.ld_mod + c, f);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) b[j] += f[j];
+          }
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          A[i].p[j] = pair_of(a[2 * j], a[2 * j + 1]);
+          B[i].p[j] = pair_of(b[2 * j], b[2 * j + 1]);
+        }
+      }
+    }
+    copy_wait<kSlots - 1>();                           // this thread's own copies: nobody else reads them
+    Vec8 s[NI];
+    float mean = 0.f, rstd = 1.f;
+    if constexpr (YW != 0) {
+      Vec8 v[NI];
+#pragma unroll
+      for (int i = 0; i < NI; ++i) ry.values(slot, i, p.y_type, v[i]);
+      if (p.post != SDVG_NORM_NONE) {
+        team.join(p, p.post, warp_moments<NI>(v, p.post, inv_count, valid), &mean, &rstd);
+        apply_norm<NI>(v, mean, rstd);
+      }
+#pragma unroll
+      for (int i = 0; i < NI; ++i) {
+        rx.values(slot, i, p.x_type, s[i]);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) s[i].p[j] = fma2(G[i].p[j], v[i].p[j], s[i].p[j]);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < NI; ++i) rx.values(slot, i, p.x_type, s[i]);
+    }
+    request(slot);
+    if (p.x_out) {
+#pragma unroll
+      for (int i = 0; i < NI; ++i)
+        if (valid(i)) store8(x_out + 256 * XW * i, p.x_type, s[i]);
+      x_out += step_x_out;
+    }
+    if (!p.out) continue;
+    if (p.norm != SDVG_NORM_NONE) {
+      team.join(p, p.norm, warp_moments<NI>(s, p.norm, inv_count, valid), &mean, &rstd);
+      apply_norm<NI>(s, mean, rstd);
+    }
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) s[i].p[j] = fma2(s[i].p[j], A[i].p[j], B[i].p[j]);
+      if (valid(i)) store8(out + 256 * out_bytes * i, p.out_type, s[i]);
+    }
+    out += step_out;
+  }
+  copy_wait<0>();
+}
+
+// Rows that are not made of aligned vectors: one CTA per row, NI single columns per thread; what is in flight comes from the
+// CTAs of an SM.
+template <int NI>
+__global__ void __launch_bounds__(256) gated_norm_single_kernel(const NormParams p) {
+  __shared__ Moments s_part[2][32];
+  __shared__ float s_count[32];
+  const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+  const long long r = blockIdx.x;
+  auto col = [&](int i) { return (int)(i * blockDim.x + threadIdx.x); };
+  auto valid = [&](int i) { return col(i) < p.cols; };
+  float s[NI], y[NI];
+#pragma unroll
+  for (int i = 0; i < NI; ++i) {
+    if (valid(i)) s[i] = load_elem(p.x, r * p.ld_x + col(i), p.x_type);
+  }
+  if (p.y) {
+#pragma unroll
+    for (int i = 0; i < NI; ++i)
+      if (valid(i)) y[i] = load_elem(p.y, r * p.ld_y + col(i), p.y_type);
+  }
+  float own = 0.f;
+#pragma unroll
+  for (int i = 0; i < NI; ++i) own += valid(i) ? 1.f : 0.f;
+  const float count = warp_sum(own), inv_count = count > 0.f ? 1.f / count : 0.f;
+  if (lane == 0) s_count[warp] = count;
+  Team<false> team{s_part, s_count};
+  auto moments = [&](const float (&v)[NI], int kind) {
+    Moments m{0.f, 0.f};
+    if (kind == SDVG_NORM_LAYER) {
+#pragma unroll
+      for (int i = 0; i < NI; ++i) m.sum += valid(i) ? v[i] : 0.f;
+      m.sum = warp_sum(m.sum);
+    }
+    const float mid = m.sum * inv_count;
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      const float d = valid(i) ? v[i] - mid : 0.f;
+      m.m2 = fmaf(d, d, m.m2);
+    }
+    m.m2 = warp_sum(m.m2);
+    return m;
+  };
+  float mean = 0.f, rstd = 1.f;
+  if (p.y) {
+    if (p.post != SDVG_NORM_NONE) team.join(p, p.post, moments(y, p.post), &mean, &rstd);
+    const float* gate = p.gate ? p.gate + ((unsigned)r / (unsigned)p.gate_rows) * p.ld_gate : nullptr;
+#pragma unroll
+    for (int i = 0; i < NI; ++i)
+      if (valid(i)) {
+        float v = p.post != SDVG_NORM_NONE ? (y[i] - mean) * rstd : y[i];
+        if (p.post_weight) v *= __ldg(p.post_weight + col(i));
+        s[i] = gate ? fmaf(__ldg(gate + col(i)), v, s[i]) : s[i] + v;
+      }
+  }
+  if (p.x_out) {
+#pragma unroll
+    for (int i = 0; i < NI; ++i)
+      if (valid(i)) store_elem(p.x_out, r * p.ld_x_out + col(i), p.x_type, s[i]);
+  }
+  if (!p.out) return;
+  if (p.norm != SDVG_NORM_NONE) team.join(p, p.norm, moments(s, p.norm), &mean, &rstd);
+  const long long group = p.scale || p.shift ? (unsigned)r / (unsigned)p.mod_rows : 0;
+  const float* scale = p.scale ? p.scale + group * p.ld_mod : nullptr;
+  const float* shift = p.shift ? p.shift + group * p.ld_mod : nullptr;
+#pragma unroll
+  for (int i = 0; i < NI; ++i)
+    if (valid(i)) {
+      float o = p.norm != SDVG_NORM_NONE ? (s[i] - mean) * rstd : s[i];
+      if (p.weight) o *= __ldg(p.weight + col(i));
+      if (p.bias) o += __ldg(p.bias + col(i));
+      if (scale) o = fmaf(o, __ldg(scale + col(i)), o);
+      if (shift) o += __ldg(shift + col(i));
+      store_elem(p.out, r * p.ld_out + col(i), p.out_type, o);
+    }
+}
+
+// ---- rows that no team can hold: one CTA per row, which reads it once per statistic -----------------------------
+
+constexpr int kLongThreads = 512;
+
+// Sum over the CTA; every thread gets it.
+__device__ __forceinline__ float block_sum(float v, float* buf) {
+  v = warp_sum(v);
+  __syncthreads();                                     // the last sum's readers are done with buf
+  if ((threadIdx.x & 31) == 0) buf[threadIdx.x >> 5] = v;
+  __syncthreads();
+  return warp_sum(threadIdx.x % 32 < kLongThreads / 32 ? buf[threadIdx.x % 32] : 0.f);
+}
+
+// `value(c)` gives the row's column c; the mean is subtracted for a layer norm, and the variance is
 // taken from the centred values.
 template <class Value>
 __device__ __forceinline__ void row_stats(const NormParams& p, int kind, Value value, float* buf, float* mean, float* rstd) {
@@ -53,19 +483,19 @@ __device__ __forceinline__ void row_stats(const NormParams& p, int kind, Value v
   if (kind == SDVG_NORM_NONE) return;
   if (kind == SDVG_NORM_LAYER) {
     float s = 0.f;
-    for (int c = threadIdx.x; c < p.cols; c += kThreads) s += value(c);
+    for (int c = threadIdx.x; c < p.cols; c += kLongThreads) s += value(c);
     *mean = block_sum(s, buf) * p.inv_cols;
   }
   float q = 0.f;
-  for (int c = threadIdx.x; c < p.cols; c += kThreads) {
+  for (int c = threadIdx.x; c < p.cols; c += kLongThreads) {
     const float d = value(c) - *mean;
     q = fmaf(d, d, q);
   }
   *rstd = 1.f / sqrtf(block_sum(q, buf) * p.inv_cols + p.eps);
 }
 
-__global__ void __launch_bounds__(kThreads) gated_norm_kernel(const NormParams p) {
-  __shared__ float buf[kThreads / 32];
+__global__ void __launch_bounds__(kLongThreads) gated_norm_long_kernel(const NormParams p) {
+  __shared__ float buf[kLongThreads / 32];
   const long long r = blockIdx.x;
   const float* gate = p.gate ? p.gate + (r / p.gate_rows) * p.ld_gate : nullptr;
   const float* scale = p.scale ? p.scale + (r / p.mod_rows) * p.ld_mod : nullptr;
@@ -83,7 +513,7 @@ __global__ void __launch_bounds__(kThreads) gated_norm_kernel(const NormParams p
   };
   float mean = 0.f, rstd = 1.f;
   if (p.out) row_stats(p, p.norm, sum, buf, &mean, &rstd);
-  for (int c = threadIdx.x; c < p.cols; c += kThreads) {
+  for (int c = threadIdx.x; c < p.cols; c += kLongThreads) {
     const float s = sum(c);                          // read before either output is written: both may be in place
     if (p.x_out) store_elem(p.x_out, r * p.ld_x_out + c, p.x_type, s);
     if (!p.out) continue;
@@ -94,6 +524,82 @@ __global__ void __launch_bounds__(kThreads) gated_norm_kernel(const NormParams p
     if (shift) o += shift[c];
     store_elem(p.out, r * p.ld_out + c, p.out_type, o);
   }
+}
+
+// ---- host side -------------------------------------------------------------------------------
+
+int device_sms(int* sms) {
+  static thread_local int cached_dev = -1, cached = 0;
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e == cudaSuccess && dev != cached_dev) {
+    e = cudaDeviceGetAttribute(&cached, cudaDevAttrMultiProcessorCount, dev);
+    if (e == cudaSuccess) cached_dev = dev;
+  }
+  *sms = cached;
+  return sdvg::cuda_status(e);
+}
+
+constexpr int kMostDynamic = 200 * 1024;
+
+// -1: a team's ring does not fit
+template <int XW, int YW, int NI, bool WARP, bool FULL>
+int launch_team_as(const NormParams& p, int threads, int sms, cudaStream_t stream) {
+  const int rows_per_cta = WARP ? threads / 32 : 1;
+  const int want = (p.rows + rows_per_cta - 1) / rows_per_cta;
+  const int dynamic = threads * kSlots * (Ring<XW, NI>::kBytes + Ring<YW, NI>::kBytes);
+  if (dynamic > kMostDynamic) return -1;
+  cudaError_t e = cudaSuccess;
+  if (dynamic > 48 * 1024) {
+    e = cudaFuncSetAttribute(gated_norm_kernel<XW, YW, NI, WARP, FULL>, cudaFuncAttributeMaxDynamicSharedMemorySize, dynamic);
+    if (e != cudaSuccess) return sdvg::cuda_status(e);
+  }
+  int grid = want;
+  if (want > sms) {
+    // a grid that the device holds at once: teams walk rows of equal number
+    int resident = 0;
+    e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&resident, gated_norm_kernel<XW, YW, NI, WARP, FULL>, threads, dynamic);
+    if (e != cudaSuccess) return sdvg::cuda_status(e);
+    grid = std::min(want, sms * std::max(resident, 1));
+  }
+  gated_norm_kernel<XW, YW, NI, WARP, FULL><<<grid, threads, dynamic, stream>>>(p);
+  return sdvg::cuda_status(cudaGetLastError());
+}
+
+template <int XW, int YW, int NI, bool WARP>
+int launch_team(const NormParams& p, int threads, int sms, cudaStream_t stream) {
+  return p.cols == (WARP ? 32 : threads) * NI * 8 ? launch_team_as<XW, YW, NI, WARP, true>(p, threads, sms, stream)
+                                                  : launch_team_as<XW, YW, NI, WARP, false>(p, threads, sms, stream);
+}
+
+template <int XW, int YW>
+int launch_vec(const NormParams& p, int sms, cudaStream_t stream) {
+  const int vecs = p.cols / 8;
+  if (vecs <= 32) return launch_team<XW, YW, 1, true>(p, 128, sms, stream);
+  if (vecs <= 64) return launch_team<XW, YW, 2, true>(p, 128, sms, stream);
+  if (vecs <= 2 * kTeamThreads) return launch_team<XW, YW, 2, false>(p, (vecs + 63) / 64 * 32, sms, stream);
+  return -1;
+}
+
+int launch(const NormParams& p, bool vec, cudaStream_t stream) {
+  int sms = 0;
+  int st = device_sms(&sms);
+  if (st != SDVG_OK) return st;
+  st = -1;                                             // -1: a row does not fit the team
+  if (vec) {
+    const bool x4 = p.x_type == SDVG_F32, y4 = p.y && p.y_type == SDVG_F32;
+    if (!p.y) st = x4 ? launch_vec<4, 0>(p, sms, stream) : launch_vec<2, 0>(p, sms, stream);
+    else if (y4) st = x4 ? launch_vec<4, 4>(p, sms, stream) : launch_vec<2, 4>(p, sms, stream);
+    else st = x4 ? launch_vec<4, 2>(p, sms, stream) : launch_vec<2, 2>(p, sms, stream);
+    if (st != -1) return st;
+  } else if (p.cols <= 256 * 8) {
+    if (p.cols <= 256) gated_norm_single_kernel<1><<<p.rows, (p.cols + 31) / 32 * 32, 0, stream>>>(p);
+    else if (p.cols <= 1024) gated_norm_single_kernel<4><<<p.rows, ((p.cols + 3) / 4 + 31) / 32 * 32, 0, stream>>>(p);
+    else gated_norm_single_kernel<8><<<p.rows, ((p.cols + 7) / 8 + 31) / 32 * 32, 0, stream>>>(p);
+    return sdvg::cuda_status(cudaGetLastError());
+  }
+  gated_norm_long_kernel<<<p.rows, kLongThreads, 0, stream>>>(p);
+  return sdvg::cuda_status(cudaGetLastError());
 }
 
 bool aligned_to(const void* p, int bytes) { return (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(bytes - 1)) == 0; }
@@ -157,8 +663,18 @@ int sdvg_gated_norm(const void* x, int64_t ld_x, int x_type, const void* y, int6
   p.cols = cols;
   p.eps = eps;
   p.inv_cols = 1.f / (float)cols;
-  gated_norm_kernel<<<rows, kThreads, 0, (cudaStream_t)stream>>>(p);
-  return sdvg::cuda_status(cudaGetLastError());
+  // whole vectors: every address a row or a vector is read or written at is a multiple of 16 bytes
+  auto rows_ok = [&](const void* base, int64_t ld, int type) {
+    return !base || (sdvg::aligned16(base) && (rows == 1 || ld * sdvg::elem_bytes(type) % 16 == 0));
+  };
+  auto groups_ok = [&](const float* base, int64_t ld, int group_rows) {
+    return !base || (sdvg::aligned16(base) && (rows <= group_rows || ld % 4 == 0));
+  };
+  const bool vec = cols % 8 == 0 && rows_ok(x, ld_x, x_type) && rows_ok(y, ld_y, y_type) && rows_ok(x_out, ld_x_out, x_type) &&
+                   rows_ok(out, ld_out, out_type) && groups_ok(gate, ld_gate, gate_rows) && groups_ok(scale, ld_mod, mod_rows) &&
+                   groups_ok(shift, ld_mod, mod_rows) && sdvg::aligned16(post_weight) && sdvg::aligned16(weight) &&
+                   sdvg::aligned16(bias);
+  return launch(p, vec, (cudaStream_t)stream);
 }
 
 }  // extern "C"
