@@ -620,48 +620,53 @@ def sdvg_block_attn_fwd_e4m3_batched(q8s, k_self8s, v_self8s, caches, block_indi
 
 _ELEM_TYPES = {torch.bfloat16: SDVG_BF16, torch.float16: SDVG_F16, torch.float32: SDVG_F32}
 
+# The checks below sit on the path of calls whose kernels take a few microseconds: attributes are compared without building
+# intermediate objects, and the messages are only made for a call that is refused.
 
-def _matrix(t: Optional[torch.Tensor], like: torch.Tensor, rows: int, cols: int, dtype: torch.dtype, what: str):
-    """(pointer, row stride) of a [rows, cols] tensor with unit column stride on `like`'s device; (None, 0) for None."""
-    if t is None:
-        return None, 0
-    if t.dtype != dtype or t.device != like.device or t.shape != (rows, cols):
-        raise ValueError(f"{what}: expected {dtype} [{rows}, {cols}] on {like.device}, got {t.dtype} "
-                         f"{list(t.shape)} on {t.device}")
+
+def _matrix(t: torch.Tensor, dev: int, shape: tuple, dtype: torch.dtype, what: str):
+    """(pointer, row stride) of a matrix with unit column stride on CUDA device `dev`."""
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != dev:
+        raise ValueError(f"{what}: expected {dtype} {list(shape)} on cuda:{dev}, got {t.dtype} {list(t.shape)} on {t.device}")
     ld, step = t.stride()
-    if step != 1 and cols > 1:
+    if step != 1 and shape[1] > 1:
         raise ValueError(f"{what}: columns must be contiguous")
     return t.data_ptr(), ld
 
 
-def _vector(t: Optional[torch.Tensor], like: torch.Tensor, n: int, what: str):
+def _vector(t: Optional[torch.Tensor], dev: int, n: int, what: str):
     if t is None:
         return None
-    if t.dtype != torch.float32 or t.device != like.device or t.shape != (n,) or (t.stride(0) != 1 and n > 1):
-        raise ValueError(f"{what}: expected contiguous float32 [{n}] on {like.device}")
+    if t.dtype is not torch.float32 or t.shape != (n,) or t.get_device() != dev or not t.is_contiguous():
+        raise ValueError(f"{what}: expected contiguous float32 [{n}] on cuda:{dev}, got {t.dtype} {list(t.shape)} on {t.device}")
     return t.data_ptr()
 
 
-def _groups(t: Optional[torch.Tensor], like: torch.Tensor, rows: int, cols: int, group_rows: int, what: str):
+def _groups(t: Optional[torch.Tensor], dev: int, rows: int, cols: int, group_rows: int, what: str):
     """Vectors that change with the row group: one row per `group_rows` rows."""
     if t is None:
         return None, 0
     if group_rows < 1:
         raise ValueError(f"{what}: rows per group must be given")
-    return _matrix(t, like, -(-rows // group_rows), cols, torch.float32, what)
+    return _matrix(t, dev, (-(-rows // group_rows), cols), torch.float32, what)
 
 
-def _call_on(t: torch.Tensor, name: str, *args) -> None:
-    """Calls an entry point whose last argument is the stream, with `t`'s device current (streams and launches are the
-    current device's); the last of `args` is the caller's stream or None."""
+def _call_on(dev: int, fn, where: str, stream, *args) -> None:
+    """Calls an entry point, whose last argument is the stream, with CUDA device `dev` current: launches and the default
+    stream are the current device's."""
+    if dev != torch._C._cuda_getDevice():
+        with torch.cuda.device(dev):
+            return _call_on(dev, fn, where, stream, *args)
+    raw = torch._C._cuda_getCurrentRawStream(dev) if stream is None else _stream(stream)
+    status = fn(*args, raw)
+    if status != SDVG_OK:
+        raise SdvgError(status, where)
+
+
+def _device_of(t: torch.Tensor) -> int:
     if not t.is_cuda:
         raise ValueError("expected CUDA tensors")
-    fn = getattr(lib(), name)
-    if t.device.index == torch.cuda.current_device():
-        _check(fn(*args[:-1], _stream(args[-1])), name)
-    else:
-        with torch.cuda.device(t.device):
-            _check(fn(*args[:-1], _stream(args[-1])), name)
+    return t.get_device()
 
 
 def sdvg_linear(x, w, out, workspace, bias=None, act: int = SDVG_ACT_NONE, residual=None, gate=None, gate_rows: int = 0,
@@ -671,18 +676,20 @@ def sdvg_linear(x, w, out, workspace, bias=None, act: int = SDVG_ACT_NONE, resid
     (x and w: multiples of 8; residual may be one expanded row); residual may be `out`."""
     rows, inner = x.shape
     cols = w.shape[0]
-    if x.dtype not in (torch.bfloat16, torch.float16) or out.dtype not in _ELEM_TYPES:
-        raise ValueError("x must be bfloat16 or float16, out also float32")
-    xp, ld_x = _matrix(x, x, rows, inner, x.dtype, "x")
-    wp, ld_w = _matrix(w, x, cols, inner, x.dtype, "w")
-    op, ld_out = _matrix(out, x, rows, cols, out.dtype, "out")
-    rp, ld_res = _matrix(residual, x, rows, cols, out.dtype, "residual")
-    gp, ld_gate = _groups(gate, x, rows, cols, gate_rows, "gate")
-    if workspace.device != x.device:
+    in_type, out_type = _ELEM_TYPES.get(x.dtype), _ELEM_TYPES.get(out.dtype)
+    if in_type is None or in_type == SDVG_F32 or out_type is None:
+        raise ValueError("x must be bfloat16 or float16, out one of these or float32")
+    dev = _device_of(x)
+    if workspace.get_device() != dev:
         raise ValueError("workspace must be on the tensors' device")
-    _call_on(x, "sdvg_linear", xp, ld_x, wp, ld_w, _vector(bias, x, cols, "bias"), act, gp, ld_gate, gate_rows, rp, ld_res,
-             op, ld_out, rows, cols, inner, _ELEM_TYPES[x.dtype], _ELEM_TYPES[out.dtype], workspace.data_ptr(),
-             workspace.numel(), stream)
+    xp, ld_x = _matrix(x, dev, (rows, inner), x.dtype, "x")
+    wp, ld_w = _matrix(w, dev, (cols, inner), x.dtype, "w")
+    op, ld_out = _matrix(out, dev, (rows, cols), out.dtype, "out")
+    rp, ld_res = (None, 0) if residual is None else _matrix(residual, dev, (rows, cols), out.dtype, "residual")
+    gp, ld_gate = _groups(gate, dev, rows, cols, gate_rows, "gate")
+    _call_on(dev, lib().sdvg_linear, "sdvg_linear", stream, xp, ld_x, wp, ld_w, _vector(bias, dev, cols, "bias"), act, gp,
+             ld_gate, gate_rows, rp, ld_res, op, ld_out, rows, cols, inner, in_type, out_type, workspace.data_ptr(),
+             workspace.numel())
 
 
 def sdvg_gated_norm(x, out, y=None, gate=None, gate_rows: int = 0, post_norm: int = SDVG_NORM_NONE, post_weight=None,
@@ -692,54 +699,65 @@ def sdvg_gated_norm(x, out, y=None, gate=None, gate_rows: int = 0, post_norm: in
     out = (norm(s) * weight + bias) * (1 + scale[row // modulate_rows]) + shift[row // modulate_rows].
     x, y, x_out, out: [rows, cols] of bf16, fp16 or fp32 (x_out has x's type; out may be None when x_out is given);
     vectors fp32 [cols], gate / scale / shift fp32 [groups, cols]."""
-    rows, cols = x.shape
-    for t in (x, y, out):
-        if t is not None and t.dtype not in _ELEM_TYPES:
-            raise ValueError("expected bfloat16, float16 or float32 tensors")
-    xp, ld_x = _matrix(x, x, rows, cols, x.dtype, "x")
-    yp, ld_y = (None, 0) if y is None else _matrix(y, x, rows, cols, y.dtype, "y")
-    xo, ld_xo = _matrix(x_out, x, rows, cols, x.dtype, "x_out")
-    op, ld_out = (None, 0) if out is None else _matrix(out, x, rows, cols, out.dtype, "out")
-    gp, ld_gate = _groups(gate, x, rows, cols, gate_rows, "gate")
-    sp, ld_mod = _groups(scale, x, rows, cols, modulate_rows, "scale")
-    hp, ld_shift = _groups(shift, x, rows, cols, modulate_rows, "shift")
-    if sp is not None and hp is not None and ld_mod != ld_shift and rows > modulate_rows:
+    shape = x.shape
+    rows, cols = shape
+    types = _ELEM_TYPES
+    if x.dtype not in types or (y is not None and y.dtype not in types) or (out is not None and out.dtype not in types):
+        raise ValueError("expected bfloat16, float16 or float32 tensors")
+    dev = _device_of(x)
+    xp, ld_x = _matrix(x, dev, shape, x.dtype, "x")
+    yp, ld_y, y_type = None, 0, 0
+    if y is not None:
+        yp, ld_y = _matrix(y, dev, shape, y.dtype, "y")
+        y_type = types[y.dtype]
+    xo, ld_xo = (None, 0) if x_out is None else _matrix(x_out, dev, shape, x.dtype, "x_out")
+    op, ld_out, out_type = None, 0, 0
+    if out is not None:
+        op, ld_out = _matrix(out, dev, shape, out.dtype, "out")
+        out_type = types[out.dtype]
+    gp, ld_gate = _groups(gate, dev, rows, cols, gate_rows, "gate")
+    sp, ld_mod = _groups(scale, dev, rows, cols, modulate_rows, "scale")
+    hp, ld_shift = _groups(shift, dev, rows, cols, modulate_rows, "shift")
+    if sp is None:
+        ld_mod = ld_shift
+    elif hp is not None and ld_mod != ld_shift and rows > modulate_rows:
         raise ValueError("scale and shift must have the same row stride")
-    _call_on(x, "sdvg_gated_norm", xp, ld_x, _ELEM_TYPES[x.dtype], yp, ld_y, 0 if y is None else _ELEM_TYPES[y.dtype],
-             post_norm, _vector(post_weight, x, cols, "post_weight"), gp, ld_gate, gate_rows, xo, ld_xo, norm,
-             _vector(weight, x, cols, "weight"), _vector(bias, x, cols, "bias"), sp, hp, ld_mod if sp is not None else ld_shift,
-             modulate_rows, eps, op, ld_out, 0 if out is None else _ELEM_TYPES[out.dtype], rows, cols, stream)
+    _call_on(dev, lib().sdvg_gated_norm, "sdvg_gated_norm", stream, xp, ld_x, types[x.dtype], yp, ld_y, y_type, post_norm,
+             _vector(post_weight, dev, cols, "post_weight"), gp, ld_gate, gate_rows, xo, ld_xo, norm,
+             _vector(weight, dev, cols, "weight"), _vector(bias, dev, cols, "bias"), sp, hp, ld_mod, modulate_rows, eps, op,
+             ld_out, out_type, rows, cols)
 
 
-def _tokens(t: Optional[torch.Tensor], cache: Cache, what: str):
+def _tokens(t: torch.Tensor, dev: int, shape: tuple, what: str, contiguous: bool = False):
     """(pointer, token stride) of a bf16 [block_tokens, heads, head_dim] tensor that is contiguous within a token."""
-    if t is None:
-        return None, 0
-    shape = (cache.block_tokens, cache.heads, cache.head_dim)
-    if t.dtype != torch.bfloat16 or t.shape != shape or t.device != cache._k_raw.device:
-        raise ValueError(f"{what}: expected bfloat16 {list(shape)} on {cache._k_raw.device}")
+    if t.dtype is not torch.bfloat16 or t.shape != shape or t.get_device() != dev:
+        raise ValueError(f"{what}: expected bfloat16 {list(shape)} on cuda:{dev}, got {t.dtype} {list(t.shape)} on {t.device}")
+    tokens, heads, dim = shape
     ld, head, step = t.stride()
-    if step != 1 or (head != cache.head_dim and cache.heads > 1):
+    if step != 1 or (head != dim and heads > 1):
         raise ValueError(f"{what}: the heads of a token must be contiguous")
-    return t.data_ptr(), ld if cache.block_tokens > 1 else cache.heads * cache.head_dim
+    if tokens == 1:
+        ld = heads * dim
+    if contiguous and ld != heads * dim:
+        raise ValueError(f"{what} must be contiguous")
+    return t.data_ptr(), ld
 
 
 def sdvg_qk_norm_rope3d_commit(cache: Cache, q, k, v, q_weight, k_weight, scope: int, eps: float, q_out, k_out, grid,
                                frame_offset: int, table, tab_frames: int, block_index: int, flags: int, stream=None) -> int:
     """sdvg_rope3d_qk_commit with an RMS norm of q and k first; q, k, v may be column ranges of a wider QKV product
     viewed as [tokens, heads, head_dim].  Returns the evicted block."""
-    width = cache.heads * cache.head_dim if scope == SDVG_SCOPE_ROW else cache.head_dim
-    dev = cache._k_raw
-    (qp, ld_q), (kp, ld_k), (vp, ld_v) = _tokens(q, cache, "q"), _tokens(k, cache, "k"), _tokens(v, cache, "v")
-    outs = []
-    for t, what in ((q_out, "q_out"), (k_out, "k_out")):
-        p, ld = _tokens(t, cache, what)
-        if t is not None and ld != cache.heads * cache.head_dim:
-            raise ValueError(f"{what} must be contiguous")
-        outs.append(p)
+    shape = (cache.block_tokens, cache.heads, cache.head_dim)
+    width = shape[1] * shape[2] if scope == SDVG_SCOPE_ROW else shape[2]
+    dev = cache._k_raw.get_device()
+    qp, ld_q = (None, 0) if q is None else _tokens(q, dev, shape, "q")
+    kp, ld_k = _tokens(k, dev, shape, "k")
+    vp, ld_v = _tokens(v, dev, shape, "v")
+    qo = None if q_out is None else _tokens(q_out, dev, shape, "q_out", True)[0]
+    ko = None if k_out is None else _tokens(k_out, dev, shape, "k_out", True)[0]
     frames, grid_h, grid_w = grid
     ev = _I64(-1)
-    _call_on(dev, "sdvg_qk_norm_rope3d_commit", cache.handle, qp, ld_q, kp, ld_k, vp, ld_v,
-             _vector(q_weight, dev, width, "q_weight"), _vector(k_weight, dev, width, "k_weight"), scope, eps, outs[0],
-             outs[1], frames, grid_h, grid_w, frame_offset, _ptr(table), tab_frames, block_index, flags, C.byref(ev), stream)
+    _call_on(dev, lib().sdvg_qk_norm_rope3d_commit, "sdvg_qk_norm_rope3d_commit", stream, cache.handle, qp, ld_q, kp, ld_k,
+             vp, ld_v, _vector(q_weight, dev, width, "q_weight"), _vector(k_weight, dev, width, "k_weight"), scope, eps, qo,
+             ko, frames, grid_h, grid_w, frame_offset, _ptr(table), tab_frames, block_index, flags, C.byref(ev))
     return ev.value

@@ -14,12 +14,14 @@
 #include <algorithm>
 
 #include "elem_types.cuh"
+#include "row_team.cuh"
 #include "sdvg_internal.h"
 
 namespace {
 
 using sdvg::load_elem;
 using sdvg::store_elem;
+using namespace rows;
 
 struct NormParams {
   const void* x;
@@ -37,121 +39,12 @@ struct NormParams {
   int post, norm;
   int gate_rows, mod_rows;
   int rows, cols;
-  float eps, inv_cols;
+  float eps, inv_cols, num_cols;
 };
 
 // Sum and centred sum of squares of a part of a row: parts combine without the cancellation of a difference of squares.
 struct Moments {
   float sum, m2;
-};
-
-__device__ __forceinline__ float warp_sum(float v) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-  return v;
-}
-
-__device__ __forceinline__ float bf16_lo(uint32_t u) { return __uint_as_float(u << 16); }
-__device__ __forceinline__ float bf16_hi(uint32_t u) { return __uint_as_float(u & 0xffff0000u); }
-
-// Eight columns as four packed pairs of fp32.
-typedef unsigned long long Pair;
-struct Vec8 {
-  Pair p[4];
-};
-__device__ __forceinline__ Pair pair_of(float lo, float hi) {
-  Pair r;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
-  return r;
-}
-__device__ __forceinline__ float2 floats_of(Pair a) {
-  float2 f;
-  asm("mov.b64 {%0, %1}, %2;" : "=f"(f.x), "=f"(f.y) : "l"(a));
-  return f;
-}
-__device__ __forceinline__ Pair add2(Pair a, Pair b) {
-  Pair r;
-  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-  return r;
-}
-__device__ __forceinline__ Pair fma2(Pair a, Pair b, Pair c) {
-  Pair r;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
-  return r;
-}
-
-__device__ __forceinline__ void unpack8(const uint4& a, int type, Vec8& v) {
-  const uint32_t w[4] = {a.x, a.y, a.z, a.w};
-  if (type == SDVG_BF16) {
-#pragma unroll
-    for (int j = 0; j < 4; ++j) v.p[j] = pair_of(bf16_lo(w[j]), bf16_hi(w[j]));
-  } else {
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[j]));
-      v.p[j] = pair_of(f.x, f.y);
-    }
-  }
-}
-
-__device__ __forceinline__ void store8(char* at, int type, const Vec8& v) {
-  float2 f[4];
-#pragma unroll
-  for (int j = 0; j < 4; ++j) f[j] = floats_of(v.p[j]);
-  if (type == SDVG_F32) {
-    float4* o = reinterpret_cast<float4*>(at);
-    __stcs(o, make_float4(f[0].x, f[0].y, f[1].x, f[1].y));
-    __stcs(o + 1, make_float4(f[2].x, f[2].y, f[3].x, f[3].y));
-    return;
-  }
-  uint32_t w[4];
-  if (type == SDVG_BF16) {
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const __nv_bfloat162 h = __floats2bfloat162_rn(f[j].x, f[j].y);
-      w[j] = *reinterpret_cast<const uint32_t*>(&h);
-    }
-  } else {
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const __half2 h = __floats2half2_rn(f[j].x, f[j].y);
-      w[j] = *reinterpret_cast<const uint32_t*>(&h);
-    }
-  }
-  __stcs(reinterpret_cast<uint4*>(at), make_uint4(w[0], w[1], w[2], w[3]));
-}
-
-__device__ __forceinline__ void copy16(void* smem, const void* src) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(smem)), "l"(src)
-               : "memory");
-}
-__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N>
-__device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
-
-// A thread's pieces of a tensor's next rows, W bytes per element (0: no such tensor): piece i of ring slot s is W / 2
-// vectors of 16 bytes, the warp's 32 threads side by side.
-template <int W, int NI>
-struct Ring {
-  static constexpr int kVecs = W / 2;
-  static constexpr int kBytes = NI * kVecs * 16;       // per thread and slot
-  uint4* mine;                                         // this thread's first vector
-  __device__ __forceinline__ uint4* at(int slot, int i, int h) const { return mine + ((slot * NI + i) * kVecs + h) * 32; }
-  __device__ __forceinline__ void request(int slot, int i, const char* row) const {
-#pragma unroll
-    for (int h = 0; h < kVecs; ++h) copy16(at(slot, i, h), row + (i * 256 * W + 16 * h));
-  }
-  __device__ __forceinline__ void values(int slot, int i, int type, Vec8& v) const {
-    if constexpr (W == 2) {
-      unpack8(*at(slot, i, 0), type, v);
-    } else if constexpr (W == 4) {
-      const float4 a = *reinterpret_cast<const float4*>(at(slot, i, 0)), b = *reinterpret_cast<const float4*>(at(slot, i, 1));
-      v.p[0] = pair_of(a.x, a.y);
-      v.p[1] = pair_of(a.z, a.w);
-      v.p[2] = pair_of(b.x, b.y);
-      v.p[3] = pair_of(b.z, b.w);
-    }
-  }
 };
 
 constexpr int kSlots = 2;                              // rows on their way per team
@@ -188,7 +81,7 @@ struct Team {
       }
       turn ^= 1;
     }
-    *mean = m.sum * p.inv_cols;
+    *mean = m.sum / p.num_cols;                        // a division: a constant row's mean is that constant
     *rstd = rsqrtf(fmaf(m.m2, p.inv_cols, p.eps));
   }
 };
@@ -230,11 +123,10 @@ __device__ __forceinline__ Moments warp_moments(const Vec8 (&v)[NI], int kind, f
 template <int NI>
 __device__ __forceinline__ void apply_norm(Vec8 (&v)[NI], float mean, float rstd) {
   const Pair r = pair_of(rstd, rstd), c = pair_of(-mean, -mean);
-  const Pair zero = pair_of(-0.f, -0.f);               // x * r + -0 is x * r to the bit
 #pragma unroll
   for (int i = 0; i < NI; ++i)
 #pragma unroll
-    for (int j = 0; j < 4; ++j) v[i].p[j] = fma2(add2(v[i].p[j], c), r, zero);
+    for (int j = 0; j < 4; ++j) v[i].p[j] = mul2(add2(v[i].p[j], c), r);
 }
 
 // Rows of aligned vectors.  XW and YW: bytes of x's and y's elements (YW = 0: no y).  A thread holds NI pieces of 8 columns; the
@@ -385,30 +277,65 @@ __global__ void __launch_bounds__(WARP ? 128 : kTeamThreads) gated_norm_kernel(c
   copy_wait<0>();
 }
 
+// Single columns of a row, 32 apart, of any type: the type is looked at once per row, not per element.
+template <int NI, class Valid>
+__device__ __forceinline__ void load_singles(float (&v)[NI], const void* base, long long at, int type, Valid valid) {
+  if (type == SDVG_F32) {
+    const float* s = static_cast<const float*>(base) + at;
+#pragma unroll
+    for (int i = 0; i < NI; ++i) v[i] = valid(i) ? s[32 * i] : 0.f;
+  } else {
+    const uint16_t* s = static_cast<const uint16_t*>(base) + at;
+    uint16_t h[NI];
+#pragma unroll
+    for (int i = 0; i < NI; ++i) h[i] = valid(i) ? s[32 * i] : 0;
+    if (type == SDVG_BF16) {
+#pragma unroll
+      for (int i = 0; i < NI; ++i) v[i] = __uint_as_float((uint32_t)h[i] << 16);
+    } else {
+#pragma unroll
+      for (int i = 0; i < NI; ++i) v[i] = __half2float(__ushort_as_half(h[i]));
+    }
+  }
+}
+template <int NI, class Valid>
+__device__ __forceinline__ void store_singles(const float (&v)[NI], void* base, long long at, int type, Valid valid) {
+  if (type == SDVG_F32) {
+    float* o = static_cast<float*>(base) + at;
+#pragma unroll
+    for (int i = 0; i < NI; ++i)
+      if (valid(i)) o[32 * i] = v[i];
+  } else {
+    uint16_t* o = static_cast<uint16_t*>(base) + at;
+    uint16_t h[NI];
+    if (type == SDVG_BF16) {
+#pragma unroll
+      for (int i = 0; i < NI; ++i) h[i] = __bfloat16_as_ushort(__float2bfloat16_rn(v[i]));
+    } else {
+#pragma unroll
+      for (int i = 0; i < NI; ++i) h[i] = __half_as_ushort(__float2half_rn(v[i]));
+    }
+#pragma unroll
+    for (int i = 0; i < NI; ++i)
+      if (valid(i)) o[32 * i] = h[i];
+  }
+}
+
 // Rows that are not made of aligned vectors: one CTA per row, NI single columns per thread; what is in flight comes from the
 // CTAs of an SM.
 template <int NI>
-__global__ void __launch_bounds__(256) gated_norm_single_kernel(const NormParams p) {
+__global__ void __launch_bounds__(NI == 16 ? 512 : 256) gated_norm_single_kernel(const NormParams p) {
   __shared__ Moments s_part[2][32];
   __shared__ float s_count[32];
   const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+  const int c0 = warp * 32 * NI + lane;                // first column; piece i: c0 + 32 i
   const long long r = blockIdx.x;
-  auto col = [&](int i) { return (int)(i * blockDim.x + threadIdx.x); };
-  auto valid = [&](int i) { return col(i) < p.cols; };
+  auto valid = [&](int i) { return c0 + 32 * i < p.cols; };
   float s[NI], y[NI];
-#pragma unroll
-  for (int i = 0; i < NI; ++i) {
-    if (valid(i)) s[i] = load_elem(p.x, r * p.ld_x + col(i), p.x_type);
-  }
-  if (p.y) {
-#pragma unroll
-    for (int i = 0; i < NI; ++i)
-      if (valid(i)) y[i] = load_elem(p.y, r * p.ld_y + col(i), p.y_type);
-  }
-  float own = 0.f;
-#pragma unroll
-  for (int i = 0; i < NI; ++i) own += valid(i) ? 1.f : 0.f;
-  const float count = warp_sum(own), inv_count = count > 0.f ? 1.f / count : 0.f;
+  load_singles<NI>(s, p.x, r * p.ld_x + c0, p.x_type, valid);
+  if (p.y) load_singles<NI>(y, p.y, r * p.ld_y + c0, p.y_type, valid);
+  const int left = p.cols - warp * 32 * NI;
+  const float count = (float)max(0, min(left, 32 * NI)), inv_count = count > 0.f ? 1.f / count : 0.f;
   if (lane == 0) s_count[warp] = count;
   Team<false> team{s_part, s_count};
   auto moments = [&](const float (&v)[NI], int kind) {
@@ -427,38 +354,40 @@ __global__ void __launch_bounds__(256) gated_norm_single_kernel(const NormParams
     m.m2 = warp_sum(m.m2);
     return m;
   };
+  // f(i, element of the vector at this piece)
+  auto with_vector = [&](const float* vec, auto f) {
+    if (!vec) return;
+#pragma unroll
+    for (int i = 0; i < NI; ++i) f(i, valid(i) ? __ldg(vec + c0 + 32 * i) : 0.f);
+  };
   float mean = 0.f, rstd = 1.f;
   if (p.y) {
-    if (p.post != SDVG_NORM_NONE) team.join(p, p.post, moments(y, p.post), &mean, &rstd);
-    const float* gate = p.gate ? p.gate + ((unsigned)r / (unsigned)p.gate_rows) * p.ld_gate : nullptr;
+    if (p.post != SDVG_NORM_NONE) {
+      team.join(p, p.post, moments(y, p.post), &mean, &rstd);
 #pragma unroll
-    for (int i = 0; i < NI; ++i)
-      if (valid(i)) {
-        float v = p.post != SDVG_NORM_NONE ? (y[i] - mean) * rstd : y[i];
-        if (p.post_weight) v *= __ldg(p.post_weight + col(i));
-        s[i] = gate ? fmaf(__ldg(gate + col(i)), v, s[i]) : s[i] + v;
-      }
-  }
-  if (p.x_out) {
-#pragma unroll
-    for (int i = 0; i < NI; ++i)
-      if (valid(i)) store_elem(p.x_out, r * p.ld_x_out + col(i), p.x_type, s[i]);
-  }
-  if (!p.out) return;
-  if (p.norm != SDVG_NORM_NONE) team.join(p, p.norm, moments(s, p.norm), &mean, &rstd);
-  const long long group = p.scale || p.shift ? (unsigned)r / (unsigned)p.mod_rows : 0;
-  const float* scale = p.scale ? p.scale + group * p.ld_mod : nullptr;
-  const float* shift = p.shift ? p.shift + group * p.ld_mod : nullptr;
-#pragma unroll
-  for (int i = 0; i < NI; ++i)
-    if (valid(i)) {
-      float o = p.norm != SDVG_NORM_NONE ? (s[i] - mean) * rstd : s[i];
-      if (p.weight) o *= __ldg(p.weight + col(i));
-      if (p.bias) o += __ldg(p.bias + col(i));
-      if (scale) o = fmaf(o, __ldg(scale + col(i)), o);
-      if (shift) o += __ldg(shift + col(i));
-      store_elem(p.out, r * p.ld_out + col(i), p.out_type, o);
+      for (int i = 0; i < NI; ++i) y[i] = (y[i] - mean) * rstd;
     }
+    with_vector(p.post_weight, [&](int i, float w) { y[i] *= w; });
+    if (p.gate) {
+      with_vector(p.gate + ((unsigned)r / (unsigned)p.gate_rows) * p.ld_gate, [&](int i, float g) { s[i] = fmaf(g, y[i], s[i]); });
+    } else {
+#pragma unroll
+      for (int i = 0; i < NI; ++i) s[i] += y[i];
+    }
+  }
+  if (p.x_out) store_singles<NI>(s, p.x_out, r * p.ld_x_out + c0, p.x_type, valid);
+  if (!p.out) return;
+  if (p.norm != SDVG_NORM_NONE) {
+    team.join(p, p.norm, moments(s, p.norm), &mean, &rstd);
+#pragma unroll
+    for (int i = 0; i < NI; ++i) s[i] = (s[i] - mean) * rstd;
+  }
+  const long long group = p.scale || p.shift ? (unsigned)r / (unsigned)p.mod_rows : 0;
+  with_vector(p.weight, [&](int i, float f) { s[i] *= f; });
+  with_vector(p.bias, [&](int i, float f) { s[i] += f; });
+  with_vector(p.scale ? p.scale + group * p.ld_mod : nullptr, [&](int i, float f) { s[i] = fmaf(s[i], f, s[i]); });
+  with_vector(p.shift ? p.shift + group * p.ld_mod : nullptr, [&](int i, float f) { s[i] += f; });
+  store_singles<NI>(s, p.out, r * p.ld_out + c0, p.out_type, valid);
 }
 
 // ---- rows that no team can hold: one CTA per row, which reads it once per statistic -----------------------------
@@ -484,7 +413,7 @@ __device__ __forceinline__ void row_stats(const NormParams& p, int kind, Value v
   if (kind == SDVG_NORM_LAYER) {
     float s = 0.f;
     for (int c = threadIdx.x; c < p.cols; c += kLongThreads) s += value(c);
-    *mean = block_sum(s, buf) * p.inv_cols;
+    *mean = block_sum(s, buf) / p.num_cols;
   }
   float q = 0.f;
   for (int c = threadIdx.x; c < p.cols; c += kLongThreads) {
@@ -549,17 +478,22 @@ int launch_team_as(const NormParams& p, int threads, int sms, cudaStream_t strea
   const int want = (p.rows + rows_per_cta - 1) / rows_per_cta;
   const int dynamic = threads * kSlots * (Ring<XW, NI>::kBytes + Ring<YW, NI>::kBytes);
   if (dynamic > kMostDynamic) return -1;
-  cudaError_t e = cudaSuccess;
-  if (dynamic > 48 * 1024) {
-    e = cudaFuncSetAttribute(gated_norm_kernel<XW, YW, NI, WARP, FULL>, cudaFuncAttributeMaxDynamicSharedMemorySize, dynamic);
-    if (e != cudaSuccess) return sdvg::cuda_status(e);
-  }
   int grid = want;
-  if (want > sms) {
-    // a grid that the device holds at once: teams walk rows of equal number
-    int resident = 0;
-    e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&resident, gated_norm_kernel<XW, YW, NI, WARP, FULL>, threads, dynamic);
+  if (want > sms || dynamic > 48 * 1024) {
+    // a grid that the device holds at once: teams walk rows of equal number.  Asked again when the shape changes.
+    static thread_local int known_dev = -1, known_dynamic = -1, resident = 0;
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return sdvg::cuda_status(e);
+    if (dev != known_dev || dynamic != known_dynamic) {
+      auto kernel = gated_norm_kernel<XW, YW, NI, WARP, FULL>;
+      known_dev = -1;
+      if (dynamic > 48 * 1024) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostDynamic);
+      if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&resident, kernel, threads, dynamic);
+      if (e != cudaSuccess) return sdvg::cuda_status(e);
+      known_dev = dev;
+      known_dynamic = dynamic;                         // a multiple of the thread count for each instance
+    }
     grid = std::min(want, sms * std::max(resident, 1));
   }
   gated_norm_kernel<XW, YW, NI, WARP, FULL><<<grid, threads, dynamic, stream>>>(p);
@@ -592,10 +526,11 @@ int launch(const NormParams& p, bool vec, cudaStream_t stream) {
     else if (y4) st = x4 ? launch_vec<4, 4>(p, sms, stream) : launch_vec<2, 4>(p, sms, stream);
     else st = x4 ? launch_vec<4, 2>(p, sms, stream) : launch_vec<2, 2>(p, sms, stream);
     if (st != -1) return st;
-  } else if (p.cols <= 256 * 8) {
+  } else if (p.cols <= 512 * 16) {
     if (p.cols <= 256) gated_norm_single_kernel<1><<<p.rows, (p.cols + 31) / 32 * 32, 0, stream>>>(p);
     else if (p.cols <= 1024) gated_norm_single_kernel<4><<<p.rows, ((p.cols + 3) / 4 + 31) / 32 * 32, 0, stream>>>(p);
-    else gated_norm_single_kernel<8><<<p.rows, ((p.cols + 7) / 8 + 31) / 32 * 32, 0, stream>>>(p);
+    else if (p.cols <= 2048) gated_norm_single_kernel<8><<<p.rows, ((p.cols + 7) / 8 + 31) / 32 * 32, 0, stream>>>(p);
+    else gated_norm_single_kernel<16><<<p.rows, ((p.cols + 15) / 16 + 31) / 32 * 32, 0, stream>>>(p);
     return sdvg::cuda_status(cudaGetLastError());
   }
   gated_norm_long_kernel<<<p.rows, kLongThreads, 0, stream>>>(p);
@@ -663,6 +598,7 @@ int sdvg_gated_norm(const void* x, int64_t ld_x, int x_type, const void* y, int6
   p.cols = cols;
   p.eps = eps;
   p.inv_cols = 1.f / (float)cols;
+  p.num_cols = (float)cols;
   // whole vectors: every address a row or a vector is read or written at is a multiple of 16 bytes
   auto rows_ok = [&](const void* base, int64_t ld, int type) {
     return !base || (sdvg::aligned16(base) && (rows == 1 || ld * sdvg::elem_bytes(type) % 16 == 0));
