@@ -46,6 +46,7 @@ struct alignas(64) LinearParams {
   int rows, cols;
   int act;
   int tile_t, tiles_f, tiles_t, k_iters, stages;
+  int split;                                         // CTAs (a cluster) that share a tile's sum; tiles only
   int group;                                         // feature tiles of a group of the tile order (pairs)
   long long tiles;
   uint32_t idesc;
@@ -205,30 +206,105 @@ struct RingPos {
   }
 };
 
+// fp32 outputs: the tensor core adds a product to the accumulator by truncation, so a sum over `inner` drifts in one
+// direction by about 2^-26 of its magnitude per 16 products (measured 3.7e-6 relative for inner = 5120, fp32's own
+// rounding giving 1e-7).  That is far below the rounding of a 16-bit output but not of an fp32 one, so there the sum is
+// cut into chunks of kChunkK: each chunk gets a fresh accumulator, and the epilogue warps add the chunks with
+// round-to-nearest into a total that stays in tensor memory.
+constexpr int kChunkK = 1024;
+constexpr int kChunkIters = kChunkK / kTileK;
+
+// ---- few tokens: a cluster per tile, which splits `inner` ---------------------------------------
+//
+// One tile is 128 features x tile_t tokens.  With few tokens there are few tiles and each is a long sum, bound by how fast
+// the weights arrive: the CTAs of a cluster each take a part of `inner`, leave their sums in shared memory, and after a
+// cluster barrier every CTA adds up its share of the tokens from all of them (distributed shared memory, always in the
+// order of the ranks) and runs the epilogue on it.  No workspace, no atomics, equal calls give equal bits.
+constexpr int kTileThreads = 192;                    // four epilogue warps, producer, issuer
+constexpr int kMaxSplit = 8;                         // portable cluster size
+
 struct TileSmem {
-  uint64_t full[kMaxStages], empty[kMaxStages], done;
+  uint64_t full[kMaxStages], empty[kMaxStages], acc_full, acc_empty;
   uint32_t tmem;
 };
 
-// One CTA per tile of 128 features x tile_t tokens: warp 0 fetches, warp 1 issues the products, then all four warps
-// run the epilogue (32 features each).
+// Tensor memory columns: the accumulator, and the total if there are several chunks; a power of two.
+__host__ __device__ constexpr uint32_t tile_tmem_cols(int tile_t, bool with_total) {
+  uint32_t cols = 32;
+  while (cols < (uint32_t)tile_t * (with_total ? 2 : 1)) cols *= 2;
+  return cols;
+}
+
+// Drains the accumulators (BUFFERS of them in turn, the total behind them) of all chunks but the last into the total: a warp's 32 features, its columns below `cols` in sets
+// of 16 from column_of(0), column_of(1) ..., which rise.  Returns false when a wait gave up.  `release` tells the issuer
+// that an accumulator is free again.
+template <int BUFFERS, class Column, class Release>
+__device__ __forceinline__ bool add_chunks(int chunks, uint32_t lanes, int acc_stride, Column column_of, int cols, RingPos& r,
+                                           uint64_t* acc_full, unsigned int* status, Release release) {
+  for (int c = 0; c < chunks - 1; ++c) {
+    if (!__all_sync(0xffffffffu, wait_for(&acc_full[r.stage], r.phase, status, kWaitLimitNs))) return false;
+    tc_fence_after();
+    const uint32_t part = lanes + r.stage * acc_stride, total = lanes + BUFFERS * acc_stride;
+#pragma unroll 1
+    for (int i = 0; column_of(i) < cols; ++i) {
+      const int col = column_of(i);
+      float v[16], sum[16];
+      tmem_ld16(part + col, reinterpret_cast<uint32_t(&)[16]>(v));
+      if (c > 0) tmem_ld16(total + col, reinterpret_cast<uint32_t(&)[16]>(sum));
+      tmem_wait_ld();
+      if (c > 0) {
+#pragma unroll
+        for (int j = 0; j < 16; ++j) v[j] += sum[j];
+      }
+      tmem_st16(total + col, reinterpret_cast<uint32_t(&)[16]>(v));
+    }
+    tmem_wait_st();
+    tc_fence_before();
+    __syncwarp();
+    release(r.stage);
+    r.next(BUFFERS);
+  }
+  return true;
+}
+
+// The accumulator of the last chunk plus the total of the others, 16 columns.
+template <int BUFFERS>
+__device__ __forceinline__ void load_sum16(float (&acc)[16], uint32_t lanes, int acc_stride, int stage, int col, bool with_total) {
+  tmem_ld16(lanes + stage * acc_stride + col, reinterpret_cast<uint32_t(&)[16]>(acc));
+  if (with_total) {
+    float sum[16];
+    tmem_ld16(lanes + BUFFERS * acc_stride + col, reinterpret_cast<uint32_t(&)[16]>(sum));
+    tmem_wait_ld();
+#pragma unroll
+    for (int j = 0; j < 16; ++j) acc[j] += sum[j];
+  }
+  tmem_wait_ld();
+}
+
 template <int OutType>
-__global__ void __launch_bounds__(128) linear_tile_kernel(const __grid_constant__ LinearParams p) {
+__global__ void __launch_bounds__(kTileThreads) linear_tile_kernel(const __grid_constant__ LinearParams p) {
+  constexpr bool kChunked = OutType == SDVG_F32;
+  using T = typename OutElem<OutType>::T;
   extern __shared__ uint8_t raw[];
   __shared__ TileSmem sm;
   uint8_t* buf = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-  const int n0 = (blockIdx.x % p.tiles_f) * kTileF;
-  const int m0 = (blockIdx.x / p.tiles_f) * p.tile_t;
+  const int rank = p.split > 1 ? (int)cluster_ctarank() : 0, tile = blockIdx.x / p.split;
+  const int n0 = (tile % p.tiles_f) * kTileF;
+  const int m0 = (tile / p.tiles_f) * p.tile_t, m_end = min(p.rows, m0 + p.tile_t);
   const int w_bytes = kTileF * 128, stage_bytes = w_bytes + p.tile_t * 128;
-  uint32_t tmem_cols = 32;
-  while (tmem_cols < (uint32_t)p.tile_t) tmem_cols *= 2;
+  // this CTA's part of `inner`: never empty
+  const int share = p.k_iters / p.split, rest = p.k_iters % p.split;
+  const int k0 = rank * share + min(rank, rest), iters = share + (rank < rest ? 1 : 0);
+  const int chunks = kChunked ? (iters + kChunkIters - 1) / kChunkIters : 1;
+  const uint32_t tmem_cols = tile_tmem_cols(p.tile_t, kChunked && p.k_iters > kChunkIters);
   if (threadIdx.x == 0) {
     for (int s = 0; s < p.stages; ++s) {
       mbar_init(&sm.full[s], 1);
       mbar_init(&sm.empty[s], 1);
     }
-    mbar_init(&sm.done, 1);
+    mbar_init(&sm.acc_full, 1);
+    mbar_init(&sm.acc_empty, 4);
     fence_mbar_init();
     prefetch_tmap(&p.w_map);
     prefetch_tmap(&p.x_map);
@@ -242,56 +318,106 @@ __global__ void __launch_bounds__(128) linear_tile_kernel(const __grid_constant_
   tc_fence_after();
   const uint32_t tmem = sm.tmem;
 
-  if (warp == 0) {
+  if (warp == 4) {
     if (elect_one()) {
       int i = 0;
       RingPos r;
-      for (; i < p.k_iters; ++i, r.next(p.stages)) {
+      for (; i < iters; ++i, r.next(p.stages)) {
         const int s = r.stage;
         if (!wait_for(&sm.empty[s], r.phase ^ 1, p.status, kWaitLimitNs)) break;
         uint8_t* st = buf + s * stage_bytes;
         mbar_expect_tx(&sm.full[s], stage_bytes);
-        tma_load_2d(st, &p.w_map, &sm.full[s], i * kTileK, n0);
-        tma_load_2d(st + w_bytes, &p.x_map, &sm.full[s], i * kTileK, m0);
+        tma_load_2d(st, &p.w_map, &sm.full[s], (k0 + i) * kTileK, n0);
+        tma_load_2d(st + w_bytes, &p.x_map, &sm.full[s], (k0 + i) * kTileK, m0);
       }
-      if (i < p.k_iters)                             // gave up: see the copies in flight land before the CTA may leave
+      if (i < iters)                                   // gave up: see the copies in flight land before the CTA may leave
         for (int j = min(i, p.stages); j > 0; --j) {
           r.back(p.stages);
           wait_for(&sm.full[r.stage], r.phase, p.status, kWaitLimitNs);
         }
     }
-  } else if (warp == 1) {
+    __syncwarp();
+  } else if (warp == 5) {
     if (elect_one()) {
       bool ok = true;
-      RingPos r;
-      for (int i = 0; i < p.k_iters; ++i, r.next(p.stages)) {
-        const int s = r.stage;
-        if (!(ok = wait_for(&sm.full[s], r.phase, p.status, kWaitLimitNs))) break;
+      RingPos r, acc;
+      for (int c = 0; ok && c < chunks; ++c, acc.next(1)) {
+        if (!(ok = wait_for(&sm.acc_empty, acc.phase ^ 1, p.status, kWaitLimitNs))) break;
         tc_fence_after();
-        const uint32_t st = smem_u32(buf + s * stage_bytes);
-        const uint64_t a = smem_desc_sw128(st, 16, 1024), b = smem_desc_sw128(st + w_bytes, 16, 1024);
+        const int i0 = c * kChunkIters, i1 = kChunked ? min(iters, i0 + kChunkIters) : iters;
+        for (int i = i0; i < i1; ++i, r.next(p.stages)) {
+          const int s = r.stage;
+          if (!(ok = wait_for(&sm.full[s], r.phase, p.status, kWaitLimitNs))) break;
+          tc_fence_after();
+          const uint32_t st = smem_u32(buf + s * stage_bytes);
+          const uint64_t a = smem_desc_sw128(st, 16, 1024), b = smem_desc_sw128(st + w_bytes, 16, 1024);
 #pragma unroll
-        for (int kk = 0; kk < 4; ++kk) mma_ss(tmem, a + 2 * kk, b + 2 * kk, p.idesc, i > 0 || kk > 0);
-        mma_commit(&sm.empty[s]);
+          for (int kk = 0; kk < 4; ++kk)
+            mma_ss(tmem, a + 2 * kk, b + 2 * kk, p.idesc, i > i0 || kk > 0);
+          mma_commit(&sm.empty[s]);
+        }
+        if (ok) mma_commit(&sm.acc_full);
       }
-      if (ok) mma_commit(&sm.done);
     }
-  }
-  __syncwarp();
-  if (__all_sync(0xffffffffu, wait_for(&sm.done, 0, p.status, kWaitLimitNs))) {
-    tc_fence_after();
-    const int m_end = min(p.rows, m0 + p.tile_t);
+    __syncwarp();
+  } else {
+    const uint32_t lanes = tmem + ((uint32_t)(warp * 32) << 16);
     const int n = n0 + warp * 32 + lane;
     const float b = p.bias && n < p.cols ? p.bias[n] : 0.f;
+    RingPos r;
+    bool ok = true;
+    if (kChunked)
+      ok = add_chunks<1>(chunks, lanes, p.tile_t, [](int i) { return 16 * i; }, m_end - m0, r, &sm.acc_full, p.status, [&](int) {
+        if (lane == 0) mbar_arrive(&sm.acc_empty);
+      });
+    if (ok) ok = __all_sync(0xffffffffu, wait_for(&sm.acc_full, r.phase, p.status, kWaitLimitNs));
+    if (ok) {
+      tc_fence_after();
+      float* mine = reinterpret_cast<float*>(buf) + warp * 32 + lane;      // [token][128 features]: the ring is read and free
 #pragma unroll 1
-    for (int c = 0; m0 + c < m_end; c += 16) {
-      float acc[16];
-      typename OutElem<OutType>::T res[16];
-      load_residual16<OutType>(p, res, n, m0 + c, m_end);
-      tmem_ld16(tmem + ((uint32_t)(warp * 32) << 16) + c, reinterpret_cast<uint32_t(&)[16]>(acc));
-      tmem_wait_ld();
-      epilogue16<OutType>(p, acc, res, n, m0 + c, m_end, b);
+      for (int c = 0; m0 + c < m_end; c += 16) {
+        float acc[16];
+        T res[16];
+        if (p.split == 1) load_residual16<OutType>(p, res, n, m0 + c, m_end);
+        load_sum16<1>(acc, lanes, p.tile_t, 0, c, chunks > 1);
+        if (p.split == 1) {
+          epilogue16<OutType>(p, acc, res, n, m0 + c, m_end, b);
+        } else {
+#pragma unroll
+          for (int j = 0; j < 16; ++j) mine[(c + j) * kTileF] = acc[j];
+        }
+      }
     }
+  }
+  if (p.split > 1) {
+    // a CTA that gave up joins the barriers as well; the status word says that the outputs are undefined
+    cluster_arrive();
+    cluster_wait();
+    if (warp < 4) {
+      const int per = (m_end - m0 + p.split - 1) / p.split, first = rank * per, last = min(m_end - m0, first + per);
+      const int n = n0 + warp * 32 + lane;
+      const float b = p.bias && n < p.cols ? p.bias[n] : 0.f;
+      const uint32_t mine = smem_u32(buf) + (warp * 32 + lane) * 4;
+#pragma unroll 1
+      for (int c = first; c < last; c += 16) {
+        T res[16];
+        load_residual16<OutType>(p, res, n, m0 + c, m0 + last);
+        float acc[16];
+#pragma unroll
+        for (int j = 0; j < 16; ++j) acc[j] = 0.f;
+#pragma unroll 1
+        for (int s = 0; s < p.split; ++s) {
+          const uint32_t from = map_to_rank(mine, s);
+#pragma unroll
+          for (int j = 0; j < 16; ++j)
+            if (c + j < last) acc[j] += ld_cluster_f32(from + (c + j) * kTileF * 4);
+        }
+        epilogue16<OutType>(p, acc, res, n, m0 + c, m0 + last, b);
+      }
+    }
+    __syncwarp();
+    cluster_arrive();
+    cluster_wait();                                    // nobody leaves while its sums may still be read
   }
   tc_fence_before();
   __syncthreads();
@@ -305,15 +431,9 @@ __global__ void __launch_bounds__(128) linear_tile_kernel(const __grid_constant_
 // accumulator lanes) and fetches half of the token tile, and one tcgen05.mma of the even CTA reads both halves, so that a
 // token tile crosses into shared memory once per pair.  Accumulators are double-buffered in tensor memory (2 x 256
 // columns): the epilogue of one tile runs under the products of the next.
-//
-// fp32 outputs: the tensor core adds a product to the accumulator by truncation, so a sum over `inner` drifts in one
-// direction by about 2^-26 of its magnitude per 16 products (measured 3.7e-6 relative for inner = 5120, fp32's own
-// rounding giving 1e-7).  That is far below the rounding of a 16-bit output but not of an fp32 one, so there the sum is
-// cut into chunks of kChunkK: each chunk gets a fresh accumulator, and the epilogue warps add the chunks with round-to-nearest.
 constexpr int kEpiWarps = 8;
 constexpr int kPairThreads = 32 * (kEpiWarps + 2);
 constexpr int kPairSmem = 227 * 1024 - 512;          // dynamic shared memory of a CTA; the barriers are static
-constexpr int kChunkK = 1024;
 // Tensor memory columns of the two accumulators; a chunked sum keeps its running total in a third set.  (Held in registers
 // between chunks, 2 or 3 blocks of 32 totals a thread spilled others into the epilogue's loop: up to 2x the time.)
 constexpr int kMaxTileChunked = 160;
@@ -348,7 +468,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
   const uint32_t rank = cluster_ctarank();
   const int pair = blockIdx.x / 2, pairs = gridDim.x / 2;
   const int w_bytes = kTileF * 128, stage_bytes = w_bytes + p.tile_t * 64;
-  const int chunks = kChunked ? (p.k_iters + kChunkK / kTileK - 1) / (kChunkK / kTileK) : 1;
+  const int chunks = kChunked ? (p.k_iters + kChunkIters - 1) / kChunkIters : 1;
   if (threadIdx.x == 0) {
     for (int s = 0; s < p.stages; ++s) {
       mbar_init(&sm.full[s], 1);                     // the even CTA's counts the bytes of both
@@ -411,8 +531,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
           const int b = acc.stage;
           if (!(ok = wait_for(&sm.acc_empty[b], acc.phase ^ 1, p.status, kWaitLimitNs))) break;
           tc_fence_after();
-          const int i0 = c * (kChunkK / kTileK);
-          const int i1 = kChunked ? min(p.k_iters, i0 + kChunkK / kTileK) : p.k_iters;
+          const int i0 = c * kChunkIters, i1 = kChunked ? min(p.k_iters, i0 + kChunkIters) : p.k_iters;
           for (int i = i0; i < i1; ++i, r.next(p.stages)) {
             const int s = r.stage;
             if (!(ok = wait_for(&sm.full[s], r.phase, p.status, kWaitLimitNs))) break;
@@ -445,54 +564,22 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
       T ahead0[16], ahead1[16];
       load_residual16<OutType>(p, ahead0, n, m0 + half * 32, m_end);
       load_residual16<OutType>(p, ahead1, n, m0 + half * 32 + 16, m_end);
-      if constexpr (kChunked) {
-        for (int c = 0; c < chunks - 1; ++c) {       // all but the last chunk: add to the total, which stays in tensor memory
-          ok = __all_sync(0xffffffffu, wait_for(&sm.acc_full[r.stage], r.phase, p.status, kWaitLimitNs));
-          if (!ok) break;
-          tc_fence_after();
-          const uint32_t part = lanes + r.stage * kAccStride<OutType>, total = lanes + 2 * kAccStride<OutType>;
-#pragma unroll 1
-          for (int col = half * 32; m0 + col < m_end; col += 64) {
-            float v[32], sum[32];
-            tmem_ld32(part + col, reinterpret_cast<uint32_t(&)[32]>(v));
-            if (c > 0) tmem_ld32(total + col, reinterpret_cast<uint32_t(&)[32]>(sum));
-            tmem_wait_ld();
-            if (c > 0) {
-#pragma unroll
-              for (int j = 0; j < 32; ++j) v[j] += sum[j];
-            }
-            tmem_st32(total + col, reinterpret_cast<uint32_t(&)[32]>(v));
-          }
-          tmem_wait_st();
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive_cluster(r.stage ? empty1 : empty0);
-          r.next(2);
-        }
+      auto release = [&](int stage) {
+        if (lane == 0) mbar_arrive_cluster(stage ? empty1 : empty0);
+      };
+      if (kChunked) {
+        ok = add_chunks<2>(chunks, lanes, kAccStride<OutType>, [&](int i) { return (i / 2 * 2 + half) * 32 + (i & 1) * 16; },
+                        m_end - m0, r, sm.acc_full, p.status, release);
         if (!ok) break;
       }
       ok = __all_sync(0xffffffffu, wait_for(&sm.acc_full[r.stage], r.phase, p.status, kWaitLimitNs));
       if (!ok) break;
       tc_fence_after();
-      const uint32_t cols = lanes + r.stage * kAccStride<OutType>;
 #pragma unroll 1
       for (int col = half * 32; m0 + col < m_end; col += 64) {
         float acc0[16], acc1[16];
-        tmem_ld16(cols + col, reinterpret_cast<uint32_t(&)[16]>(acc0));
-        tmem_ld16(cols + col + 16, reinterpret_cast<uint32_t(&)[16]>(acc1));
-        if (kChunked && chunks > 1) {
-          float sum0[16], sum1[16];
-          const uint32_t total = lanes + 2 * kAccStride<OutType> + col;
-          tmem_ld16(total, reinterpret_cast<uint32_t(&)[16]>(sum0));
-          tmem_ld16(total + 16, reinterpret_cast<uint32_t(&)[16]>(sum1));
-          tmem_wait_ld();
-#pragma unroll
-          for (int j = 0; j < 16; ++j) {
-            acc0[j] += sum0[j];
-            acc1[j] += sum1[j];
-          }
-        }
-        tmem_wait_ld();
+        load_sum16<2>(acc0, lanes, kAccStride<OutType>, r.stage, col, kChunked && chunks > 1);
+        load_sum16<2>(acc1, lanes, kAccStride<OutType>, r.stage, col + 16, kChunked && chunks > 1);
         epilogue16<OutType>(p, acc0, ahead0, n, m0 + col, m_end, bias);
         load_residual16<OutType>(p, ahead0, n, m0 + col + 64, m_end);
         epilogue16<OutType>(p, acc1, ahead1, n, m0 + col + 16, m_end, bias);
@@ -500,7 +587,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
       }
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive_cluster(r.stage ? empty1 : empty0);
+      release(r.stage);
       r.next(2);
     }
   }
@@ -533,7 +620,9 @@ int make_map(CUtensorMap* m, const void* base, int type, int inner, int rows, in
 
 std::mutex g_setup_mu;
 
-constexpr int kPairRows = 256;                       // more tokens than this go to the pairs
+// More tokens than this go to the pairs.  At 5120 x 5120: 64 tokens 17.7 us (clusters of four) against 19.5, 128 tokens 20.6
+// (clusters of two) against 19.4.
+constexpr int kPairRows = 64;
 
 // Tokens per tile of the pairs: the size whose waves of tiles cost least.  A tile's time grows linearly with its tokens on
 // top of a part that does not depend on them (the features' operand tiles come in whatever the token count), worth about
@@ -555,7 +644,29 @@ int pair_tile(int rows, int tiles_f, int pairs, int largest) {
   return best;
 }
 
-constexpr int kTileDynamic = 4 * (kTileF + kMaxTileT) * 128 + 1024;
+constexpr int kMaxTileFew = kPairRows;               // tokens per tile of the clusters
+constexpr int kTileStages = 4;
+constexpr int kTileDynamic = kTileStages * (kTileF + kMaxTileFew) * 128 + 1024;
+
+// The CTAs that an SM can hold find their tensor memory columns at once, because no tile takes a larger share of an SM's
+// columns than of its shared memory.  That matters for a cluster: its CTAs wait for each other, and if one of them could
+// wait for columns that a CTA of another waiting cluster holds, two clusters could wait for each other for good.
+constexpr bool columns_within_share(int tile_t) {
+  return tile_tmem_cols(tile_t, true) * (228 * 1024 / 512) <= (uint32_t)(kTileStages * (kTileF + tile_t) * 128 + 1024);
+}
+static_assert(columns_within_share(16) && columns_within_share(32) && columns_within_share(48) && columns_within_share(64));
+static_assert(kMaxTileFew == 64, "the sizes checked above");
+
+// CTAs per tile: as many as it takes to give every SM work, while each keeps eight stages of the sum or more and all of
+// them run at once.  One row: inner 256 4.3 us whole, 5.7 in two parts; inner 1536 x 1536 features 7.4, 7.1, 6.8 and 7.5 us in
+// 1, 2, 4 and 8 parts; 5120 x 5120 25.9, 18.1, 15.0 and 16.5.
+int tile_split(long long tiles, int k_iters, int tile_t, int sms) {
+  const int per_sm = 228 * 1024 / (kTileStages * (kTileF + tile_t) * 128 + 3 * 1024);
+  int split = 1;
+  while (split < kMaxSplit && tiles * split < sms && tiles * 2 * split <= (long long)sms * per_sm && k_iters >= 8 * split)
+    split *= 2;
+  return split;
+}
 
 // One-time set-up per device and output type: the opt-in to the kernels' dynamic shared memory, and how many CTA pairs
 // the device runs at once.
@@ -600,11 +711,11 @@ int launch(LinearParams& p, const void* x, int64_t ld_x, const void* w, int64_t 
   const bool by_pair = p.rows > kPairRows;
   const int feature_tile = by_pair ? 2 * kTileF : kTileF;
   p.tiles_f = (p.cols + feature_tile - 1) / feature_tile;
-  p.tile_t = p.rows >= kMaxTileT ? kMaxTileT : (p.rows + 15) / 16 * 16;
   if (by_pair) p.tile_t = pair_tile(p.rows, p.tiles_f, pairs, OutType == SDVG_F32 ? kMaxTileChunked : kMaxTileT);
+  else p.tile_t = (std::min(p.rows, kMaxTileFew) + 15) / 16 * 16;
   p.tiles_t = (p.rows + p.tile_t - 1) / p.tile_t;
   p.tiles = (long long)p.tiles_f * p.tiles_t;
-  if (p.tiles >= 1ll << 31) return SDVG_ERR_BAD_SHAPE;
+  if (p.tiles >= 1ll << 28) return SDVG_ERR_BAD_SHAPE;
   p.idesc = idesc_16bit_f32(feature_tile, p.tile_t, in_type == SDVG_BF16);
   if ((st = make_map(&p.w_map, w, in_type, inner, p.cols, ld_w, kTileF)) != SDVG_OK) return st;
   if ((st = make_map(&p.x_map, x, in_type, inner, p.rows, ld_x, by_pair ? p.tile_t / 2 : p.tile_t)) != SDVG_OK) return st;
@@ -613,11 +724,22 @@ int launch(LinearParams& p, const void* x, int64_t ld_x, const void* w, int64_t 
     p.stages = std::min(kMaxStages, (kPairSmem - 1024) / (kTileF * 128 + p.tile_t * 64));
     const int grid = 2 * (int)std::min((long long)pairs, p.tiles);
     linear_pair_kernel<OutType><<<grid, kPairThreads, kPairSmem, stream>>>(p);
-  } else {
-    p.stages = 4;
-    linear_tile_kernel<OutType><<<(unsigned)p.tiles, 128, p.stages * (kTileF + p.tile_t) * 128 + 1024, stream>>>(p);
+    return sdvg::cuda_status(cudaGetLastError());
   }
-  return sdvg::cuda_status(cudaGetLastError());
+  p.split = tile_split(p.tiles, p.k_iters, p.tile_t, 2 * pairs);
+  p.stages = kTileStages;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)p.tiles * p.split);
+  cfg.blockDim = dim3(kTileThreads);
+  cfg.dynamicSmemBytes = p.stages * (kTileF + p.tile_t) * 128 + 1024;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr;
+  attr.id = cudaLaunchAttributeClusterDimension;
+  attr.val.clusterDim.x = p.split;
+  attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = p.split > 1 ? 1 : 0;
+  return sdvg::cuda_status(cudaLaunchKernelEx(&cfg, linear_tile_kernel<OutType>, p));
 }
 
 bool aligned_to(const void* p, int bytes) { return (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(bytes - 1)) == 0; }
