@@ -14,6 +14,7 @@
 #include <algorithm>
 
 #include "elem_types.cuh"
+#include "overlap.cuh"
 #include "row_team.cuh"
 #include "sdvg_internal.h"
 
@@ -133,10 +134,12 @@ __device__ __forceinline__ void apply_norm(Vec8 (&v)[NI], float mean, float rstd
 // pieces of a warp are 32 vectors apart, so that they are a constant distance from one address per row, which moves on by the
 // row stride.  FULL: the team's pieces are all inside the row.
 template <int XW, int YW, int NI, bool WARP, bool FULL>
-__global__ void __launch_bounds__(WARP ? 128 : kTeamThreads) gated_norm_kernel(const NormParams p) {
+__global__ void __launch_bounds__(WARP ? 128 : kTeamThreads) gated_norm_kernel(const __grid_constant__ NormParams p) {
   extern __shared__ uint4 s_ring[];
   __shared__ Moments s_part[2][32];
   __shared__ float s_count[32];
+  sdvg::overlap_begin();
+  sdvg::overlap_wait();
   const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
   const int c0 = ((WARP ? 0 : warp * 32 * NI) + lane) * 8;             // first piece; piece i: c0 + 256 i
   auto valid = [&](int i) { return FULL || c0 + 256 * i < p.cols; };
@@ -324,9 +327,11 @@ __device__ __forceinline__ void store_singles(const float (&v)[NI], void* base, 
 // Rows that are not made of aligned vectors: one CTA per row, NI single columns per thread; what is in flight comes from the
 // CTAs of an SM.
 template <int NI>
-__global__ void __launch_bounds__(NI == 16 ? 512 : 256) gated_norm_single_kernel(const NormParams p) {
+__global__ void __launch_bounds__(NI == 16 ? 512 : 256) gated_norm_single_kernel(const __grid_constant__ NormParams p) {
   __shared__ Moments s_part[2][32];
   __shared__ float s_count[32];
+  sdvg::overlap_begin();
+  sdvg::overlap_wait();
   const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
   const int c0 = warp * 32 * NI + lane;                // first column; piece i: c0 + 32 i
   const long long r = blockIdx.x;
@@ -423,8 +428,10 @@ __device__ __forceinline__ void row_stats(const NormParams& p, int kind, Value v
   *rstd = 1.f / sqrtf(block_sum(q, buf) * p.inv_cols + p.eps);
 }
 
-__global__ void __launch_bounds__(kLongThreads) gated_norm_long_kernel(const NormParams p) {
+__global__ void __launch_bounds__(kLongThreads) gated_norm_long_kernel(const __grid_constant__ NormParams p) {
   __shared__ float buf[kLongThreads / 32];
+  sdvg::overlap_begin();
+  sdvg::overlap_wait();
   const long long r = blockIdx.x;
   const float* gate = p.gate ? p.gate + (r / p.gate_rows) * p.ld_gate : nullptr;
   const float* scale = p.scale ? p.scale + (r / p.mod_rows) * p.ld_mod : nullptr;
@@ -496,8 +503,7 @@ int launch_team_as(const NormParams& p, int threads, int sms, cudaStream_t strea
     }
     grid = std::min(want, sms * std::max(resident, 1));
   }
-  gated_norm_kernel<XW, YW, NI, WARP, FULL><<<grid, threads, dynamic, stream>>>(p);
-  return sdvg::cuda_status(cudaGetLastError());
+  return sdvg::cuda_status(sdvg::launch_overlapped(gated_norm_kernel<XW, YW, NI, WARP, FULL>, grid, threads, dynamic, 0, stream, p));
 }
 
 template <int XW, int YW, int NI, bool WARP>
@@ -527,14 +533,16 @@ int launch(const NormParams& p, bool vec, cudaStream_t stream) {
     else st = x4 ? launch_vec<4, 2>(p, sms, stream) : launch_vec<2, 2>(p, sms, stream);
     if (st != -1) return st;
   } else if (p.cols <= 512 * 16) {
-    if (p.cols <= 256) gated_norm_single_kernel<1><<<p.rows, (p.cols + 31) / 32 * 32, 0, stream>>>(p);
-    else if (p.cols <= 1024) gated_norm_single_kernel<4><<<p.rows, ((p.cols + 3) / 4 + 31) / 32 * 32, 0, stream>>>(p);
-    else if (p.cols <= 2048) gated_norm_single_kernel<8><<<p.rows, ((p.cols + 7) / 8 + 31) / 32 * 32, 0, stream>>>(p);
-    else gated_norm_single_kernel<16><<<p.rows, ((p.cols + 15) / 16 + 31) / 32 * 32, 0, stream>>>(p);
-    return sdvg::cuda_status(cudaGetLastError());
+    auto single = [&](void (*kernel)(NormParams), int pieces) {
+      const int threads = ((p.cols + pieces - 1) / pieces + 31) / 32 * 32;
+      return sdvg::cuda_status(sdvg::launch_overlapped(kernel, p.rows, threads, 0, 0, stream, p));
+    };
+    if (p.cols <= 256) return single(gated_norm_single_kernel<1>, 1);
+    if (p.cols <= 1024) return single(gated_norm_single_kernel<4>, 4);
+    if (p.cols <= 2048) return single(gated_norm_single_kernel<8>, 8);
+    return single(gated_norm_single_kernel<16>, 16);
   }
-  gated_norm_long_kernel<<<p.rows, kLongThreads, 0, stream>>>(p);
-  return sdvg::cuda_status(cudaGetLastError());
+  return sdvg::cuda_status(sdvg::launch_overlapped(gated_norm_long_kernel, p.rows, kLongThreads, 0, 0, stream, p));
 }
 
 bool aligned_to(const void* p, int bytes) { return (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(bytes - 1)) == 0; }

@@ -18,6 +18,7 @@
 
 #include "bounded_wait.cuh"
 #include "elem_types.cuh"
+#include "overlap.cuh"
 #include "sdvg_internal.h"
 #include "sm100_ptx.cuh"
 #include "tensor_map.h"
@@ -317,6 +318,7 @@ __global__ void __launch_bounds__(kTileThreads) linear_tile_kernel(const __grid_
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = sm.tmem;
+  sdvg::overlap_wait();
 
   if (warp == 4) {
     if (elect_one()) {
@@ -330,6 +332,9 @@ __global__ void __launch_bounds__(kTileThreads) linear_tile_kernel(const __grid_
         tma_load_2d(st, &p.w_map, &sm.full[s], (k0 + i) * kTileK, n0);
         tma_load_2d(st + w_bytes, &p.x_map, &sm.full[s], (k0 + i) * kTileK, m0);
       }
+      // only now: SMs hold several of these CTAs, and a next grid that starts while they still hold them lands on the SMs
+      // with room, which are not the ones that will be idle (3 x 5120 x 30720 back to back: 62 us when begun at the start, 51 here)
+      sdvg::overlap_begin();
       if (i < iters)                                   // gave up: see the copies in flight land before the CTA may leave
         for (int j = min(i, p.stages); j > 0; --j) {
           r.back(p.stages);
@@ -469,6 +474,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
   const int pair = blockIdx.x / 2, pairs = gridDim.x / 2;
   const int w_bytes = kTileF * 128, stage_bytes = w_bytes + p.tile_t * 64;
   const int chunks = kChunked ? (p.k_iters + kChunkIters - 1) / kChunkIters : 1;
+  sdvg::overlap_begin();
   if (threadIdx.x == 0) {
     for (int s = 0; s < p.stages; ++s) {
       mbar_init(&sm.full[s], 1);                     // the even CTA's counts the bytes of both
@@ -492,6 +498,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
   cluster_wait();                                    // the other CTA's barriers are initialised as well
   tc_fence_after();
   const uint32_t tmem = sm.tmem;
+  sdvg::overlap_wait();
 
   if (warp == kEpiWarps) {
     // ================= producer: this CTA's features and its half of the token tile =================
@@ -723,23 +730,14 @@ int launch(LinearParams& p, const void* x, int64_t ld_x, const void* w, int64_t 
     p.group = 8;
     p.stages = std::min(kMaxStages, (kPairSmem - 1024) / (kTileF * 128 + p.tile_t * 64));
     const int grid = 2 * (int)std::min((long long)pairs, p.tiles);
-    linear_pair_kernel<OutType><<<grid, kPairThreads, kPairSmem, stream>>>(p);
-    return sdvg::cuda_status(cudaGetLastError());
+    return sdvg::cuda_status(
+        sdvg::launch_overlapped(linear_pair_kernel<OutType>, grid, kPairThreads, kPairSmem, 0, stream, p));
   }
   p.split = tile_split(p.tiles, p.k_iters, p.tile_t, 2 * pairs);
   p.stages = kTileStages;
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)p.tiles * p.split);
-  cfg.blockDim = dim3(kTileThreads);
-  cfg.dynamicSmemBytes = p.stages * (kTileF + p.tile_t) * 128 + 1024;
-  cfg.stream = stream;
-  cudaLaunchAttribute attr;
-  attr.id = cudaLaunchAttributeClusterDimension;
-  attr.val.clusterDim.x = p.split;
-  attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
-  cfg.attrs = &attr;
-  cfg.numAttrs = p.split > 1 ? 1 : 0;
-  return sdvg::cuda_status(cudaLaunchKernelEx(&cfg, linear_tile_kernel<OutType>, p));
+  return sdvg::cuda_status(sdvg::launch_overlapped(linear_tile_kernel<OutType>, (unsigned)p.tiles * p.split, kTileThreads,
+                                                   p.stages * (kTileF + p.tile_t) * 128 + 1024, p.split > 1 ? p.split : 0,
+                                                   stream, p));
 }
 
 bool aligned_to(const void* p, int bytes) { return (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(bytes - 1)) == 0; }

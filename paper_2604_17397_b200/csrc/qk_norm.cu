@@ -4,6 +4,7 @@
 
 #include <algorithm>
 
+#include "overlap.cuh"
 #include "rope_args.h"
 #include "row_team.cuh"
 #include "sdvg_internal.h"
@@ -91,6 +92,8 @@ __global__ void __launch_bounds__(WARP ? 128 : NI == 2 ? kTeamThreads : 512) qk_
   constexpr int kGroup = D / 8;                        // lanes of a head
   extern __shared__ uint4 s_ring[];
   __shared__ float2 s_part[2][32];
+  sdvg::overlap_begin();
+  sdvg::overlap_wait();
   const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
   const int width = p.heads * D;
   const int c0 = ((WARP ? 0 : warp * 32 * NI) + lane) * 8;             // first piece; piece i: c0 + 256 i
@@ -243,8 +246,8 @@ int launch_team(const QkParams& p, int threads, cudaStream_t stream) {
   }
   const int rows_per_cta = WARP ? threads / 32 : 1;
   const int want = (p.tokens + rows_per_cta - 1) / rows_per_cta;
-  qk_norm_kernel<D, NI, WARP><<<std::min(want, sms * std::max(resident, 1)), threads, dynamic, stream>>>(p);
-  return sdvg::cuda_status(cudaGetLastError());
+  return sdvg::cuda_status(sdvg::launch_overlapped(qk_norm_kernel<D, NI, WARP>, std::min(want, sms * std::max(resident, 1)),
+                                                   threads, dynamic, 0, stream, p));
 }
 
 template <int D>
