@@ -74,17 +74,24 @@ class ModelState:
         if self.tiled:
             api.sdvg_rope3d_qk_commit_e4m3_tiled(self.cache, q, k, v, q_roped, self.q_tile_scale, self.grid,
                                                  block * self.frames, self.table, self.tab_frames, block, api.SDVG_STAGE)
-            api.sdvg_block_attn_fwd_e4m3_tiled(q_roped, self.q_tile_scale, self.cache, block, out, None, self.scale,
-                                               self.workspace)
         elif self.e4m3:
             api.sdvg_rope3d_qk_commit_e4m3(self.cache, q, k, v, q_roped, self.q_inv_scale, self.k_inv_scale,
                                            self.v_inv_scale, self.grid, block * self.frames, self.table,
                                            self.tab_frames, block, api.SDVG_STAGE)
-            api.sdvg_block_attn_fwd_e4m3(q_roped, None, None, self.cache, block, self.qk_descale, self.v_descale, out,
-                                         None, self.scale, self.workspace)
         else:
             api.sdvg_rope3d_qk_commit(self.cache, q, k, v, q_roped, None, self.grid, block * self.frames, self.table,
                                       self.tab_frames, block, api.SDVG_STAGE)
+        self.attend(q_roped, block, out)
+
+    def attend(self, q_roped, block: int, out) -> None:
+        """Attention of the staged `block` against the ring; q_roped holds what the prologue of this ring wrote."""
+        if self.tiled:
+            api.sdvg_block_attn_fwd_e4m3_tiled(q_roped, self.q_tile_scale, self.cache, block, out, None, self.scale,
+                                               self.workspace)
+        elif self.e4m3:
+            api.sdvg_block_attn_fwd_e4m3(q_roped, None, None, self.cache, block, self.qk_descale, self.v_descale, out,
+                                         None, self.scale, self.workspace)
+        else:
             api.sdvg_block_attn_fwd(q_roped, None, None, self.cache, block, out, None, self.scale, self.workspace)
 
     def block_steps(self, qs, ks, vs, block: int, q_ropeds, outs) -> None:
@@ -125,6 +132,148 @@ class ModelState:
 
 
 @dataclass
+class LayerWeights:
+    """A transformer layer around the block attention: matrices as stored ([out features, in features], bf16), vectors
+    fp32.  width = heads * head_dim of the model's ring."""
+    w_qkv: torch.Tensor                    # [3 * width, width]: q, k, v stacked
+    w_out: torch.Tensor                    # [width, width]
+    w_up: torch.Tensor                     # [hidden, width]
+    w_down: torch.Tensor                   # [width, hidden]
+    b_qkv: torch.Tensor = None
+    b_out: torch.Tensor = None
+    b_up: torch.Tensor = None
+    b_down: torch.Tensor = None
+    q_norm: torch.Tensor = None            # RMS norm weights of q and k: [width], or [head_dim] with SDVG_SCOPE_HEAD
+    k_norm: torch.Tensor = None
+    scope: int = api.SDVG_SCOPE_ROW
+    post_attn: torch.Tensor = None         # weight of an RMS norm after the attention projection; None: no such norm
+    post_ff: torch.Tensor = None           # and after the feed-forward pair
+    act: int = api.SDVG_ACT_GELU_TANH
+    eps: float = 1e-6
+
+
+class TransformerLayer:
+    """One layer of a model (Sec. 4.1 "Models") in library calls: modulated norm, QKV projection, norm of q and k with
+    rotary and stage, block attention, output projection onto the residual stream, modulated norm, feed-forward pair.
+
+    ``x`` is the residual stream [block_tokens, width] (bf16 or fp32), ``mod`` the modulation of the step, fp32
+    [groups, 6 * width]: shift, scale, gate of the attention half, then of the feed-forward half; token t uses row
+    t // ceil(block_tokens / groups) (one row per latent frame, or one for the block).  The buffers between the calls
+    belong to the layer: steps of one layer must not overlap on the device.
+    """
+
+    def __init__(self, weights: LayerWeights, m: ModelState, x_dtype: torch.dtype = torch.bfloat16):
+        c = m.cache
+        self.w, self.m, self.width, self.tokens = weights, m, c.heads * c.head_dim, c.block_tokens
+        hidden, dev = weights.w_up.shape[0], m.table.device
+        new = lambda cols, dtype=torch.bfloat16: torch.empty((self.tokens, cols), dtype=dtype, device=dev)
+        self.h, self.qkv, self.ff = new(self.width), new(3 * self.width), new(hidden)
+        self.x1 = new(self.width, x_dtype)                       # the stream between the two halves
+        post = weights.post_attn is not None or weights.post_ff is not None
+        self.y = new(self.width) if post else None
+        self.q8 = [new(self.width) for _ in range(3)] if m.e4m3 else None
+
+    def _mod(self, mod: torch.Tensor):
+        rows = -(-self.tokens // mod.shape[0])
+        return [mod[:, i * self.width:(i + 1) * self.width] for i in range(6)], rows
+
+    def _heads(self, t: torch.Tensor) -> torch.Tensor:
+        return t.unflatten(1, (self.m.cache.heads, self.m.cache.head_dim))
+
+    def _qkv(self, x, mod, with_q: bool = True):
+        """q (or None), k, v of the stream x as column ranges of one product."""
+        w, n = self.w, self.width
+        (shift, scale, *_), rows = self._mod(mod)
+        api.sdvg_gated_norm(x, self.h, scale=scale, shift=shift, modulate_rows=rows, eps=w.eps)
+        first = 0 if with_q else n
+        out = self.qkv[:, first:]
+        api.sdvg_linear(self.h, w.w_qkv[first:], out, self.m.workspace, bias=None if w.b_qkv is None else w.b_qkv[first:])
+        parts = [out[:, i:i + n] for i in range(0, 3 * n - first, n)]
+        return parts if with_q else [None] + parts
+
+    def _rms(self, t, weight, out) -> torch.Tensor:
+        """RMS norm of a column range into a contiguous [tokens, heads, dim] tensor (an 8-bit ring takes such tensors)."""
+        if self.w.scope == api.SDVG_SCOPE_ROW:
+            api.sdvg_gated_norm(t, out, norm=api.SDVG_NORM_RMS, weight=weight, eps=self.w.eps)
+        else:
+            dim = self.m.cache.head_dim
+            api.sdvg_gated_norm(t, out, norm=api.SDVG_NORM_NONE)           # columns of the product to contiguous rows
+            rows = out.view(-1, dim)
+            api.sdvg_gated_norm(rows, rows, norm=api.SDVG_NORM_RMS, weight=weight, eps=self.w.eps)
+        return self._heads(out)
+
+    def _write_kv(self, q, k, v, block: int, flags: int, q_roped=None) -> int:
+        """Norm, rotary and ring write; returns the evicted block."""
+        m, w = self.m, self.w
+        if not m.e4m3:
+            q, k, v = (None if t is None else self._heads(t) for t in (q, k, v))
+            return api.sdvg_qk_norm_rope3d_commit(m.cache, q, k, v, w.q_norm, w.k_norm, w.scope, w.eps, q_roped, None, m.grid,
+                                                  block * m.frames, m.table, m.tab_frames, block, flags)
+        q = None if q is None else self._rms(q, w.q_norm, self.q8[0])
+        k = self._rms(k, w.k_norm, self.q8[1])
+        api.sdvg_gated_norm(v, self.q8[2], norm=api.SDVG_NORM_NONE)
+        v = self._heads(self.q8[2])
+        if m.tiled:
+            return api.sdvg_rope3d_qk_commit_e4m3_tiled(m.cache, q, k, v, q_roped, None if q is None else m.q_tile_scale,
+                                                        m.grid, block * m.frames, m.table, m.tab_frames, block, flags)
+        return api.sdvg_rope3d_qk_commit_e4m3(m.cache, q, k, v, q_roped, None if q is None else m.q_inv_scale, m.k_inv_scale,
+                                              m.v_inv_scale, m.grid, block * m.frames, m.table, m.tab_frames, block, flags)
+
+    def step(self, x, mod, block: int, x_out) -> None:
+        """One denoise step of `block`: the ring's slot of the block is staged, x_out (may be x) receives the stream."""
+        m, w = self.m, self.w
+        q, k, v = self._qkv(x, mod)
+        self._write_kv(q, k, v, block, api.SDVG_STAGE, m.q_roped)
+        m.attend(m.q_roped, block, m.out)
+        (_, _, gate1, shift2, scale2, gate2), rows = self._mod(mod)
+        attn = m.out.view(self.tokens, self.width)
+        if w.post_attn is None:
+            api.sdvg_linear(attn, w.w_out, self.x1, m.workspace, bias=w.b_out, gate=gate1, gate_rows=rows, residual=x)
+            api.sdvg_gated_norm(self.x1, self.h, scale=scale2, shift=shift2, modulate_rows=rows, eps=w.eps)
+        else:
+            api.sdvg_linear(attn, w.w_out, self.y, m.workspace, bias=w.b_out)
+            api.sdvg_gated_norm(x, self.h, y=self.y, gate=gate1, gate_rows=rows, post_norm=api.SDVG_NORM_RMS,
+                                post_weight=w.post_attn, x_out=self.x1, scale=scale2, shift=shift2, modulate_rows=rows,
+                                eps=w.eps)
+        api.sdvg_linear(self.h, w.w_up, self.ff, m.workspace, bias=w.b_up, act=w.act)
+        if w.post_ff is None:
+            api.sdvg_linear(self.ff, w.w_down, x_out, m.workspace, bias=w.b_down, gate=gate2, gate_rows=rows, residual=self.x1)
+        else:
+            api.sdvg_linear(self.ff, w.w_down, self.y, m.workspace, bias=w.b_down)
+            api.sdvg_gated_norm(self.x1, None, y=self.y, gate=gate2, gate_rows=rows, post_norm=api.SDVG_NORM_RMS,
+                                post_weight=w.post_ff, x_out=x_out, eps=w.eps)
+
+    def commit(self, x, mod, block: int) -> int:
+        """The block's final K/V from its final stream into the ring (SDVG_FINAL); returns the evicted block."""
+        _, k, v = self._qkv(x, mod, with_q=False)
+        return self._write_kv(None, k, v, block, api.SDVG_FINAL)
+
+
+@dataclass
+class TimeModulation:
+    """The modulation of a step from its time features (Sec. 4.1: the sampler's time steps): fp32 [groups, 6 * width] =
+    offsets + W_mod silu(W2 silu(W1 features + b1) + b2) + b_mod, features bf16 [groups, ...]."""
+    w1: torch.Tensor
+    w2: torch.Tensor
+    w_mod: torch.Tensor
+    b1: torch.Tensor = None
+    b2: torch.Tensor = None
+    b_mod: torch.Tensor = None
+    offsets: torch.Tensor = None           # learned, fp32 [1, 6 * width]
+
+    def __call__(self, features, workspace, out=None) -> torch.Tensor:
+        rows, dev = features.shape[0], features.device
+        new = lambda cols, dtype=torch.bfloat16: torch.empty((rows, cols), dtype=dtype, device=dev)
+        a, e = new(self.w1.shape[0]), new(self.w2.shape[0])
+        out = new(self.w_mod.shape[0], torch.float32) if out is None else out
+        api.sdvg_linear(features, self.w1, a, workspace, bias=self.b1, act=api.SDVG_ACT_SILU)
+        api.sdvg_linear(a, self.w2, e, workspace, bias=self.b2, act=api.SDVG_ACT_SILU)
+        api.sdvg_linear(e, self.w_mod, out, workspace, bias=self.b_mod,
+                        residual=None if self.offsets is None else self.offsets.expand(rows, -1))
+        return out
+
+
+@dataclass
 class TraceResult:
     accept: np.ndarray
     q_min: np.ndarray
@@ -135,23 +284,33 @@ class TraceResult:
     target_source: list = field(default_factory=list)     # per block: "accepted" or "regenerated"
 
 
-def _denoise(model: str, m: ModelState, block: int, steps: int, provider, on_attention) -> int:
+def _denoise(model: str, m: ModelState, block: int, steps: int, provider, on_attention, layer) -> int:
     for s in range(steps):
-        q, k, v = provider(model, block, "step", s)
-        m.stage_and_attend(q, k, v, block, m.q_roped, m.out)
+        if layer is not None:
+            x, mod, x_out = provider(model, block, "step", s)
+            layer.step(x, mod, block, x_out)
+        else:
+            q, k, v = provider(model, block, "step", s)
+            m.stage_and_attend(q, k, v, block, m.q_roped, m.out)
         if on_attention is not None:
             on_attention(model, block, s, m.q_roped, m.out)
     return steps
 
 
-def _commit_clean(m: ModelState, block: int, k, v) -> int:
+def _commit_clean(m: ModelState, block: int, layer, given) -> int:
+    if layer is not None:
+        x, mod, _ = given
+        return layer.commit(x, mod, block)
+    _, k, v = given
     return m.commit_final(k, v, block)
 
 
 def run_schedule(num_blocks: int, steps: int, scores: torch.Tensor, tau: float,
                  drafter: ModelState, target: ModelState,
                  provider: Callable, first_block_index: int = 0,
-                 on_attention: Optional[Callable] = None) -> TraceResult:
+                 on_attention: Optional[Callable] = None,
+                 drafter_layer: Optional[TransformerLayer] = None,
+                 target_layer: Optional[TransformerLayer] = None) -> TraceResult:
     """Generate ``num_blocks`` blocks with the drafter/router/target flow.
 
     scores    device fp32 [num_blocks, frames]: the per-frame reward of every draft block
@@ -163,6 +322,9 @@ def run_schedule(num_blocks: int, steps: int, scores: torch.Tensor, tau: float,
     on_attention  optional ``f(model, block, step, q_roped, out)`` called after each
               attention launch (the tensors are reused by the next step; q_roped holds E4M3
               codes when the model's ring is an 8-bit one)
+    drafter_layer, target_layer   optional layers around the models' attention: for such a model the provider gives
+              (x, mod, x_out), the residual stream, the step's modulation and where the step's stream goes, in
+              place of (q, k, v); for "clean" and "accepted" x_out is not used
     A model whose ``cache`` is an 8-bit ring takes every step through the _e4m3 entry points.
     The accept decision is read back to the host once per block, which is the only
     synchronisation point of the flow.
@@ -177,23 +339,22 @@ def run_schedule(num_blocks: int, steps: int, scores: torch.Tensor, tau: float,
     flat = scores.reshape(-1)
     for i in range(num_blocks):
         b = first_block_index + i
-        res.drafter_attn_calls += _denoise("drafter", drafter, b, steps, provider, on_attention)
+        res.drafter_attn_calls += _denoise("drafter", drafter, b, steps, provider, on_attention, drafter_layer)
         api.sdvg_route(flat[i * frames:(i + 1) * frames], None, 1, frames, b, tau, accept_d[i:i + 1],
                        qmin_d[i:i + 1], None)
         accepted = bool(accept_d[i].item())               # the flow's one synchronisation point per block
         # a kernel that gave up leaves undefined outputs: stop before anything derived from them enters a ring
         drafter.check_status(f"drafter steps of block {b}")
-        _, k, v = provider("drafter", b, "clean", 0)
-        res.drafter_evicted.append(_commit_clean(drafter, b, k, v))
+        res.drafter_evicted.append(_commit_clean(drafter, b, drafter_layer, provider("drafter", b, "clean", 0)))
         if accepted:
-            _, k, v = provider("target", b, "accepted", 0)
+            given = provider("target", b, "accepted", 0)
             res.target_source.append("accepted")
         else:
-            res.target_attn_calls += _denoise("target", target, b, steps, provider, on_attention)
+            res.target_attn_calls += _denoise("target", target, b, steps, provider, on_attention, target_layer)
             target.check_status(f"target steps of block {b}")
-            _, k, v = provider("target", b, "clean", 0)
+            given = provider("target", b, "clean", 0)
             res.target_source.append("regenerated")
-        res.target_evicted.append(_commit_clean(target, b, k, v))
+        res.target_evicted.append(_commit_clean(target, b, target_layer, given))
     res.accept = accept_d.cpu().numpy()
     res.q_min = qmin_d.cpu().numpy()
     return res
