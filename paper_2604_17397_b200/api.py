@@ -651,22 +651,21 @@ def _groups(t: Optional[torch.Tensor], dev: int, rows: int, cols: int, group_row
     return _matrix(t, dev, (-(-rows // group_rows), cols), torch.float32, what)
 
 
-def _call_on(dev: int, fn, where: str, stream, *args) -> None:
-    """Calls an entry point, whose last argument is the stream, with CUDA device `dev` current: launches and the default
-    stream are the current device's."""
-    if dev != torch._C._cuda_getDevice():
-        with torch.cuda.device(dev):
-            return _call_on(dev, fn, where, stream, *args)
-    raw = torch._C._cuda_getCurrentRawStream(dev) if stream is None else _stream(stream)
-    status = fn(*args, raw)
-    if status != SDVG_OK:
-        raise SdvgError(status, where)
+def _raw_stream(dev: int, stream) -> int:
+    """The stream to launch on: the caller's, or the current one of CUDA device `dev`, which must be current."""
+    return torch._C._cuda_getCurrentRawStream(dev) if stream is None else _stream(stream)
 
 
 def _device_of(t: torch.Tensor) -> int:
     if not t.is_cuda:
         raise ValueError("expected CUDA tensors")
     return t.get_device()
+
+
+def _elsewhere(dev: int) -> bool:
+    """Whether another device than `dev` is current: launches and the default stream are the current device's, so such a call
+    is made again with `dev` current."""
+    return dev != torch._C._cuda_getDevice()
 
 
 def sdvg_linear(x, w, out, workspace, bias=None, act: int = SDVG_ACT_NONE, residual=None, gate=None, gate_rows: int = 0,
@@ -680,6 +679,9 @@ def sdvg_linear(x, w, out, workspace, bias=None, act: int = SDVG_ACT_NONE, resid
     if in_type is None or in_type == SDVG_F32 or out_type is None:
         raise ValueError("x must be bfloat16 or float16, out one of these or float32")
     dev = _device_of(x)
+    if _elsewhere(dev):
+        with torch.cuda.device(dev):
+            return sdvg_linear(x, w, out, workspace, bias, act, residual, gate, gate_rows, stream)
     if workspace.get_device() != dev:
         raise ValueError("workspace must be on the tensors' device")
     xp, ld_x = _matrix(x, dev, (rows, inner), x.dtype, "x")
@@ -687,9 +689,10 @@ def sdvg_linear(x, w, out, workspace, bias=None, act: int = SDVG_ACT_NONE, resid
     op, ld_out = _matrix(out, dev, (rows, cols), out.dtype, "out")
     rp, ld_res = (None, 0) if residual is None else _matrix(residual, dev, (rows, cols), out.dtype, "residual")
     gp, ld_gate = _groups(gate, dev, rows, cols, gate_rows, "gate")
-    _call_on(dev, lib().sdvg_linear, "sdvg_linear", stream, xp, ld_x, wp, ld_w, _vector(bias, dev, cols, "bias"), act, gp,
-             ld_gate, gate_rows, rp, ld_res, op, ld_out, rows, cols, inner, in_type, out_type, workspace.data_ptr(),
-             workspace.numel())
+    st = lib().sdvg_linear(xp, ld_x, wp, ld_w, _vector(bias, dev, cols, "bias"), act, gp, ld_gate, gate_rows, rp, ld_res, op,
+                           ld_out, rows, cols, inner, in_type, out_type, workspace.data_ptr(), workspace.numel(),
+                           _raw_stream(dev, stream))
+    _check(st, "sdvg_linear")
 
 
 def sdvg_gated_norm(x, out, y=None, gate=None, gate_rows: int = 0, post_norm: int = SDVG_NORM_NONE, post_weight=None,
@@ -705,6 +708,10 @@ def sdvg_gated_norm(x, out, y=None, gate=None, gate_rows: int = 0, post_norm: in
     if x.dtype not in types or (y is not None and y.dtype not in types) or (out is not None and out.dtype not in types):
         raise ValueError("expected bfloat16, float16 or float32 tensors")
     dev = _device_of(x)
+    if _elsewhere(dev):
+        with torch.cuda.device(dev):
+            return sdvg_gated_norm(x, out, y, gate, gate_rows, post_norm, post_weight, x_out, norm, weight, bias, scale, shift,
+                                   modulate_rows, eps, stream)
     xp, ld_x = _matrix(x, dev, shape, x.dtype, "x")
     yp, ld_y, y_type = None, 0, 0
     if y is not None:
@@ -722,10 +729,11 @@ def sdvg_gated_norm(x, out, y=None, gate=None, gate_rows: int = 0, post_norm: in
         ld_mod = ld_shift
     elif hp is not None and ld_mod != ld_shift and rows > modulate_rows:
         raise ValueError("scale and shift must have the same row stride")
-    _call_on(dev, lib().sdvg_gated_norm, "sdvg_gated_norm", stream, xp, ld_x, types[x.dtype], yp, ld_y, y_type, post_norm,
-             _vector(post_weight, dev, cols, "post_weight"), gp, ld_gate, gate_rows, xo, ld_xo, norm,
-             _vector(weight, dev, cols, "weight"), _vector(bias, dev, cols, "bias"), sp, hp, ld_mod, modulate_rows, eps, op,
-             ld_out, out_type, rows, cols)
+    st = lib().sdvg_gated_norm(xp, ld_x, types[x.dtype], yp, ld_y, y_type, post_norm,
+                               _vector(post_weight, dev, cols, "post_weight"), gp, ld_gate, gate_rows, xo, ld_xo, norm,
+                               _vector(weight, dev, cols, "weight"), _vector(bias, dev, cols, "bias"), sp, hp, ld_mod,
+                               modulate_rows, eps, op, ld_out, out_type, rows, cols, _raw_stream(dev, stream))
+    _check(st, "sdvg_gated_norm")
 
 
 def _tokens(t: torch.Tensor, dev: int, shape: tuple, what: str, contiguous: bool = False):
@@ -750,6 +758,10 @@ def sdvg_qk_norm_rope3d_commit(cache: Cache, q, k, v, q_weight, k_weight, scope:
     shape = (cache.block_tokens, cache.heads, cache.head_dim)
     width = shape[1] * shape[2] if scope == SDVG_SCOPE_ROW else shape[2]
     dev = cache._k_raw.get_device()
+    if _elsewhere(dev):
+        with torch.cuda.device(dev):
+            return sdvg_qk_norm_rope3d_commit(cache, q, k, v, q_weight, k_weight, scope, eps, q_out, k_out, grid, frame_offset,
+                                              table, tab_frames, block_index, flags, stream)
     qp, ld_q = (None, 0) if q is None else _tokens(q, dev, shape, "q")
     kp, ld_k = _tokens(k, dev, shape, "k")
     vp, ld_v = _tokens(v, dev, shape, "v")
@@ -757,7 +769,10 @@ def sdvg_qk_norm_rope3d_commit(cache: Cache, q, k, v, q_weight, k_weight, scope:
     ko = None if k_out is None else _tokens(k_out, dev, shape, "k_out", True)[0]
     frames, grid_h, grid_w = grid
     ev = _I64(-1)
-    _call_on(dev, lib().sdvg_qk_norm_rope3d_commit, "sdvg_qk_norm_rope3d_commit", stream, cache.handle, qp, ld_q, kp, ld_k,
-             vp, ld_v, _vector(q_weight, dev, width, "q_weight"), _vector(k_weight, dev, width, "k_weight"), scope, eps, qo,
-             ko, frames, grid_h, grid_w, frame_offset, _ptr(table), tab_frames, block_index, flags, C.byref(ev))
+    st = lib().sdvg_qk_norm_rope3d_commit(cache.handle, qp, ld_q, kp, ld_k, vp, ld_v,
+                                          _vector(q_weight, dev, width, "q_weight"),
+                                          _vector(k_weight, dev, width, "k_weight"), scope, eps, qo, ko, frames, grid_h,
+                                          grid_w, frame_offset, _ptr(table), tab_frames, block_index, flags, C.byref(ev),
+                                          _raw_stream(dev, stream))
+    _check(st, "sdvg_qk_norm_rope3d_commit")
     return ev.value

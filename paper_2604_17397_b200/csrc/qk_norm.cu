@@ -92,7 +92,6 @@ __global__ void __launch_bounds__(WARP ? 128 : NI == 2 ? kTeamThreads : 512) qk_
   constexpr int kGroup = D / 8;                        // lanes of a head
   extern __shared__ uint4 s_ring[];
   __shared__ float2 s_part[2][32];
-  sdvg::overlap_begin();
   sdvg::overlap_wait();
   const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
   const int width = p.heads * D;
@@ -222,6 +221,9 @@ __global__ void __launch_bounds__(WARP ? 128 : NI == 2 ? kTeamThreads : 512) qk_
     to_ring += 2 * D;
   }
   copy_wait<0>();
+  // not earlier: a next grid's teams that take over an SM one by one run out of step with the others (target block: 56.1 us
+  // back to back when begun at the start, 53.8 here)
+  sdvg::overlap_begin();
 }
 
 template <int D, int NI, bool WARP>
