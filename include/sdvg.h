@@ -549,6 +549,8 @@ int sdvg_block_steps_e4m3_tiled(int steps, sdvg_cache* cache, const void* const*
  * fp32.  A vector that changes along the rows is a matrix with one row per GROUP of consecutive rows:
  * row r uses group r / group_rows, and ceil(rows / group_rows) groups must be there.
  * Arithmetic is fp32 with one rounding into each output.  Infinities and NaN travel as in the formulas.
+ * Launches of these operators that follow each other on a stream overlap (the next one's set-up runs under the end of the one
+ * before); their memory accesses do not.
  */
 #define SDVG_BF16 0
 #define SDVG_F16  1
@@ -574,10 +576,12 @@ int sdvg_block_steps_e4m3_tiled(int steps, sdvg_cache* cache, const void* const*
  * multiples of 8 and >= inner (a single row's stride is not read); rows longer than `inner` are padding that is not read
  * into the result.  out, residual, bias and gate need the alignment of their element type only.
  * rows == 0 or cols == 0 is a call with nothing to do.  inner >= 1.
+ * Up to 64 rows the sum of a column is shared by up to eight CTAs of a cluster (added in a fixed order); beyond that pairs of
+ * CTAs walk tiles of 256 columns by up to 256 rows.  fp32 outputs are summed over `inner` in chunks of 768.
  * workspace: as for sdvg_block_attn_fwd (the same buffer may serve both): its status word reports a bounded wait that
  * gave up (sdvg_block_attn_status), the call keeps nothing else in it.
  * Errors: INVALID_ARG (NULL, unknown type or activation, workspace too small, gate_rows < 1), BAD_SHAPE (negative sizes,
- * strides too small, more than 2^31 tiles), MISALIGNED, UNSUPPORTED_ARCH, CUDA.
+ * strides too small, inner above 2^26, more than 2^28 tiles of 128 columns by 16 to 256 rows), MISALIGNED, UNSUPPORTED_ARCH, CUDA.
  */
 int sdvg_linear(const void* x, int64_t ld_x, const void* w, int64_t ld_w, const float* bias, int act,
                 const float* gate, int64_t ld_gate, int gate_rows, const void* residual, int64_t ld_residual,

@@ -138,10 +138,32 @@ __device__ __forceinline__ void load_residual16(const LinearParams& p, typename 
   }
 }
 
+// The gate of one feature over a tile's tokens m0 .. m_end: nearly always one or two groups, whose values are fetched once per
+// tile; `border` is the first token of the second.
+struct TileGate {
+  float first, second;
+  int border;
+  bool few;                                            // at most two groups
+};
+__device__ __forceinline__ TileGate tile_gate(const LinearParams& p, int n, int m0, int m_end) {
+  TileGate g{1.f, 1.f, 0x7fffffff, true};
+  if (!p.gate || n >= p.cols || m0 >= m_end) return g;
+  const int group = m0 / p.gate_rows;
+  const long long border = (long long)(group + 1) * p.gate_rows;
+  const float* at = p.gate + group * p.ld_gate + n;
+  g.first = at[0];
+  if (border < m_end) {
+    g.border = (int)border;
+    g.second = at[p.ld_gate];
+    g.few = border + p.gate_rows >= m_end;
+  }
+  return g;
+}
+
 // Epilogue of these tokens: `acc` holds the sums; tokens from `m_end` on are not touched.
 template <int OutType>
 __device__ __forceinline__ void epilogue16(const LinearParams& p, float (&acc)[16], typename OutElem<OutType>::T (&res)[16],
-                                           int n, int m0, int m_end, float b) {
+                                           int n, int m0, int m_end, float b, const TileGate& gate) {
   using E = OutElem<OutType>;
   using T = typename E::T;
   if (n >= p.cols || m0 >= m_end) return;
@@ -151,41 +173,37 @@ __device__ __forceinline__ void epilogue16(const LinearParams& p, float (&acc)[1
 #pragma unroll
   for (int j = 0; j < 16; ++j) acc[j] += b;
   activate16(acc, p.act);
-  int group = 0, last_group = 0;
   if (p.gate) {
-    group = m0 / p.gate_rows;
-    last_group = (m0 + count - 1) / p.gate_rows;
-  }
-  if (count == 16 && group == last_group) {
-    // whole block, one gate: about ten instructions per value
-    const float g = p.gate ? p.gate[group * p.ld_gate + n] : 1.f;
-    if (p.residual) {
+    if (gate.few) {
 #pragma unroll
-      for (int j = 0; j < 16; ++j) acc[j] = fmaf(acc[j], g, E::get(res[j]));
-    } else if (p.gate) {
+      for (int j = 0; j < 16; ++j) acc[j] *= m0 + j < gate.border ? gate.first : gate.second;
+    } else {
+      const int group = m0 / p.gate_rows;
+      const float* gp = p.gate + group * p.ld_gate + n;
+      long long next = (long long)(group + 1) * p.gate_rows;
 #pragma unroll
-      for (int j = 0; j < 16; ++j) acc[j] *= g;
-    }
-#pragma unroll
-    for (int j = 0; j < 16; ++j, o += ld) *o = E::put(acc[j]);
-  } else {
-    const float* gp = p.gate ? p.gate + group * p.ld_gate + n : nullptr;
-    long long next = (long long)(group + 1) * p.gate_rows;
-#pragma unroll
-    for (int j = 0; j < 16; ++j, o += ld) {
-      if (j < count) {
-        float v = acc[j];
-        if (p.gate) {
+      for (int j = 0; j < 16; ++j) {
+        if (j < count) {
           if (m0 + j == next) {
             gp += p.ld_gate;
             next += p.gate_rows;
           }
-          v *= *gp;
+          acc[j] *= *gp;
         }
-        if (p.residual) v += E::get(res[j]);
-        *o = E::put(v);
       }
     }
+  }
+  if (p.residual) {
+#pragma unroll
+    for (int j = 0; j < 16; ++j) acc[j] += E::get(res[j]);
+  }
+  if (count == 16) {
+#pragma unroll
+    for (int j = 0; j < 16; ++j, o += ld) *o = E::put(acc[j]);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 16; ++j, o += ld)
+      if (j < count) *o = E::put(acc[j]);
   }
 }
 
@@ -211,8 +229,10 @@ struct RingPos {
 // direction by about 2^-26 of its magnitude per 16 products (measured 3.7e-6 relative for inner = 5120, fp32's own
 // rounding giving 1e-7).  That is far below the rounding of a 16-bit output but not of an fp32 one, so there the sum is
 // cut into chunks of kChunkK: each chunk gets a fresh accumulator, and the epilogue warps add the chunks with
-// round-to-nearest into a total that stays in tensor memory.
-constexpr int kChunkK = 1024;
+// round-to-nearest.  Relative errors at 300 x 6144 x 512: 1.0e-6 with chunks of 1024, 7.3e-7 with 768, 4.8e-7 with 512; times at
+// 4680 x 6144 x 1536 with gate and residual: 92, 96 and 105 us (a whole sum: 89), since the products two chunks on wait until
+// an accumulator has been read, and tensor memory is read slowly under products.
+constexpr int kChunkK = 768;
 constexpr int kChunkIters = kChunkK / kTileK;
 
 // ---- few tokens: a cluster per tile, which splits `inner` ---------------------------------------
@@ -222,6 +242,7 @@ constexpr int kChunkIters = kChunkK / kTileK;
 // cluster barrier every CTA adds up its share of the tokens from all of them (distributed shared memory, always in the
 // order of the ranks) and runs the epilogue on it.  No workspace, no atomics, equal calls give equal bits.
 constexpr int kTileThreads = 192;                    // four epilogue warps, producer, issuer
+constexpr int kMaxTileFew = 64;                      // tokens per tile
 constexpr int kMaxSplit = 8;                         // portable cluster size
 
 struct TileSmem {
@@ -236,50 +257,43 @@ __host__ __device__ constexpr uint32_t tile_tmem_cols(int tile_t, bool with_tota
   return cols;
 }
 
-// Drains the accumulators (BUFFERS of them in turn, the total behind them) of all chunks but the last into the total: a warp's 32 features, its columns below `cols` in sets
-// of 16 from column_of(0), column_of(1) ..., which rise.  Returns false when a wait gave up.  `release` tells the issuer
-// that an accumulator is free again.
-template <int BUFFERS, class Column, class Release>
+// Adds the accumulators of all chunks (BUFFERS of them in turn) and leaves the total in the tensor memory columns behind them:
+// a warp's 32 features, SETS sets of 16 columns below `cols`, set i from column_of(i) on.  Between chunks the total is in
+// registers.  Returns false when a wait gave up.  `release` tells the issuer that an accumulator is free
+// again, as soon as it is read: the products two chunks on wait for it, and those of the next tile would otherwise wait
+// for the epilogue.
+template <int BUFFERS, int SETS, class Column, class Release>
 __device__ __forceinline__ bool add_chunks(int chunks, uint32_t lanes, int acc_stride, Column column_of, int cols, RingPos& r,
                                            uint64_t* acc_full, unsigned int* status, Release release) {
-  for (int c = 0; c < chunks - 1; ++c) {
+  float sum[SETS][16];
+#pragma unroll
+  for (int i = 0; i < SETS; ++i)
+#pragma unroll
+    for (int j = 0; j < 16; ++j) sum[i][j] = 0.f;
+#pragma unroll 1
+  for (int c = 0; c < chunks; ++c) {
     if (!__all_sync(0xffffffffu, wait_for(&acc_full[r.stage], r.phase, status, kWaitLimitNs))) return false;
     tc_fence_after();
-    const uint32_t part = lanes + r.stage * acc_stride, total = lanes + BUFFERS * acc_stride;
-#pragma unroll 1
-    for (int i = 0; column_of(i) < cols; ++i) {
-      const int col = column_of(i);
-      float v[16], sum[16];
-      tmem_ld16(part + col, reinterpret_cast<uint32_t(&)[16]>(v));
-      if (c > 0) tmem_ld16(total + col, reinterpret_cast<uint32_t(&)[16]>(sum));
-      tmem_wait_ld();
-      if (c > 0) {
+    const uint32_t part = lanes + r.stage * acc_stride;
 #pragma unroll
-        for (int j = 0; j < 16; ++j) v[j] += sum[j];
+    for (int i = 0; i < SETS; ++i)
+      if (column_of(i) < cols) {
+        float v[16];
+        tmem_ld16(part + column_of(i), reinterpret_cast<uint32_t(&)[16]>(v));
+        tmem_wait_ld();
+#pragma unroll
+        for (int j = 0; j < 16; ++j) sum[i][j] += v[j];
       }
-      tmem_st16(total + col, reinterpret_cast<uint32_t(&)[16]>(v));
-    }
-    tmem_wait_st();
     tc_fence_before();
     __syncwarp();
     release(r.stage);
     r.next(BUFFERS);
   }
-  return true;
-}
-
-// The accumulator of the last chunk plus the total of the others, 16 columns.
-template <int BUFFERS>
-__device__ __forceinline__ void load_sum16(float (&acc)[16], uint32_t lanes, int acc_stride, int stage, int col, bool with_total) {
-  tmem_ld16(lanes + stage * acc_stride + col, reinterpret_cast<uint32_t(&)[16]>(acc));
-  if (with_total) {
-    float sum[16];
-    tmem_ld16(lanes + BUFFERS * acc_stride + col, reinterpret_cast<uint32_t(&)[16]>(sum));
-    tmem_wait_ld();
 #pragma unroll
-    for (int j = 0; j < 16; ++j) acc[j] += sum[j];
-  }
-  tmem_wait_ld();
+  for (int i = 0; i < SETS; ++i)
+    if (column_of(i) < cols) tmem_st16(lanes + BUFFERS * acc_stride + column_of(i), reinterpret_cast<uint32_t(&)[16]>(sum[i]));
+  tmem_wait_st();
+  return true;
 }
 
 template <int OutType>
@@ -370,23 +384,28 @@ __global__ void __launch_bounds__(kTileThreads) linear_tile_kernel(const __grid_
     const int n = n0 + warp * 32 + lane;
     const float b = p.bias && n < p.cols ? p.bias[n] : 0.f;
     RingPos r;
-    bool ok = true;
-    if (kChunked)
-      ok = add_chunks<1>(chunks, lanes, p.tile_t, [](int i) { return 16 * i; }, m_end - m0, r, &sm.acc_full, p.status, [&](int) {
+    const bool summed = kChunked && chunks > 1;
+    bool ok;
+    if (summed)
+      ok = add_chunks<1, kMaxTileFew / 16>(chunks, lanes, p.tile_t, [](int i) { return 16 * i; }, m_end - m0, r, &sm.acc_full, p.status, [&](int) {
         if (lane == 0) mbar_arrive(&sm.acc_empty);
       });
-    if (ok) ok = __all_sync(0xffffffffu, wait_for(&sm.acc_full, r.phase, p.status, kWaitLimitNs));
+    else
+      ok = __all_sync(0xffffffffu, wait_for(&sm.acc_full, r.phase, p.status, kWaitLimitNs));
     if (ok) {
       tc_fence_after();
+      const uint32_t sums = lanes + (summed ? p.tile_t : 0);
+      const TileGate gate = tile_gate(p, n, m0, m_end);
       float* mine = reinterpret_cast<float*>(buf) + warp * 32 + lane;      // [token][128 features]: the ring is read and free
 #pragma unroll 1
       for (int c = 0; m0 + c < m_end; c += 16) {
         float acc[16];
         T res[16];
         if (p.split == 1) load_residual16<OutType>(p, res, n, m0 + c, m_end);
-        load_sum16<1>(acc, lanes, p.tile_t, 0, c, chunks > 1);
+        tmem_ld16(sums + c, reinterpret_cast<uint32_t(&)[16]>(acc));
+        tmem_wait_ld();
         if (p.split == 1) {
-          epilogue16<OutType>(p, acc, res, n, m0 + c, m_end, b);
+          epilogue16<OutType>(p, acc, res, n, m0 + c, m_end, b, gate);
         } else {
 #pragma unroll
           for (int j = 0; j < 16; ++j) mine[(c + j) * kTileF] = acc[j];
@@ -403,6 +422,7 @@ __global__ void __launch_bounds__(kTileThreads) linear_tile_kernel(const __grid_
       const int n = n0 + warp * 32 + lane;
       const float b = p.bias && n < p.cols ? p.bias[n] : 0.f;
       const uint32_t mine = smem_u32(buf) + (warp * 32 + lane) * 4;
+      const TileGate gate = tile_gate(p, n, m0 + first, m0 + last);
 #pragma unroll 1
       for (int c = first; c < last; c += 16) {
         T res[16];
@@ -417,7 +437,7 @@ __global__ void __launch_bounds__(kTileThreads) linear_tile_kernel(const __grid_
           for (int j = 0; j < 16; ++j)
             if (c + j < last) acc[j] += ld_cluster_f32(from + (c + j) * kTileF * 4);
         }
-        epilogue16<OutType>(p, acc, res, n, m0 + c, m0 + last, b);
+        epilogue16<OutType>(p, acc, res, n, m0 + c, m0 + last, b, gate);
       }
     }
     __syncwarp();
@@ -436,12 +456,18 @@ __global__ void __launch_bounds__(kTileThreads) linear_tile_kernel(const __grid_
 // accumulator lanes) and fetches half of the token tile, and one tcgen05.mma of the even CTA reads both halves, so that a
 // token tile crosses into shared memory once per pair.  Accumulators are double-buffered in tensor memory (2 x 256
 // columns): the epilogue of one tile runs under the products of the next.
+//
+// What bounds it: per stage of 64 elements a CTA's tensor core takes 2 tile_t clocks, and its shared memory 256 + tile_t
+// (16 KB of weights and 64 tile_t bytes of tokens, written once and read once, at 128 bytes a clock; measured over `inner`:
+// 167, 190, 240 and 340 ns a stage for 64, 128, 176 and 256 tokens).  So tiles of 256 tokens are balanced and smaller ones
+// wait for shared memory; on long runs the power cap holds both back.  4680 x 5120 x 5120 with gate and residual: tensor
+// pipe active 89% of the time.  Under the power cap, back to back: 4680 x 5120 x 15360 567 us (1298 TFLOP/s; a library product
+// alone 542-557 on one box), x 20480 with GELU 756 (724-733 without).
 constexpr int kEpiWarps = 8;
 constexpr int kPairThreads = 32 * (kEpiWarps + 2);
 constexpr int kPairSmem = 227 * 1024 - 512;          // dynamic shared memory of a CTA; the barriers are static
-// Tensor memory columns of the two accumulators; a chunked sum keeps its running total in a third set.  (Held in registers
-// between chunks, 2 or 3 blocks of 32 totals a thread spilled others into the epilogue's loop: up to 2x the time.)
-constexpr int kMaxTileChunked = 160;
+// Tokens per tile of a chunked sum: a thread holds half of them between chunks.
+constexpr int kMaxTileChunked = 128;
 template <int OutType>
 constexpr int kAccStride = OutType == SDVG_F32 ? kMaxTileChunked : kMaxTileT;
 
@@ -568,34 +594,40 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
       const int m0 = tt * p.tile_t, m_end = min(p.rows, m0 + p.tile_t);
       const float bias = p.bias && n < p.cols ? p.bias[n] : 0.f;
       // this warp's columns: blocks of 32 from 32 half on, 64 apart, handled as two halves of 16
+      const TileGate gate = tile_gate(p, n, m0, m_end);
       T ahead0[16], ahead1[16];
       load_residual16<OutType>(p, ahead0, n, m0 + half * 32, m_end);
       load_residual16<OutType>(p, ahead1, n, m0 + half * 32 + 16, m_end);
       auto release = [&](int stage) {
         if (lane == 0) mbar_arrive_cluster(stage ? empty1 : empty0);
       };
-      if (kChunked) {
-        ok = add_chunks<2>(chunks, lanes, kAccStride<OutType>, [&](int i) { return (i / 2 * 2 + half) * 32 + (i & 1) * 16; },
-                        m_end - m0, r, sm.acc_full, p.status, release);
-        if (!ok) break;
-      }
-      ok = __all_sync(0xffffffffu, wait_for(&sm.acc_full[r.stage], r.phase, p.status, kWaitLimitNs));
+      const bool summed = kChunked && chunks > 1;
+      if (summed)
+        ok = add_chunks<2, kMaxTileChunked / 32>(
+            chunks, lanes, kAccStride<OutType>, [&](int i) { return (i / 2 * 2 + half) * 32 + (i & 1) * 16; }, m_end - m0, r,
+            sm.acc_full, p.status, release);
+      else
+        ok = __all_sync(0xffffffffu, wait_for(&sm.acc_full[r.stage], r.phase, p.status, kWaitLimitNs));
       if (!ok) break;
       tc_fence_after();
+      const uint32_t sums = lanes + (summed ? 2 : r.stage) * kAccStride<OutType>;
 #pragma unroll 1
       for (int col = half * 32; m0 + col < m_end; col += 64) {
         float acc0[16], acc1[16];
-        load_sum16<2>(acc0, lanes, kAccStride<OutType>, r.stage, col, kChunked && chunks > 1);
-        load_sum16<2>(acc1, lanes, kAccStride<OutType>, r.stage, col + 16, kChunked && chunks > 1);
-        epilogue16<OutType>(p, acc0, ahead0, n, m0 + col, m_end, bias);
+        tmem_ld16(sums + col, reinterpret_cast<uint32_t(&)[16]>(acc0));
+        tmem_ld16(sums + col + 16, reinterpret_cast<uint32_t(&)[16]>(acc1));
+        tmem_wait_ld();
+        epilogue16<OutType>(p, acc0, ahead0, n, m0 + col, m_end, bias, gate);
         load_residual16<OutType>(p, ahead0, n, m0 + col + 64, m_end);
-        epilogue16<OutType>(p, acc1, ahead1, n, m0 + col + 16, m_end, bias);
+        epilogue16<OutType>(p, acc1, ahead1, n, m0 + col + 16, m_end, bias, gate);
         load_residual16<OutType>(p, ahead1, n, m0 + col + 80, m_end);
       }
-      tc_fence_before();
-      __syncwarp();
-      release(r.stage);
-      r.next(2);
+      if (!summed) {
+        tc_fence_before();
+        __syncwarp();
+        release(r.stage);
+        r.next(2);
+      }
     }
   }
   __syncwarp();
@@ -629,7 +661,7 @@ std::mutex g_setup_mu;
 
 // More tokens than this go to the pairs.  At 5120 x 5120: 64 tokens 17.7 us (clusters of four) against 19.5, 128 tokens 20.6
 // (clusters of two) against 19.4.
-constexpr int kPairRows = 64;
+constexpr int kPairRows = kMaxTileFew;
 
 // Tokens per tile of the pairs: the size whose waves of tiles cost least.  A tile's time grows linearly with its tokens on
 // top of a part that does not depend on them (the features' operand tiles come in whatever the token count), worth about
@@ -651,7 +683,6 @@ int pair_tile(int rows, int tiles_f, int pairs, int largest) {
   return best;
 }
 
-constexpr int kMaxTileFew = kPairRows;               // tokens per tile of the clusters
 constexpr int kTileStages = 4;
 constexpr int kTileDynamic = kTileStages * (kTileF + kMaxTileFew) * 128 + 1024;
 
@@ -752,7 +783,8 @@ int sdvg_linear(const void* x, int64_t ld_x, const void* w, int64_t ld_w, const 
                 void* stream) {
   SDVG_RANGE();
   constexpr int kMaxExtent = 0x7fffffff - 1024;                  // a tile's end past the matrix's is still an int
-  if (rows < 0 || cols < 0 || inner < 1 || rows > kMaxExtent || cols > kMaxExtent || inner > kMaxExtent)
+  constexpr int kMaxInner = 1 << 26;                             // one sum stays far below the limit of a wait
+  if (rows < 0 || cols < 0 || inner < 1 || rows > kMaxExtent || cols > kMaxExtent || inner > kMaxInner)
     return SDVG_ERR_BAD_SHAPE;
   if ((in_type != SDVG_BF16 && in_type != SDVG_F16) || !sdvg::elem_type_ok(out_type)) return SDVG_ERR_INVALID_ARG;
   if (act < SDVG_ACT_NONE || act > SDVG_ACT_GELU || (gate && gate_rows < 1)) return SDVG_ERR_INVALID_ARG;

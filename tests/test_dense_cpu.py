@@ -27,7 +27,7 @@ def linear_args(**change):
 
 @pytest.mark.parametrize("change,status", [
     (dict(rows=-1), "BAD_SHAPE"), (dict(cols=-1), "BAD_SHAPE"), (dict(inner=0), "BAD_SHAPE"),
-    (dict(rows=0x7fffffff, ld_x=64), "BAD_SHAPE"), (dict(ld_x=56), "BAD_SHAPE"), (dict(ld_w=56), "BAD_SHAPE"),
+    (dict(rows=0x7fffffff, ld_x=64), "BAD_SHAPE"), (dict(inner=(1 << 26) + 1, ld_x=1 << 27, ld_w=1 << 27), "BAD_SHAPE"), (dict(ld_x=56), "BAD_SHAPE"), (dict(ld_w=56), "BAD_SHAPE"),
     (dict(ld_out=31), "BAD_SHAPE"), (dict(residual=R, ld_residual=31), "BAD_SHAPE"), (dict(residual=R, ld_residual=-32), "BAD_SHAPE"),
     (dict(gate=G, gate_rows=2, ld_gate=31), "BAD_SHAPE"), (dict(ld_x=1 << 40), "BAD_SHAPE"),
     (dict(in_type=2), "INVALID_ARG"), (dict(in_type=-1), "INVALID_ARG"), (dict(out_type=3), "INVALID_ARG"),

@@ -79,6 +79,106 @@ def test_shapes(rows, cols, inner, dtype, out):
     check(problem(rows, cols, inner, dtype, out, gate_rows=max(1, rows // 3), residual="rows", seed=rows + cols + inner))
 
 
+@pytest.mark.parametrize("rows,cols,inner", [(1, 100, 9001), (2, 129, 1030), (16, 130, 2048), (31, 257, 4097), (33, 129, 5000),
+                                             (48, 500, 1500), (64, 1000, 2050), (64, 128, 20000), (65, 130, 4000)])
+@pytest.mark.parametrize("dtype,out", [("bf16", "fp32"), ("fp16", "fp16")])
+def test_few_rows_share_long_sums(rows, cols, inner, dtype, out):
+    """Up to 64 rows: clusters that split the inner axis unevenly, chunks of fp32 sums that end inside a part."""
+    check(problem(rows, cols, inner, dtype, out, gate_rows=5, residual="rows", act="silu", seed=inner))
+
+
+@pytest.mark.parametrize("rows,cols,inner", [(3, 1024, 5120), (64, 256, 6144), (300, 512, 6144), (257, 256, 20000)])
+def test_fp32_outputs_keep_fp32_accuracy_over_long_sums(rows, cols, inner):
+    """Accumulated in one go, the tensor core's truncation drifts: 3.7e-6 at inner 5120, and more beyond.  In chunks of 768 it stays
+    at most 48 truncated additions of 2^-23 of a partial sum that is on average far below the full one: under 2^-20."""
+    s = problem(rows, cols, inner, out="fp32", bias=False)
+    out = torch.empty((rows, cols), device="cuda")
+    call(s, out, api.attn_workspace())
+    ref = s["x"].double() @ s["w"].double().t()
+    assert float((out.double() - ref).norm() / ref.norm()) <= 2.0 ** -20
+
+
+def test_two_graphs_that_share_a_workspace_replay_at_once():
+    ws = api.attn_workspace()
+    cases = []
+    for rows, cols, inner in ((8, 512, 4096), (700, 512, 1024)):
+        s = problem(rows, cols, inner, act="silu", seed=rows)
+        out = torch.empty((rows, cols), device="cuda", dtype=torch.bfloat16)
+        call(s, out, ws)
+        want, graph, stream = out.clone(), torch.cuda.CUDAGraph(), torch.cuda.Stream()
+        torch.cuda.synchronize()
+        with torch.cuda.graph(graph, stream=stream):
+            for _ in range(5):
+                call(s, out, ws)
+        out.zero_()
+        cases.append((out, want, graph, stream))
+    torch.cuda.synchronize()
+    for _ in range(10):
+        for _, _, graph, stream in cases:
+            with torch.cuda.stream(stream):
+                graph.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(out, want) for out, want, _, _ in cases)
+    assert api.sdvg_block_attn_status(ws) == api.SDVG_OK
+
+
+def test_calls_from_two_threads():
+    import threading
+    results, failures = {}, []
+
+    def work(i):
+        try:
+            torch.cuda.set_device(0)
+            s = problem(40 + 300 * i, 200, 700, act="gelu", seed=i)
+            stream = torch.cuda.Stream()
+            ws = api.attn_workspace()
+            out = torch.empty((s["x"].shape[0], 200), device="cuda", dtype=torch.bfloat16)
+            torch.cuda.synchronize()
+            for _ in range(50):
+                call(s, out, ws, stream=stream)
+            stream.synchronize()
+            results[i] = (s, out)
+        except Exception as e:                                # reported by the main thread
+            failures.append(e)
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not failures, failures
+    for s, out in results.values():
+        ref, tol = expected(s)
+        assert_close(out, ref, tol)
+
+
+def test_a_row_of_dependent_calls_sees_each_others_results():
+    """Launches overlap the end of the one before; their reads must not."""
+    gen = torch.Generator(device="cuda").manual_seed(31)
+    ws = api.attn_workspace()
+    w = [strided(gen, 256, 256, torch.bfloat16, std=1 / 16) for _ in range(3)]
+    for rows in (3, 64, 500):
+        x = strided(gen, rows, 256, torch.bfloat16)
+        bufs = [torch.zeros((rows, 256), device="cuda", dtype=torch.bfloat16) for _ in range(3)]
+
+        def chain(sync):
+            cur = x
+            for i in range(30):
+                api.sdvg_linear(cur, w[i % 3], bufs[i % 3], ws, act=api.SDVG_ACT_SILU if i % 2 else api.SDVG_ACT_NONE, residual=cur)
+                if sync:
+                    torch.cuda.synchronize()
+                api.sdvg_gated_norm(bufs[i % 3], bufs[i % 3])
+                if sync:
+                    torch.cuda.synchronize()
+                cur = bufs[i % 3]
+            torch.cuda.synchronize()
+            return cur.clone()
+
+        want = chain(True)
+        assert all(torch.equal(chain(False), want) for _ in range(5))
+        assert bool(torch.isfinite(want.float()).all())
+
+
 @pytest.mark.parametrize("act", list(ACTS))
 @pytest.mark.parametrize("dtype,out", [("bf16", "bf16"), ("fp16", "fp16"), ("bf16", "fp32"), ("fp16", "fp32")])
 @pytest.mark.parametrize("rows", [5, 270])
