@@ -617,43 +617,21 @@ def sdvg_block_attn_fwd_e4m3_batched(q8s, k_self8s, v_self8s, caches, block_indi
 
 
 # ---------------------------------------------------------------- dense operators around the attention
+#
+# Their kernels take a few microseconds on small inputs, so that their arguments are read and checked in a compiled module
+# (csrc/binding.cpp; ValueError for tensors that do not fit).
 
-_ELEM_TYPES = {torch.bfloat16: SDVG_BF16, torch.float16: SDVG_F16, torch.float32: SDVG_F32}
-
-# The checks below sit on the path of calls whose kernels take a few microseconds: attributes are compared without building
-# intermediate objects, and the messages are only made for a call that is refused.
-
-
-def _matrix(t: torch.Tensor, dev: int, shape: tuple, dtype: torch.dtype, what: str):
-    """(pointer, row stride) of a matrix with unit column stride on CUDA device `dev`."""
-    if t.dtype is not dtype or t.shape != shape or t.get_device() != dev:
-        raise ValueError(f"{what}: expected {dtype} {list(shape)} on cuda:{dev}, got {t.dtype} {list(t.shape)} on {t.device}")
-    ld, step = t.stride()
-    if step != 1 and shape[1] > 1:
-        raise ValueError(f"{what}: columns must be contiguous")
-    return t.data_ptr(), ld
+_compiled = None
 
 
-def _vector(t: Optional[torch.Tensor], dev: int, n: int, what: str):
-    if t is None:
-        return None
-    if t.dtype is not torch.float32 or t.shape != (n,) or t.get_device() != dev or not t.is_contiguous():
-        raise ValueError(f"{what}: expected contiguous float32 [{n}] on cuda:{dev}, got {t.dtype} {list(t.shape)} on {t.device}")
-    return t.data_ptr()
-
-
-def _groups(t: Optional[torch.Tensor], dev: int, rows: int, cols: int, group_rows: int, what: str):
-    """Vectors that change with the row group: one row per `group_rows` rows."""
-    if t is None:
-        return None, 0
-    if group_rows < 1:
-        raise ValueError(f"{what}: rows per group must be given")
-    return _matrix(t, dev, (-(-rows // group_rows), cols), torch.float32, what)
-
-
-def _raw_stream(dev: int, stream) -> int:
-    """The stream to launch on: the caller's, or the current one of CUDA device `dev`, which must be current."""
-    return torch._C._cuda_getCurrentRawStream(dev) if stream is None else _stream(stream)
+def _binding():
+    global _compiled
+    if _compiled is None:
+        if not os.path.exists(os.path.join(_HERE, "_binding.so")):
+            raise RuntimeError("_binding.so not found: run `python -m paper_2604_17397_b200.build` first")
+        from . import _binding as compiled
+        _compiled = compiled
+    return _compiled
 
 
 def _device_of(t: torch.Tensor) -> int:
@@ -668,31 +646,23 @@ def _elsewhere(dev: int) -> bool:
     return dev != torch._C._cuda_getDevice()
 
 
+def _raw_stream(dev: int, stream) -> int:
+    """The stream to launch on: the caller's, or the current one of CUDA device `dev`, which must be current."""
+    return torch._C._cuda_getCurrentRawStream(dev) if stream is None else _stream(stream)
+
+
 def sdvg_linear(x, w, out, workspace, bias=None, act: int = SDVG_ACT_NONE, residual=None, gate=None, gate_rows: int = 0,
                 stream=None) -> None:
     """out = residual + gate[row // gate_rows] * act(x @ w.T + bias): x [rows, inner] and w [cols, inner] bf16 or fp16,
     out and residual [rows, cols] of one type, bias fp32 [cols], gate fp32 [groups, cols].  Row strides are free
     (x and w: multiples of 8; residual may be one expanded row); residual may be `out`."""
-    rows, inner = x.shape
-    cols = w.shape[0]
-    in_type, out_type = _ELEM_TYPES.get(x.dtype), _ELEM_TYPES.get(out.dtype)
-    if in_type is None or in_type == SDVG_F32 or out_type is None:
-        raise ValueError("x must be bfloat16 or float16, out one of these or float32")
     dev = _device_of(x)
     if _elsewhere(dev):
         with torch.cuda.device(dev):
             return sdvg_linear(x, w, out, workspace, bias, act, residual, gate, gate_rows, stream)
-    if workspace.get_device() != dev:
-        raise ValueError("workspace must be on the tensors' device")
-    xp, ld_x = _matrix(x, dev, (rows, inner), x.dtype, "x")
-    wp, ld_w = _matrix(w, dev, (cols, inner), x.dtype, "w")
-    op, ld_out = _matrix(out, dev, (rows, cols), out.dtype, "out")
-    rp, ld_res = (None, 0) if residual is None else _matrix(residual, dev, (rows, cols), out.dtype, "residual")
-    gp, ld_gate = _groups(gate, dev, rows, cols, gate_rows, "gate")
-    st = lib().sdvg_linear(xp, ld_x, wp, ld_w, _vector(bias, dev, cols, "bias"), act, gp, ld_gate, gate_rows, rp, ld_res, op,
-                           ld_out, rows, cols, inner, in_type, out_type, workspace.data_ptr(), workspace.numel(),
-                           _raw_stream(dev, stream))
-    _check(st, "sdvg_linear")
+    st = _binding().linear(x, w, out, workspace, bias, act, residual, gate, gate_rows, _raw_stream(dev, stream))
+    if st != SDVG_OK:
+        raise SdvgError(st, "sdvg_linear")
 
 
 def sdvg_gated_norm(x, out, y=None, gate=None, gate_rows: int = 0, post_norm: int = SDVG_NORM_NONE, post_weight=None,
@@ -702,77 +672,32 @@ def sdvg_gated_norm(x, out, y=None, gate=None, gate_rows: int = 0, post_norm: in
     out = (norm(s) * weight + bias) * (1 + scale[row // modulate_rows]) + shift[row // modulate_rows].
     x, y, x_out, out: [rows, cols] of bf16, fp16 or fp32 (x_out has x's type; out may be None when x_out is given);
     vectors fp32 [cols], gate / scale / shift fp32 [groups, cols]."""
-    shape = x.shape
-    rows, cols = shape
-    types = _ELEM_TYPES
-    if x.dtype not in types or (y is not None and y.dtype not in types) or (out is not None and out.dtype not in types):
-        raise ValueError("expected bfloat16, float16 or float32 tensors")
     dev = _device_of(x)
     if _elsewhere(dev):
         with torch.cuda.device(dev):
             return sdvg_gated_norm(x, out, y, gate, gate_rows, post_norm, post_weight, x_out, norm, weight, bias, scale, shift,
                                    modulate_rows, eps, stream)
-    xp, ld_x = _matrix(x, dev, shape, x.dtype, "x")
-    yp, ld_y, y_type = None, 0, 0
-    if y is not None:
-        yp, ld_y = _matrix(y, dev, shape, y.dtype, "y")
-        y_type = types[y.dtype]
-    xo, ld_xo = (None, 0) if x_out is None else _matrix(x_out, dev, shape, x.dtype, "x_out")
-    op, ld_out, out_type = None, 0, 0
-    if out is not None:
-        op, ld_out = _matrix(out, dev, shape, out.dtype, "out")
-        out_type = types[out.dtype]
-    gp, ld_gate = _groups(gate, dev, rows, cols, gate_rows, "gate")
-    sp, ld_mod = _groups(scale, dev, rows, cols, modulate_rows, "scale")
-    hp, ld_shift = _groups(shift, dev, rows, cols, modulate_rows, "shift")
-    if sp is None:
-        ld_mod = ld_shift
-    elif hp is not None and ld_mod != ld_shift and rows > modulate_rows:
-        raise ValueError("scale and shift must have the same row stride")
-    st = lib().sdvg_gated_norm(xp, ld_x, types[x.dtype], yp, ld_y, y_type, post_norm,
-                               _vector(post_weight, dev, cols, "post_weight"), gp, ld_gate, gate_rows, xo, ld_xo, norm,
-                               _vector(weight, dev, cols, "weight"), _vector(bias, dev, cols, "bias"), sp, hp, ld_mod,
-                               modulate_rows, eps, op, ld_out, out_type, rows, cols, _raw_stream(dev, stream))
-    _check(st, "sdvg_gated_norm")
-
-
-def _tokens(t: torch.Tensor, dev: int, shape: tuple, what: str, contiguous: bool = False):
-    """(pointer, token stride) of a bf16 [block_tokens, heads, head_dim] tensor that is contiguous within a token."""
-    if t.dtype is not torch.bfloat16 or t.shape != shape or t.get_device() != dev:
-        raise ValueError(f"{what}: expected bfloat16 {list(shape)} on cuda:{dev}, got {t.dtype} {list(t.shape)} on {t.device}")
-    tokens, heads, dim = shape
-    ld, head, step = t.stride()
-    if step != 1 or (head != dim and heads > 1):
-        raise ValueError(f"{what}: the heads of a token must be contiguous")
-    if tokens == 1:
-        ld = heads * dim
-    if contiguous and ld != heads * dim:
-        raise ValueError(f"{what} must be contiguous")
-    return t.data_ptr(), ld
+    st = _binding().gated_norm(x, out, y, gate, gate_rows, post_norm, post_weight, x_out, norm, weight, bias, scale, shift,
+                               modulate_rows, eps, _raw_stream(dev, stream))
+    if st != SDVG_OK:
+        raise SdvgError(st, "sdvg_gated_norm")
 
 
 def sdvg_qk_norm_rope3d_commit(cache: Cache, q, k, v, q_weight, k_weight, scope: int, eps: float, q_out, k_out, grid,
                                frame_offset: int, table, tab_frames: int, block_index: int, flags: int, stream=None) -> int:
     """sdvg_rope3d_qk_commit with an RMS norm of q and k first; q, k, v may be column ranges of a wider QKV product
     viewed as [tokens, heads, head_dim].  Returns the evicted block."""
-    shape = (cache.block_tokens, cache.heads, cache.head_dim)
-    width = shape[1] * shape[2] if scope == SDVG_SCOPE_ROW else shape[2]
     dev = cache._k_raw.get_device()
     if _elsewhere(dev):
         with torch.cuda.device(dev):
             return sdvg_qk_norm_rope3d_commit(cache, q, k, v, q_weight, k_weight, scope, eps, q_out, k_out, grid, frame_offset,
                                               table, tab_frames, block_index, flags, stream)
-    qp, ld_q = (None, 0) if q is None else _tokens(q, dev, shape, "q")
-    kp, ld_k = _tokens(k, dev, shape, "k")
-    vp, ld_v = _tokens(v, dev, shape, "v")
-    qo = None if q_out is None else _tokens(q_out, dev, shape, "q_out", True)[0]
-    ko = None if k_out is None else _tokens(k_out, dev, shape, "k_out", True)[0]
+    if k.get_device() != dev:
+        raise ValueError("k must be on the cache's device")
     frames, grid_h, grid_w = grid
-    ev = _I64(-1)
-    st = lib().sdvg_qk_norm_rope3d_commit(cache.handle, qp, ld_q, kp, ld_k, vp, ld_v,
-                                          _vector(q_weight, dev, width, "q_weight"),
-                                          _vector(k_weight, dev, width, "k_weight"), scope, eps, qo, ko, frames, grid_h,
-                                          grid_w, frame_offset, _ptr(table), tab_frames, block_index, flags, C.byref(ev),
-                                          _raw_stream(dev, stream))
-    _check(st, "sdvg_qk_norm_rope3d_commit")
-    return ev.value
+    evicted = _binding().qk_norm(cache.handle.value or 0, cache.block_tokens, cache.heads, cache.head_dim, q, k, v, q_weight,
+                                 k_weight, scope, eps, q_out, k_out, frames, grid_h, grid_w, frame_offset, table, tab_frames,
+                                 block_index, flags, _raw_stream(dev, stream))
+    if evicted < -1:
+        raise SdvgError(-1000 - evicted, "sdvg_qk_norm_rope3d_commit")
+    return evicted

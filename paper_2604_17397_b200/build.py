@@ -14,6 +14,9 @@ SOURCES = ["sdvg_host.cu", "rope_commit.cu", "route.cu", "state.cu", "quant.cu",
            "linear.cu", "gated_norm.cu", "qk_norm.cu"]
 
 
+BINDING_PATH = os.path.join(HERE, "_binding.so")
+
+
 def nvcc_path() -> str:
     for cand in (os.environ.get("NVCC"), shutil.which("nvcc"), "/usr/local/cuda/bin/nvcc"):
         if cand and os.path.exists(cand):
@@ -31,6 +34,8 @@ def needs_build(out: str = LIB_PATH) -> bool:
 
 def build(force: bool = False, out: str = LIB_PATH, extra_flags=(), verbose: bool = False) -> str:
     if not force and not needs_build(out):
+        if out == LIB_PATH:
+            build_binding()
         return out
     cmd = [nvcc_path(), "-shared", "-Xcompiler", "-fPIC", "-std=c++17", "-O3", "-lineinfo",
            "-gencode", "arch=compute_100a,code=sm_100a",
@@ -40,7 +45,29 @@ def build(force: bool = False, out: str = LIB_PATH, extra_flags=(), verbose: boo
     if verbose:
         print(" ".join(cmd), file=sys.stderr)
     subprocess.run(cmd, check=True)
+    if out == LIB_PATH:
+        build_binding(force)
     return out
+
+
+def build_binding(force: bool = False) -> str:
+    """The compiled argument marshalling of the dense operators: links the library and torch's Python types."""
+    sources = [os.path.join(CSRC, "binding.cpp"), os.path.join(ROOT, "include", "sdvg.h")]
+    if not force and os.path.exists(BINDING_PATH) and all(os.path.getmtime(s) <= os.path.getmtime(BINDING_PATH) for s in sources):
+        return BINDING_PATH
+    import sysconfig
+
+    import torch
+    torch_dir = os.path.dirname(torch.__file__)
+    include = [os.path.join(torch_dir, "include"), os.path.join(torch_dir, "include", "torch", "csrc", "api", "include"),
+               sysconfig.get_paths()["include"]]
+    libs = os.path.join(torch_dir, "lib")
+    subprocess.run([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-shared", "-fPIC",
+                    f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+                    *[a for d in include for a in ("-isystem", d)], "-I", os.path.join(ROOT, "include"), sources[0], "-o",
+                    BINDING_PATH, LIB_PATH, "-Wl,-rpath,$ORIGIN", "-L" + libs, "-Wl,-rpath," + libs, "-ltorch_python",
+                    "-ltorch_cpu", "-lc10"], check=True)
+    return BINDING_PATH
 
 
 if __name__ == "__main__":

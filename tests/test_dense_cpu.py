@@ -47,6 +47,24 @@ def test_linear_with_nothing_to_do(lib):
     assert lib.sdvg_linear(*linear_args(cols=0, w=None)) == api.SDVG_OK
 
 
+def test_the_binding_refuses_what_is_not_on_a_gpu(lib):
+    x, ws = torch.zeros((2, 16), dtype=torch.bfloat16), torch.zeros(256, dtype=torch.uint8)
+    with pytest.raises(ValueError):
+        api.sdvg_linear(x, x, x, ws)
+    with pytest.raises(ValueError):
+        api.sdvg_gated_norm(x, x)
+    b = api._binding()
+    for call in (lambda: b.linear(x, x, x, ws, None, 0, None, None, 0, 0), lambda: b.linear(None, x, x, ws, None, 0, None, None, 0, 0),
+                 lambda: b.gated_norm(x, x, None, None, 0, 0, None, None, 2, None, None, None, None, 0, 1e-6, 0),
+                 lambda: b.qk_norm(0, 1, 1, 64, None, x, x, None, None, 0, 1e-6, None, None, 1, 1, 1, 0, x, 1, 0, 1, 0)):
+        with pytest.raises(ValueError):
+            call()
+    with pytest.raises(TypeError):
+        b.linear(x)
+    with pytest.raises(TypeError):
+        b.gated_norm(x)
+
+
 def norm_args(**change):
     a = dict(x=X, ld_x=32, x_type=0, y=None, ld_y=0, y_type=0, post=0, post_weight=None, gate=None, ld_gate=0, gate_rows=0,
              x_out=None, ld_x_out=0, norm=2, weight=None, bias=None, scale=None, shift=None, ld_mod=0, mod_rows=0, eps=1e-6,
