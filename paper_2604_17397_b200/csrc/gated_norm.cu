@@ -477,6 +477,7 @@ int device_sms(int* sms) {
 }
 
 constexpr int kMostDynamic = 200 * 1024;
+constexpr int kFreeDynamic = 40 * 1024;                // needs no opt-in, with what the kernel has statically: 48 KB in all
 
 // -1: a team's ring does not fit
 template <int XW, int YW, int NI, bool WARP, bool FULL>
@@ -486,7 +487,7 @@ int launch_team_as(const NormParams& p, int threads, int sms, cudaStream_t strea
   const int dynamic = threads * kSlots * (Ring<XW, NI>::kBytes + Ring<YW, NI>::kBytes);
   if (dynamic > kMostDynamic) return -1;
   int grid = want;
-  if (want > sms || dynamic > 48 * 1024) {
+  if (want > sms || dynamic > kFreeDynamic) {
     // a grid that the device holds at once: teams walk rows of equal number.  Asked again when the shape changes.
     static thread_local int known_dev = -1, known_dynamic = -1, resident = 0;
     int dev = 0;
@@ -495,7 +496,7 @@ int launch_team_as(const NormParams& p, int threads, int sms, cudaStream_t strea
     if (dev != known_dev || dynamic != known_dynamic) {
       auto kernel = gated_norm_kernel<XW, YW, NI, WARP, FULL>;
       known_dev = -1;
-      if (dynamic > 48 * 1024) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostDynamic);
+      if (dynamic > kFreeDynamic) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostDynamic);
       if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&resident, kernel, threads, dynamic);
       if (e != cudaSuccess) return sdvg::cuda_status(e);
       known_dev = dev;

@@ -31,7 +31,9 @@ cudaError_t launch_overlapped(void (*kernel)(Params), unsigned grid, int threads
   attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = cluster > 0 ? 2 : 1;
-  return cudaLaunchKernelEx(&cfg, kernel, params);
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, params);
+  if (e != cudaSuccess) cudaGetLastError();            // reported here; the next call must not find it again
+  return e;
 }
 
 }  // namespace sdvg

@@ -86,6 +86,21 @@ def test_widths(cols, norm, post):
     check(problem(9, cols, norm=norm, post=post, affine=True, mod_rows=4, gate_rows=5, seed=cols, eps=1e-2 if cols < 8 else 1e-6))
 
 
+@pytest.mark.parametrize("rows", [3, 400])
+@pytest.mark.parametrize("x,y", [("fp32", "fp32"), ("fp32", "bf16"), ("bf16", "bf16"), ("bf16", "")])
+def test_every_team_size(rows, x, y):
+    """Widths that differ by a warp of the team, up to the widest: among them rings of just under, at and over 48 KB."""
+    for cols in range(512, 10241, 512 if x == "bf16" else 256):
+        for c in (cols - 8, cols):
+            s = problem(rows, c, x, y, "bf16", gate_rows=rows if y else 0, seed=c)
+            out = torch.full((rows, c), float("nan"), device="cuda", dtype=torch.bfloat16)
+            call(s, None, out)
+            v = s["x"].double() + (s["gate"].double() * s["y"].double() if y else 0)
+            n = (v - v.mean(1, keepdim=True)) / torch.sqrt(v.var(1, keepdim=True, unbiased=False) + 1e-6)
+            # half a step of bf16, and far less for the fp32 arithmetic
+            assert bool(((out.double() - n).abs() <= 2.0 ** -8 * n.abs() + 2.0 ** -14 * (1 + n.abs())).all()), c
+
+
 @pytest.mark.parametrize("x", list(DTYPES))
 @pytest.mark.parametrize("y", ["", *DTYPES])
 @pytest.mark.parametrize("out", list(DTYPES))
