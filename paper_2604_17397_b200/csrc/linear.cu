@@ -228,12 +228,12 @@ struct RingPos {
 // fp32 outputs: the tensor core adds a product to the accumulator by truncation, so a sum over `inner` drifts in one
 // direction by about 2^-26 of its magnitude per 16 products (measured 3.7e-6 relative for inner = 5120, fp32's own
 // rounding giving 1e-7).  That is far below the rounding of a 16-bit output but not of an fp32 one, so there the sum is
-// cut into chunks of kChunkK: each chunk gets a fresh accumulator, and the epilogue warps add the chunks with
-// round-to-nearest.  Relative errors at 300 x 6144 x 512: 1.0e-6 with chunks of 1024, 7.3e-7 with 768, 4.8e-7 with 512; times at
-// 4680 x 6144 x 1536 with gate and residual: 92, 96 and 105 us (a whole sum: 89), since the products two chunks on wait until
-// an accumulator has been read, and tensor memory is read slowly under products.
-constexpr int kChunkK = 768;
-constexpr int kChunkIters = kChunkK / kTileK;
+// cut into chunks: each chunk gets a fresh accumulator, and the epilogue warps add the chunks with round-to-nearest.
+// Relative errors at 300 x 6144 x 512: 1.0e-6 with chunks of 1024, 7.3e-7 with 768, 6.1e-7 with 640, 4.8e-7 with 512.  For many
+// tokens short chunks cost time, since tensor memory is read slowly under products (4680 x 6144 x 1536 with gate and
+// residual: 93, 96 and 100 us with 768, 640 and 512; a whole sum 89); for few they do not.
+constexpr int kPairChunkIters = 640 / kTileK;
+constexpr int kTileChunkIters = 512 / kTileK;
 
 // ---- few tokens: a cluster per tile, which splits `inner` ---------------------------------------
 //
@@ -311,8 +311,8 @@ __global__ void __launch_bounds__(kTileThreads) linear_tile_kernel(const __grid_
   // this CTA's part of `inner`: never empty
   const int share = p.k_iters / p.split, rest = p.k_iters % p.split;
   const int k0 = rank * share + min(rank, rest), iters = share + (rank < rest ? 1 : 0);
-  const int chunks = kChunked ? (iters + kChunkIters - 1) / kChunkIters : 1;
-  const uint32_t tmem_cols = tile_tmem_cols(p.tile_t, kChunked && p.k_iters > kChunkIters);
+  const int chunks = kChunked ? (iters + kTileChunkIters - 1) / kTileChunkIters : 1;
+  const uint32_t tmem_cols = tile_tmem_cols(p.tile_t, kChunked && p.k_iters > kTileChunkIters);
   if (threadIdx.x == 0) {
     for (int s = 0; s < p.stages; ++s) {
       mbar_init(&sm.full[s], 1);
@@ -363,7 +363,7 @@ __global__ void __launch_bounds__(kTileThreads) linear_tile_kernel(const __grid_
       for (int c = 0; ok && c < chunks; ++c, acc.next(1)) {
         if (!(ok = wait_for(&sm.acc_empty, acc.phase ^ 1, p.status, kWaitLimitNs))) break;
         tc_fence_after();
-        const int i0 = c * kChunkIters, i1 = kChunked ? min(iters, i0 + kChunkIters) : iters;
+        const int i0 = c * kTileChunkIters, i1 = kChunked ? min(iters, i0 + kTileChunkIters) : iters;
         for (int i = i0; i < i1; ++i, r.next(p.stages)) {
           const int s = r.stage;
           if (!(ok = wait_for(&sm.full[s], r.phase, p.status, kWaitLimitNs))) break;
@@ -468,11 +468,16 @@ constexpr int kPairThreads = 32 * (kEpiWarps + 2);
 constexpr int kPairSmem = 227 * 1024 - 512;          // dynamic shared memory of a CTA; the barriers are static
 // Tokens per tile of a chunked sum: a thread holds half of them between chunks.
 constexpr int kMaxTileChunked = 128;
+// Accumulators in tensor memory and their columns.  A chunked sum has three (and its total behind them): reading one takes about
+// as long as the products of a chunk, and with two the products waited for it (chunks of 512: 105 against 100 us).
+template <int OutType>
+constexpr int kAccs = OutType == SDVG_F32 ? 3 : 2;
 template <int OutType>
 constexpr int kAccStride = OutType == SDVG_F32 ? kMaxTileChunked : kMaxTileT;
+static_assert((kAccs<SDVG_F32> + 1) * kAccStride<SDVG_F32> <= 512 && kAccs<SDVG_BF16> * kAccStride<SDVG_BF16> <= 512);
 
 struct PairSmem {
-  uint64_t full[kMaxStages], empty[kMaxStages], acc_full[2], acc_empty[2];
+  uint64_t full[kMaxStages], empty[kMaxStages], acc_full[3], acc_empty[3];
   uint32_t tmem;
 };
 
@@ -499,14 +504,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
   const uint32_t rank = cluster_ctarank();
   const int pair = blockIdx.x / 2, pairs = gridDim.x / 2;
   const int w_bytes = kTileF * 128, stage_bytes = w_bytes + p.tile_t * 64;
-  const int chunks = kChunked ? (p.k_iters + kChunkIters - 1) / kChunkIters : 1;
+  const int chunks = kChunked ? (p.k_iters + kPairChunkIters - 1) / kPairChunkIters : 1;
   sdvg::overlap_begin();
   if (threadIdx.x == 0) {
     for (int s = 0; s < p.stages; ++s) {
       mbar_init(&sm.full[s], 1);                     // the even CTA's counts the bytes of both
       mbar_init(&sm.empty[s], 1);
     }
-    for (int b = 0; b < 2; ++b) {
+    for (int b = 0; b < kAccs<OutType>; ++b) {
       mbar_init(&sm.acc_full[b], 1);
       mbar_init(&sm.acc_empty[b], 2 * kEpiWarps);    // the even CTA's: the epilogue warps of both
     }
@@ -560,11 +565,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
       RingPos r, acc;
       bool ok = true;
       for (long long t = pair; ok && t < p.tiles; t += pairs) {
-        for (int c = 0; ok && c < chunks; ++c, acc.next(2)) {
+        for (int c = 0; ok && c < chunks; ++c, acc.next(kAccs<OutType>)) {
           const int b = acc.stage;
           if (!(ok = wait_for(&sm.acc_empty[b], acc.phase ^ 1, p.status, kWaitLimitNs))) break;
           tc_fence_after();
-          const int i0 = c * kChunkIters, i1 = kChunked ? min(p.k_iters, i0 + kChunkIters) : p.k_iters;
+          const int i0 = c * kPairChunkIters, i1 = kChunked ? min(p.k_iters, i0 + kPairChunkIters) : p.k_iters;
           for (int i = i0; i < i1; ++i, r.next(p.stages)) {
             const int s = r.stage;
             if (!(ok = wait_for(&sm.full[s], r.phase, p.status, kWaitLimitNs))) break;
@@ -584,7 +589,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
     // ================= epilogue: warps w and w + 4 share 32 features and take 32-token column blocks in turn ==========
     const int quad = warp % 4, half = warp / 4;
     const uint32_t lanes = tmem + ((uint32_t)(quad * 32) << 16);
-    const uint32_t empty0 = map_to_rank(smem_u32(&sm.acc_empty[0]), 0), empty1 = map_to_rank(smem_u32(&sm.acc_empty[1]), 0);
+    const uint32_t empty = map_to_rank(smem_u32(sm.acc_empty), 0);
     RingPos r;
     bool ok = true;
     for (long long t = pair; ok && t < p.tiles; t += pairs) {
@@ -599,18 +604,18 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
       load_residual16<OutType>(p, ahead0, n, m0 + half * 32, m_end);
       load_residual16<OutType>(p, ahead1, n, m0 + half * 32 + 16, m_end);
       auto release = [&](int stage) {
-        if (lane == 0) mbar_arrive_cluster(stage ? empty1 : empty0);
+        if (lane == 0) mbar_arrive_cluster(empty + 8 * stage);
       };
       const bool summed = kChunked && chunks > 1;
       if (summed)
-        ok = add_chunks<2, kMaxTileChunked / 32>(
+        ok = add_chunks<kAccs<OutType>, kMaxTileChunked / 32>(
             chunks, lanes, kAccStride<OutType>, [&](int i) { return (i / 2 * 2 + half) * 32 + (i & 1) * 16; }, m_end - m0, r,
             sm.acc_full, p.status, release);
       else
         ok = __all_sync(0xffffffffu, wait_for(&sm.acc_full[r.stage], r.phase, p.status, kWaitLimitNs));
       if (!ok) break;
       tc_fence_after();
-      const uint32_t sums = lanes + (summed ? 2 : r.stage) * kAccStride<OutType>;
+      const uint32_t sums = lanes + (summed ? kAccs<OutType> : r.stage) * kAccStride<OutType>;
 #pragma unroll 1
       for (int col = half * 32; m0 + col < m_end; col += 64) {
         float acc0[16], acc1[16];
@@ -626,7 +631,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
         tc_fence_before();
         __syncwarp();
         release(r.stage);
-        r.next(2);
+        r.next(kAccs<OutType>);
       }
     }
   }

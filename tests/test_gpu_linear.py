@@ -89,8 +89,8 @@ def test_few_rows_share_long_sums(rows, cols, inner, dtype, out):
 
 @pytest.mark.parametrize("rows,cols,inner", [(3, 1024, 5120), (64, 256, 6144), (300, 512, 6144), (257, 256, 20000)])
 def test_fp32_outputs_keep_fp32_accuracy_over_long_sums(rows, cols, inner):
-    """Accumulated in one go, the tensor core's truncation drifts: 3.7e-6 at inner 5120, and more beyond.  In chunks of 768 it stays
-    at most 48 truncated additions of 2^-23 of a partial sum that is on average far below the full one: under 2^-20."""
+    """Accumulated in one go, the tensor core's truncation drifts: 3.7e-6 at inner 5120, and more beyond.  In chunks of at most 640 it stays
+    at most 40 truncated additions of 2^-23 of a partial sum that is on average far below the full one: under 2^-20."""
     s = problem(rows, cols, inner, out="fp32", bias=False)
     out = torch.empty((rows, cols), device="cuda")
     call(s, out, api.attn_workspace())
