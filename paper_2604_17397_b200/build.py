@@ -65,7 +65,7 @@ def build_binding(force: bool = False) -> str:
     subprocess.run([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-shared", "-fPIC",
                     f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
                     *[a for d in include for a in ("-isystem", d)], "-I", os.path.join(ROOT, "include"), sources[0], "-o",
-                    BINDING_PATH, LIB_PATH, "-Wl,-rpath,$ORIGIN", "-L" + libs, "-Wl,-rpath," + libs, "-ltorch_python",
+                    BINDING_PATH, "-L" + HERE, "-l:libsdvg.so", "-Wl,-rpath,$ORIGIN", "-L" + libs, "-Wl,-rpath," + libs, "-ltorch_python",
                     "-ltorch_cpu", "-lc10"], check=True)
     return BINDING_PATH
 
