@@ -577,7 +577,7 @@ int sdvg_block_steps_e4m3_tiled(int steps, sdvg_cache* cache, const void* const*
  * into the result.  out, residual, bias and gate need the alignment of their element type only.
  * rows == 0 or cols == 0 is a call with nothing to do.  inner >= 1.
  * Up to 64 rows the sum of a column is shared by up to eight CTAs of a cluster (added in a fixed order); beyond that pairs of
- * CTAs walk tiles of 256 columns by up to 256 rows.  fp32 outputs are summed over `inner` in chunks of 512 or 640,
+ * CTAs walk tiles of 256 columns by up to 256 rows.  fp32 outputs are summed over `inner` in chunks of 256 or 640,
  * 16-bit ones in one go (the truncating accumulation of the tensor core drifts by about 7e-10 of the sum per element of inner).
  * workspace: as for sdvg_block_attn_fwd (the same buffer may serve both): its status word reports a bounded wait that
  * gave up (sdvg_block_attn_status), the call keeps nothing else in it.

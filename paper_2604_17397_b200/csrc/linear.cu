@@ -231,9 +231,10 @@ struct RingPos {
 // cut into chunks: each chunk gets a fresh accumulator, and the epilogue warps add the chunks with round-to-nearest.
 // Relative errors at 300 x 6144 x 512: 1.0e-6 with chunks of 1024, 7.3e-7 with 768, 6.1e-7 with 640, 4.8e-7 with 512.  For many
 // tokens short chunks cost time, since tensor memory is read slowly under products (4680 x 6144 x 1536 with gate and
-// residual: 93, 96 and 100 us with 768, 640 and 512; a whole sum 89); for few they do not.
+// residual: 93, 96 and 100 us with 768, 640 and 512; a whole sum 89); for few they do not (3 x 5120 x 30720: 50 us and 4.8e-7
+// with 512, 50 and 2.4e-7 with 256, 51 and 1.7e-7 with 128).
 constexpr int kPairChunkIters = 640 / kTileK;
-constexpr int kTileChunkIters = 512 / kTileK;
+constexpr int kTileChunkIters = 256 / kTileK;
 
 // ---- few tokens: a cluster per tile, which splits `inner` ---------------------------------------
 //
@@ -700,13 +701,15 @@ constexpr bool columns_within_share(int tile_t) {
 static_assert(columns_within_share(16) && columns_within_share(32) && columns_within_share(48) && columns_within_share(64));
 static_assert(kMaxTileFew == 64, "the sizes checked above");
 
-// CTAs per tile: as many as it takes to give every SM work, while each keeps eight stages of the sum or more and all of
-// them run at once.  One row: inner 256 4.3 us whole, 5.7 in two parts; inner 1536 x 1536 features 7.4, 7.1, 6.8 and 7.5 us in
-// 1, 2, 4 and 8 parts; 5120 x 5120 25.9, 18.1, 15.0 and 16.5.
+// CTAs per tile: as many as it takes to give every SM work, while all of them run at once and each keeps four stages of the sum,
+// or eight where the SMs have more than one CTA then (a second CTA per SM brings less).  Measured in graphs, times in us for
+// 1, 2, 4 and 8 parts: one row, 1536 x 1536 5.9, 5.6, 5.2, 6.1; 3 rows, 5120 x 5120 24.3, 16.2, 13.7, 15.3 and 1536 x 9216 9.7, 9.2,
+// 10.2, 17.2; 5 rows, 700 x 12000 5.8, 7.1, 8.2, 18.6; 64 rows, 6144 x 1536 27.2, 18.2, 12.7, 11.9.
 int tile_split(long long tiles, int k_iters, int tile_t, int sms) {
   const int per_sm = 228 * 1024 / (kTileStages * (kTileF + tile_t) * 128 + 3 * 1024);
   int split = 1;
-  while (split < kMaxSplit && tiles * split < sms && tiles * 2 * split <= (long long)sms * per_sm && k_iters >= 8 * split)
+  while (split < kMaxSplit && tiles * split < sms && tiles * 2 * split <= (long long)sms * per_sm &&
+         k_iters >= (tiles * 2 * split <= sms ? 8 : 16) * split)
     split *= 2;
   return split;
 }
