@@ -72,13 +72,14 @@ template <> struct OutElem<SDVG_F32> {
 };
 
 // The exponential forms keep their relative accuracy where the value vanishes: v / (1 + e^-z) tends to -0 for z -> -inf
-// (the exponential overflows to infinity).
+// (the exponential overflows to infinity; a denominator past 2^126 gives 0 already, for a value of 1e-36).
 //
 // GELU: v Phi(v) with the lower tail h = erfc(z) / 2, z = |v| / sqrt 2, taken directly, without the cancellation of 1 + erf:
 // erfc(z) e^(z^2) / t with t = 1 / (1 + 0.45 z) is smooth on 0 < t <= 1, and a polynomial of degree 9 in t, fitted by
 // least squares with weights driven towards an even relative error, is within 3.3e-8 of it (relative, in exact arithmetic;
 // 6.2e-7 in fp32 for |v| < 3, 4.1e-6 at |v| = 12, where the rounding of v^2 counts).  The library's erfcf, 16 at a time,
-// took so many registers that others spilled.
+// took so many registers that others spilled.  For v > 0 the tail is taken off with a bounded factor: past 15 it is 0 in fp32 and
+// the result is v itself, at infinity too, where v h would be infinity times 0.
 __device__ __forceinline__ float gelu_erf(float v) {
   const float z = fabsf(v);
   const float t = __fdividef(1.f, fmaf(0.31819805f, z, 1.f));
@@ -93,7 +94,7 @@ __device__ __forceinline__ float gelu_erf(float v) {
   q = fmaf(q, t, 0.12694158118874f);
   q = fmaf(q, t, 0.12694266037636f);
   const float h = q * t * __expf(-0.5f * v * v);
-  return v > 0.f ? fmaf(-v, h, v) : v * h;
+  return v > 0.f ? fmaf(-fminf(v, 1e4f), h, v) : v * h;
 }
 
 // The choice is made once for the 16 values, and the epilogue is instantiated once per kernel: unrolled over a tile with

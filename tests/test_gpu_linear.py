@@ -5,7 +5,7 @@ import numpy as np
 import pytest
 import torch
 
-from dense_utils import DTYPES, assert_close, f64, linear_tolerance
+from dense_utils import DTYPES, assert_close, f64, linear_tolerance, rounding
 from oracle import dense_oracle as O
 from paper_2604_17397_b200 import api
 
@@ -332,3 +332,23 @@ def test_binding_refuses_mismatched_tensors():
     with pytest.raises(api.SdvgError) as e:
         call({**s, "x": shifted}, out, ws)
     assert e.value.status == api.SDVG_ERR_MISALIGNED
+
+
+@pytest.mark.parametrize("act", list(ACTS))
+@pytest.mark.parametrize("rows", [1, 70])
+@pytest.mark.parametrize("out", ["fp32", "bf16"])
+def test_activations_of_infinities_nan_and_the_largest_values(act, rows, out):
+    """In both kernels, whether the infinity comes from the bias or from a sum past the range of fp32."""
+    v = torch.tensor([math.inf, -math.inf, math.nan, 3e38, -3e38, 1e20, -1e20, 40.0, -40.0, 0.0, 0.0], device="cuda")
+    x = torch.full((rows, 8), 2.0 ** 100, device="cuda", dtype=torch.bfloat16)
+    w = torch.zeros((len(v), 8), device="cuda", dtype=torch.bfloat16)
+    w[-2], w[-1] = 2.0 ** 100, -(2.0 ** 100)
+    got = torch.zeros((rows, len(v)), device="cuda", dtype=DTYPES[out])
+    api.sdvg_linear(x, w, got, api.attn_workspace(), bias=v, act=ACTS[act])
+    sums = f64(v)
+    sums[-2:] = math.inf, -math.inf
+    with np.errstate(invalid="ignore"):
+        ref = np.broadcast_to(O.activation(sums, act), (rows, len(v)))
+    with np.errstate(invalid="ignore"):
+        tol = 2.0 ** -14 * np.abs(ref) + 1e-36 + rounding(ref, DTYPES[out])
+    assert_close(got, ref, tol)
