@@ -111,7 +111,7 @@ class ModelState:
                                  self.tab_frames, block, self.scale, self.workspace)
 
     def check_status(self, where: str) -> None:
-        """Raise if an attention kernel of this model gave up on a bounded wait since the workspace was last reset
+        """Raise if a kernel of this model gave up on a bounded wait since the workspace was last reset
         (the status word is sticky, so one check covers every launch since then); synchronises the stream."""
         st = api.sdvg_block_attn_status(self.workspace)
         if st != api.SDVG_OK:
@@ -243,9 +243,13 @@ class TransformerLayer:
             api.sdvg_gated_norm(self.x1, None, y=self.y, gate=gate2, gate_rows=rows, post_norm=api.SDVG_NORM_RMS,
                                 post_weight=w.post_ff, x_out=x_out, eps=w.eps)
 
-    def commit(self, x, mod, block: int) -> int:
-        """The block's final K/V from its final stream into the ring (SDVG_FINAL); returns the evicted block."""
+    def commit(self, x, mod, block: int, check: bool = False) -> int:
+        """The block's final K/V from its final stream into the ring (SDVG_FINAL); returns the evicted block.  K and V come from
+        a product with bounded waits; ``check`` reads the status word (and so synchronises) before the ring is written, and
+        raises if a kernel of this model gave up."""
         _, k, v = self._qkv(x, mod, with_q=False)
+        if check:
+            self.m.check_status(f"final K/V of block {block}")
         return self._write_kv(None, k, v, block, api.SDVG_FINAL)
 
 
@@ -300,7 +304,7 @@ def _denoise(model: str, m: ModelState, block: int, steps: int, provider, on_att
 def _commit_clean(m: ModelState, block: int, layer, given) -> int:
     if layer is not None:
         x, mod, _ = given
-        return layer.commit(x, mod, block)
+        return layer.commit(x, mod, block, check=True)
     _, k, v = given
     return m.commit_final(k, v, block)
 
@@ -326,8 +330,8 @@ def run_schedule(num_blocks: int, steps: int, scores: torch.Tensor, tau: float,
               (x, mod, x_out), the residual stream, the step's modulation and where the step's stream goes, in
               place of (q, k, v); for "clean" and "accepted" x_out is not used
     A model whose ``cache`` is an 8-bit ring takes every step through the _e4m3 entry points.
-    The accept decision is read back to the host once per block, which is the only
-    synchronisation point of the flow.
+    The flow synchronises where it reads something back: the accept decision of a block, the status word after each
+    model's steps, and with a layer once more between a commit's projection of K and V and its ring write.
     """
     if scores.dtype != torch.float32 or scores.dim() != 2 or scores.shape[0] != num_blocks:
         raise ValueError("scores must be float32 [num_blocks, frames]")
@@ -342,7 +346,7 @@ def run_schedule(num_blocks: int, steps: int, scores: torch.Tensor, tau: float,
         res.drafter_attn_calls += _denoise("drafter", drafter, b, steps, provider, on_attention, drafter_layer)
         api.sdvg_route(flat[i * frames:(i + 1) * frames], None, 1, frames, b, tau, accept_d[i:i + 1],
                        qmin_d[i:i + 1], None)
-        accepted = bool(accept_d[i].item())               # the flow's one synchronisation point per block
+        accepted = bool(accept_d[i].item())               # synchronises
         # a kernel that gave up leaves undefined outputs: stop before anything derived from them enters a ring
         drafter.check_status(f"drafter steps of block {b}")
         res.drafter_evicted.append(_commit_clean(drafter, b, drafter_layer, provider("drafter", b, "clean", 0)))
