@@ -51,8 +51,10 @@ struct Moments {
 constexpr int kSlots = 2;                              // rows on their way per team
 constexpr int kTeamThreads = 640;                      // most threads of a CTA team; leaves a thread 96 registers
 
+// Ordinary loads, here and wherever these kernels read: the read-only path is for data that no one writes during the kernel's
+// whole life, which begins under the end of the kernel before it, and that may be the one which writes these vectors.
 __device__ __forceinline__ void load_vector(const float* p, float (&v)[8]) {
-  const float4 a = __ldg(reinterpret_cast<const float4*>(p)), b = __ldg(reinterpret_cast<const float4*>(p) + 1);
+  const float4 a = *reinterpret_cast<const float4*>(p), b = *(reinterpret_cast<const float4*>(p) + 1);
   v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
 }
 
@@ -363,7 +365,7 @@ __global__ void __launch_bounds__(NI == 16 ? 512 : 256) gated_norm_single_kernel
   auto with_vector = [&](const float* vec, auto f) {
     if (!vec) return;
 #pragma unroll
-    for (int i = 0; i < NI; ++i) f(i, valid(i) ? __ldg(vec + c0 + 32 * i) : 0.f);
+    for (int i = 0; i < NI; ++i) f(i, valid(i) ? vec[c0 + 32 * i] : 0.f);
   };
   float mean = 0.f, rstd = 1.f;
   if (p.y) {

@@ -58,8 +58,8 @@ __device__ __forceinline__ void load_weights(Vec8 (&w)[NI], const float* weight,
     float4 a = make_float4(1.f, 1.f, 1.f, 1.f), b = a;
     if (weight && c < width) {
       const float4* at = reinterpret_cast<const float4*>(weight + (per_head ? c % dim : c));
-      a = __ldg(at);
-      b = __ldg(at + 1);
+      a = at[0];
+      b = at[1];
     }
     w[i].p[0] = pair_of(a.x, a.y);
     w[i].p[1] = pair_of(a.z, a.w);
@@ -155,7 +155,7 @@ __global__ void __launch_bounds__(WARP ? 128 : NI == 2 ? kTeamThreads : 512) qk_
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const int pos = axis[e] == 0 ? p.frame_offset + f : axis[e] == 1 ? y : x;
-      cs[e] = __ldg(p.tab + pair_at[e] + pos * pair_step[e]);
+      cs[e] = p.tab[pair_at[e] + pos * pair_step[e]];
     }
     if (++x == p.grid_w) {
       x = 0;

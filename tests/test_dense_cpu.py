@@ -159,3 +159,16 @@ def test_qk_norm_without_scaling_is_the_rotary_embedding(scope):
     got = O.qk_norm_rope_ref(x, None, scope, 0.0, grid, 4, tab, 6)
     ref = SO.rope_ref(synth.f32_to_bf16_bits(x.astype(np.float32)), grid, 4)
     assert np.allclose(got, ref, atol=1e-6)
+
+
+def test_overlapped_kernels_do_not_read_through_the_read_only_path():
+    """A kernel that starts under the end of the one before it may read what that one writes; non-coherent loads are allowed only
+    for data that nothing writes while the kernel lives."""
+    import os
+    import re
+    csrc = os.path.join(os.path.dirname(build.__file__), "csrc")
+    text = {f: re.sub(r"//[^\n]*", "", open(os.path.join(csrc, f)).read()) for f in os.listdir(csrc)}
+    overlapped = [f for f, t in text.items() if f.endswith(".cu") and "overlap_wait()" in t]
+    assert sorted(overlapped) == ["gated_norm.cu", "linear.cu", "qk_norm.cu"]
+    for f in overlapped + ["row_team.cuh", "elem_types.cuh"]:
+        assert not re.search(r"__ldg\w*\(|ld\.global\S*\.nc|__restrict__", text[f]), f

@@ -208,3 +208,67 @@ def test_time_modulation_against_fp64():
     ref = D.linear_ref(e, f64(tm.w_mod), f64(tm.b_mod)) + f64(tm.offsets)
     # two intermediate results rounded to bf16
     assert np.linalg.norm(f64(got) - ref) <= 2 * 2.0 ** -8 * np.linalg.norm(ref)
+
+
+@pytest.mark.parametrize("cols", [64, 1536, 1537, 10248])
+@pytest.mark.parametrize("groups", [3, 100])
+def test_norms_see_the_modulation_that_the_call_before_them_wrote(cols, groups):
+    """One modulation buffer rewritten in place by a linear layer, each time just before the norm that reads it as gate, scale and
+    shift; launches overlap, results are those of calls with a wait between them."""
+    gen = torch.Generator(device="cuda").manual_seed(41)
+    rows, ws = 300, api.attn_workspace()
+    feats = [randn(gen, groups, 64).bfloat16() for _ in range(4)]
+    w = randn(gen, 3 * cols, 64, std=1 / 8).bfloat16()
+    x, y = (randn(gen, rows, cols).bfloat16() for _ in range(2))
+    mod = torch.zeros((groups, 3 * cols), device="cuda")
+    gate, scale, shift = (mod[:, i * cols:(i + 1) * cols] for i in range(3))
+
+    def chain(sync):
+        outs = torch.full((24, rows, cols), float("nan"), device="cuda", dtype=torch.bfloat16)
+        torch.cuda.synchronize()
+        for i, out in enumerate(outs):
+            api.sdvg_linear(feats[i % 4], w, mod, ws)
+            if sync:
+                torch.cuda.synchronize()
+            api.sdvg_gated_norm(x, out, y=y, gate=gate, gate_rows=rows // groups, scale=scale, shift=shift, modulate_rows=rows // groups)
+            if sync:
+                torch.cuda.synchronize()
+        torch.cuda.synchronize()
+        return outs
+
+    want = chain(True)
+    assert not torch.equal(want[0], want[1]) and torch.equal(want[0], want[4])
+    assert all(torch.equal(chain(False), want) for _ in range(5))
+
+
+@pytest.mark.parametrize("heads,dim", [(2, 64), (24, 128)])
+def test_the_prologue_sees_the_norm_weights_that_the_call_before_it_wrote(heads, dim):
+    gen = torch.Generator(device="cuda").manual_seed(42)
+    grid, c, ws = (2, 10, 15), heads * dim, api.attn_workspace()
+    tokens = 300
+    q, k, v = (randn(gen, tokens, heads, dim).bfloat16() for _ in range(3))
+    feats = [randn(gen, 1, 64).bfloat16() for _ in range(4)]
+    w = randn(gen, c, 64, std=1 / 8).bfloat16()
+    weight = torch.zeros((1, c), device="cuda")
+    tab = api.sdvg_rope3d_table(dim, 2, 10, 15).cuda()
+    cache = api.Cache(2, heads, tokens, dim)
+
+    def chain(sync):
+        outs = torch.zeros((24, tokens, heads, dim), device="cuda", dtype=torch.bfloat16)
+        torch.cuda.synchronize()
+        for i, out in enumerate(outs):
+            api.sdvg_linear(feats[i % 4], w, weight, ws)
+            if sync:
+                torch.cuda.synchronize()
+            api.sdvg_qk_norm_rope3d_commit(cache, q, k, v, weight[0], weight[0], api.SDVG_SCOPE_ROW, 1e-6, out, None, grid, 0, tab, 2, 0,
+                                           api.SDVG_STAGE)
+            if sync:
+                torch.cuda.synchronize()
+        torch.cuda.synchronize()
+        return outs, cache.read_block(0)[0]
+
+    want, ring = chain(True)
+    assert not torch.equal(want[0], want[1]) and torch.equal(want[0], want[4])
+    for _ in range(5):
+        got, got_ring = chain(False)
+        assert torch.equal(got, want) and torch.equal(got_ring, ring)
