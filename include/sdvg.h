@@ -609,6 +609,8 @@ int sdvg_linear(const void* x, int64_t ld_x, const void* w, int64_t ld_w, const 
  * read).  Each pointer needs the alignment of its element type; rows whose addresses are all multiples of 16 bytes with
  * cols a multiple of 8 are moved in whole vectors, others element by element.
  * Means and variances are fp32, the variance from the centred values.  eps >= 0 and finite.
+ * Rows moved in whole vectors take the vectors of a group combined, norm(s) * (weight * (1 + scale)) + (bias * (1 + scale) + shift):
+ * where scale is infinite and a bias is given, the two infinite products may cancel to NaN.
  * rows == 0 is a call with nothing to do.  cols >= 1.
  * Errors: INVALID_ARG, BAD_SHAPE, MISALIGNED, UNSUPPORTED_ARCH, CUDA.
  */

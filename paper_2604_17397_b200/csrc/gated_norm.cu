@@ -222,7 +222,7 @@ __global__ void __launch_bounds__(WARP ? 128 : kTeamThreads) gated_norm_kernel(c
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
               a[j] = fmaf(a[j], f[j], a[j]);
-              b[j] = fmaf(b[j], f[j], b[j]);
+              if (p.bias) b[j] = fmaf(b[j], f[j], b[j]);     // without one: not 0 times a scale that may be infinite
             }
           }
           if (p.shift) {

@@ -226,3 +226,23 @@ def test_binding_refuses_mismatched_tensors():
             call({**s, **change}, None, out)
     with pytest.raises(api.SdvgError):
         api.sdvg_gated_norm(s["x"], None)
+
+
+@pytest.mark.parametrize("cols", [64, 1536, 1537, 20001])
+@pytest.mark.parametrize("norm", ["rms", "layer"])
+@pytest.mark.parametrize("affine", [False, True])
+def test_infinite_scales_travel_as_in_the_formula(cols, norm, affine):
+    """In every kernel (a warp per row, a CTA, single columns, long rows); without a bias, whose product with an infinite
+    scale may cancel the other term's."""
+    s = problem(6, cols, "bf16", "bf16", "fp32", norm=norm, affine=affine, mod_rows=3, gate_rows=2, seed=cols)
+    s["bias"] = None
+    s["scale"][0, 3], s["scale"][1, 5], s["scale"][1, 7], s["shift"][0, 9] = float("inf"), float("-inf"), float("nan"), float("inf")
+    out = torch.empty((6, cols), device="cuda")
+    for shift in (s["shift"], None):
+        s["shift"] = shift
+        (_, ref), _ = expected(s)
+        call(s, None, out)
+        got = f64(out)
+        assert np.isinf(ref[:3, 3]).all() and np.isinf(ref[3:, 5]).all()
+        assert np.array_equal(np.isnan(got), np.isnan(ref))
+        assert np.array_equal(got[np.isinf(ref)], ref[np.isinf(ref)]) and np.array_equal(np.isinf(got), np.isinf(ref))
