@@ -136,10 +136,13 @@ PyObject* linear(PyObject*, PyObject* const* args, Py_ssize_t n) {
   const float* bias = vector(r, 4, cols, "bias");
   void* stream = r.address(9);
   if (!r.ok) return nullptr;
+  // whatever may throw is read before the interpreter lock is released
+  void* const space = ws->data_ptr();
+  const size_t space_bytes = ws->nbytes();
   int st;
   Py_BEGIN_ALLOW_THREADS
   st = sdvg_linear(mx.p, mx.ld, mw.p, mw.ld, bias, act, static_cast<const float*>(gate.p), gate.ld, gate_rows, res.p, res.ld,
-                   mo.p, mo.ld, (int)rows, (int)cols, (int)inner, mx.type, mo.type, ws->data_ptr(), ws->nbytes(), stream);
+                   mo.p, mo.ld, (int)rows, (int)cols, (int)inner, mx.type, mo.type, space, space_bytes, stream);
   Py_END_ALLOW_THREADS
   return PyLong_FromLong(st);
 }
@@ -220,11 +223,12 @@ PyObject* qk_norm(PyObject*, PyObject* const* args, Py_ssize_t n) {
   const int64_t index = r.integer(19);
   void* stream = r.address(21);
   if (!r.ok) return nullptr;
+  const float* const tab = static_cast<const float*>(table->data_ptr());      // may throw: before the lock is released
   int64_t evicted = -1;
   int st;
   Py_BEGIN_ALLOW_THREADS
   st = sdvg_qk_norm_rope3d_commit(cache, q.p, q.ld, k.p, k.ld, v.p, v.ld, qw, kw, scope, eps, q_out.p, k_out.p, frames, grid_h,
-                                  grid_w, offset, static_cast<const float*>(table->data_ptr()), tab_frames, index, flags,
+                                  grid_w, offset, tab, tab_frames, index, flags,
                                   &evicted, stream);
   Py_END_ALLOW_THREADS
   return PyLong_FromLongLong(st == SDVG_OK ? evicted : -1000 - st);

@@ -172,3 +172,63 @@ def test_overlapped_kernels_do_not_read_through_the_read_only_path():
     assert sorted(overlapped) == ["gated_norm.cu", "linear.cu", "qk_norm.cu"]
     for f in overlapped + ["row_team.cuh", "elem_types.cuh"]:
         assert not re.search(r"__ldg\w*\(|ld\.global\S*\.nc|__restrict__", text[f]), f
+
+
+class OnPaper(torch.Tensor):
+    """A tensor that says it is on a GPU and has no memory: the binding takes it, and the library refuses its null address."""
+
+    @staticmethod
+    def __new__(cls, *shape, dtype=torch.bfloat16):
+        return torch.Tensor._make_wrapper_subclass(cls, shape, dtype=dtype, device="cuda")
+
+    @classmethod
+    def __torch_dispatch__(cls, func, types, args=(), kwargs=None):
+        raise NotImplementedError
+
+
+def without_address(*shape, dtype):
+    """One whose address cannot be asked for, as that of a tensor that is being traced."""
+    t = OnPaper(*shape, dtype=dtype)
+    torch._C._set_throw_on_mutable_data_ptr(t)
+    return t
+
+
+def linear_on_paper(**change):
+    a = dict(x=OnPaper(4, 64), w=OnPaper(8, 64), out=OnPaper(4, 8), ws=OnPaper(256, dtype=torch.uint8), bias=None, act=0, residual=None,
+             gate=None, gate_rows=0, stream=0)
+    return api._binding().linear(*{**a, **change}.values())
+
+
+def qk_on_paper(cache, **change):
+    block = lambda: OnPaper(64, 2, 64)
+    a = dict(handle=cache.value, tokens=64, heads=2, dim=64, q=None, k=block(), v=block(), q_weight=None, k_weight=None, scope=0, eps=1e-6,
+             q_out=None, k_out=None, frames=1, grid_h=8, grid_w=8, offset=0,
+             table=OnPaper(api.lib().sdvg_rope3d_table_floats(64, 4, 8, 8), dtype=torch.float32), tab_frames=4, block=0,
+             flags=api.SDVG_STAGE, stream=0)
+    return api._binding().qk_norm(*{**a, **change}.values())
+
+
+@pytest.fixture
+def ring(lib):
+    import ctypes as C
+    h = C.c_void_p()
+    assert lib.sdvg_cache_create(C.byref(h), 0x10000, 0x20000, 3, 2, 64, 64) == api.SDVG_OK
+    yield h
+    lib.sdvg_cache_destroy(h)
+
+
+def test_a_tensor_without_an_address_raises(ring):
+    """In every place: also the ones read last, just before the interpreter lock is given up."""
+    assert linear_on_paper() == api.SDVG_ERR_INVALID_ARG and qk_on_paper(ring) == -1000 - api.SDVG_ERR_INVALID_ARG
+    for change in (dict(ws=without_address(256, dtype=torch.uint8)), dict(x=without_address(4, 64, dtype=torch.bfloat16)),
+                   dict(bias=without_address(8, dtype=torch.float32))):
+        with pytest.raises(RuntimeError):
+            linear_on_paper(**change)
+    n = api.lib().sdvg_rope3d_table_floats(64, 4, 8, 8)
+    for change in (dict(table=without_address(n, dtype=torch.float32)), dict(v=without_address(64, 2, 64, dtype=torch.bfloat16))):
+        with pytest.raises(RuntimeError):
+            qk_on_paper(ring, **change)
+    x = OnPaper(4, 64)
+    with pytest.raises(RuntimeError):
+        api._binding().gated_norm(x, without_address(4, 64, dtype=torch.bfloat16), None, None, 0, 0, None, None, 2, None, None, None, None, 0,
+                                  1e-6, 0)
