@@ -220,6 +220,9 @@ PyObject* qk_norm(PyObject*, PyObject* const* args, Py_ssize_t n) {
   const Tensor* table = r.tensor(17, "table", false);
   if (table && (table->scalar_type() != ScalarType::Float || !table->is_contiguous()))
     r.fail("table", "expected a contiguous float32 tensor");
+  // 0 for sizes that the call refuses below
+  if (table && r.ok && (uint64_t)table->numel() < sdvg_rope3d_table_floats((int)dim, tab_frames, grid_h, grid_w))
+    r.fail("table", "shorter than that of the block's grid and tab_frames");
   const int64_t index = r.integer(19);
   void* stream = r.address(21);
   if (!r.ok) return nullptr;
@@ -228,8 +231,7 @@ PyObject* qk_norm(PyObject*, PyObject* const* args, Py_ssize_t n) {
   int st;
   Py_BEGIN_ALLOW_THREADS
   st = sdvg_qk_norm_rope3d_commit(cache, q.p, q.ld, k.p, k.ld, v.p, v.ld, qw, kw, scope, eps, q_out.p, k_out.p, frames, grid_h,
-                                  grid_w, offset, tab, tab_frames, index, flags,
-                                  &evicted, stream);
+                                  grid_w, offset, tab, tab_frames, index, flags, &evicted, stream);
   Py_END_ALLOW_THREADS
   return PyLong_FromLongLong(st == SDVG_OK ? evicted : -1000 - st);
 }

@@ -232,3 +232,15 @@ def test_a_tensor_without_an_address_raises(ring):
     with pytest.raises(RuntimeError):
         api._binding().gated_norm(x, without_address(4, 64, dtype=torch.bfloat16), None, None, 0, 0, None, None, 2, None, None, None, None, 0,
                                   1e-6, 0)
+
+
+def test_the_binding_refuses_a_rotary_table_that_is_too_short(ring):
+    n = api.lib().sdvg_rope3d_table_floats(64, 4, 8, 8)
+    table = lambda floats: OnPaper(floats, dtype=torch.float32)
+    reached = -1000 - api.SDVG_ERR_INVALID_ARG                  # the library, which refuses the null addresses
+    assert qk_on_paper(ring, table=table(n)) == qk_on_paper(ring, table=table(n + 5)) == reached
+    for change in (dict(table=table(n - 1)), dict(tab_frames=5), dict(grid_h=9), dict(grid_w=1 << 20), dict(tab_frames=1 << 30),
+                   dict(table=OnPaper(n, dtype=torch.bfloat16))):
+        with pytest.raises(ValueError, match="table"):
+            qk_on_paper(ring, **change)
+    assert qk_on_paper(ring, tab_frames=0) == qk_on_paper(ring, grid_h=0) == reached
