@@ -8,6 +8,7 @@ raised.
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 from typing import Optional
 
@@ -168,14 +169,30 @@ def sdvg_rope3d_table(head_dim: int, tab_frames: int, grid_h: int, grid_w: int) 
     return out
 
 
+@functools.lru_cache(maxsize=256)
+def _table_floats(head_dim: int, tab_frames: int, grid_h: int, grid_w: int) -> int:
+    return lib().sdvg_rope3d_table_floats(head_dim, tab_frames, grid_h, grid_w)
+
+
+def _rope_table(table: Optional[torch.Tensor], head_dim: int, tab_frames: int, grid):
+    """Address of a rotary table that holds what the kernels read of it."""
+    if table is not None:
+        if table.dtype != torch.float32:
+            raise ValueError("table: expected float32")
+        if table.numel() < _table_floats(head_dim, tab_frames, grid[1], grid[2]):     # 0 for sizes the library refuses
+            raise ValueError("table: shorter than that of the block's grid and tab_frames")
+    return _ptr(table)
+
+
 def sdvg_rope3d_qk(q, k, q_out, k_out, grid, frame_offset: int, table: torch.Tensor, tab_frames: int,
                    stream=None) -> None:
     ref = q if q is not None else k
     tokens, heads, head_dim = ref.shape
     frames, grid_h, grid_w = grid
+    tab = _rope_table(table, head_dim, tab_frames, grid)
     st = lib().sdvg_rope3d_qk(_bf16(q), _bf16(k), _bf16(q_out, None if q is None else q.shape),
                               _bf16(k_out, None if k is None else k.shape), tokens, heads, head_dim,
-                              frames, grid_h, grid_w, frame_offset, _ptr(table), tab_frames, _stream(stream))
+                              frames, grid_h, grid_w, frame_offset, tab, tab_frames, _stream(stream))
     _check(st, "sdvg_rope3d_qk")
 
 
@@ -257,10 +274,11 @@ def sdvg_rope3d_qk_commit(cache: Cache, q, k, v, q_out, k_out, grid, frame_offse
     shape = (cache.block_tokens, cache.heads, cache.head_dim)
     frames, grid_h, grid_w = grid
     ev = _I64(-1)
+    tab = _rope_table(table, cache.head_dim, tab_frames, grid)
     st = lib().sdvg_rope3d_qk_commit(cache.handle, _bf16(q, None if q is None else shape), _bf16(k, shape),
                                      _bf16(v, shape), _bf16(q_out, None if q_out is None else shape),
                                      _bf16(k_out, None if k_out is None else shape),
-                                     frames, grid_h, grid_w, frame_offset, _ptr(table), tab_frames,
+                                     frames, grid_h, grid_w, frame_offset, tab, tab_frames,
                                      block_index, flags, C.byref(ev), _stream(stream))
     _check(st, "sdvg_rope3d_qk_commit")
     return ev.value
@@ -461,11 +479,12 @@ def sdvg_rope3d_qk_commit_e4m3(cache: Cache, q, k, v, q8_out, q_inv_scale, k_inv
     shape = (cache.block_tokens, cache.heads, cache.head_dim)
     frames, grid_h, grid_w = grid
     ev = _I64(-1)
+    tab = _rope_table(table, cache.head_dim, tab_frames, grid)
     st = lib().sdvg_rope3d_qk_commit_e4m3(cache.handle, _bf16(q, None if q is None else shape), _bf16(k, shape),
                                           _bf16(v, shape), _u8(q8_out, None if q8_out is None else shape),
                                           None if q_inv_scale is None else _scales(q_inv_scale, cache.heads),
                                           _scales(k_inv_scale, cache.heads), _scales(v_inv_scale, cache.heads),
-                                          frames, grid_h, grid_w, frame_offset, _ptr(table), tab_frames, block_index,
+                                          frames, grid_h, grid_w, frame_offset, tab, tab_frames, block_index,
                                           flags, C.byref(ev), _stream(stream))
     _check(st, "sdvg_rope3d_qk_commit_e4m3")
     return ev.value
@@ -513,10 +532,11 @@ def sdvg_rope3d_qk_commit_e4m3_tiled(cache: Cache, q, k, v, q8_out, q_tile_scale
     shape = (cache.block_tokens, cache.heads, cache.head_dim)
     frames, grid_h, grid_w = grid
     ev = _I64(-1)
+    tab = _rope_table(table, cache.head_dim, tab_frames, grid)
     st = lib().sdvg_rope3d_qk_commit_e4m3_tiled(cache.handle, _bf16(q, None if q is None else shape), _bf16(k, shape),
                                                 _bf16(v, shape), _u8(q8_out, None if q8_out is None else shape),
                                                 _tile_scales(q_tile_scale, cache.heads, cache.block_tokens), frames,
-                                                grid_h, grid_w, frame_offset, _ptr(table), tab_frames, block_index,
+                                                grid_h, grid_w, frame_offset, tab, tab_frames, block_index,
                                                 flags, C.byref(ev), _stream(stream))
     _check(st, "sdvg_rope3d_qk_commit_e4m3_tiled")
     return ev.value
@@ -548,8 +568,9 @@ def sdvg_block_steps(cache: Cache, qs, ks, vs, q_ropeds, outs, grid, frame_offse
     shape = (cache.block_tokens, cache.heads, cache.head_dim)
     bf = lambda t: _bf16(t, shape)
     arrays = [_ptr_array(x, bf) for x in (qs, ks, vs, q_ropeds, outs)]
+    tab = _rope_table(table, cache.head_dim, tab_frames, grid)
     st = lib().sdvg_block_steps(n, cache.handle, *[C.cast(a, _VP) for a in arrays], grid[0], grid[1], grid[2],
-                                frame_offset, _ptr(table), tab_frames, block_index, scale, workspace.data_ptr(),
+                                frame_offset, tab, tab_frames, block_index, scale, workspace.data_ptr(),
                                 workspace.numel(), _stream(stream))
     _check(st, "sdvg_block_steps")
 
@@ -566,8 +587,9 @@ def sdvg_block_steps_e4m3(cache: Cache, qs, ks, vs, q8_ropeds, outs, q_inv_scale
     u8 = lambda t: _u8(t, shape)
     arrays = [_ptr_array(qs, bf), _ptr_array(ks, bf), _ptr_array(vs, bf), _ptr_array(q8_ropeds, u8), _ptr_array(outs, bf)]
     sc = [_scales(t, cache.heads) for t in (q_inv_scale, k_inv_scale, v_inv_scale, qk_descale, v_descale)]
+    tab = _rope_table(table, cache.head_dim, tab_frames, grid)
     st = lib().sdvg_block_steps_e4m3(n, cache.handle, *[C.cast(a, _VP) for a in arrays], *sc, grid[0], grid[1], grid[2],
-                                     frame_offset, _ptr(table), tab_frames, block_index, scale, workspace.data_ptr(),
+                                     frame_offset, tab, tab_frames, block_index, scale, workspace.data_ptr(),
                                      workspace.numel(), _stream(stream))
     _check(st, "sdvg_block_steps_e4m3")
 
@@ -585,8 +607,9 @@ def sdvg_block_steps_e4m3_tiled(cache: Cache, qs, ks, vs, q8_ropeds, q_tile_scal
     ts = lambda t: _tile_scales(t, cache.heads, cache.block_tokens)
     arrays = [_ptr_array(qs, bf), _ptr_array(ks, bf), _ptr_array(vs, bf), _ptr_array(q8_ropeds, u8),
               _ptr_array(q_tile_scales, ts), _ptr_array(outs, bf)]
+    tab = _rope_table(table, cache.head_dim, tab_frames, grid)
     st = lib().sdvg_block_steps_e4m3_tiled(n, cache.handle, *[C.cast(a, _VP) for a in arrays], grid[0], grid[1], grid[2],
-                                           frame_offset, _ptr(table), tab_frames, block_index, scale,
+                                           frame_offset, tab, tab_frames, block_index, scale,
                                            workspace.data_ptr(), workspace.numel(), _stream(stream))
     _check(st, "sdvg_block_steps_e4m3_tiled")
 
