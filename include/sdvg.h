@@ -612,7 +612,7 @@ int sdvg_linear(const void* x, int64_t ld_x, const void* w, int64_t ld_w, const 
  * Rows moved in whole vectors take the vectors of a group combined, norm(s) * (weight * (1 + scale)) + (bias * (1 + scale) + shift):
  * where scale is infinite and a bias is given, the two infinite products may cancel to NaN.
  * rows == 0 is a call with nothing to do.  cols >= 1.
- * Errors: INVALID_ARG, BAD_SHAPE, MISALIGNED, UNSUPPORTED_ARCH, CUDA.
+ * Errors: INVALID_ARG, BAD_SHAPE (also rows or cols above 2^31 - 1025), MISALIGNED, UNSUPPORTED_ARCH, CUDA.
  */
 int sdvg_gated_norm(const void* x, int64_t ld_x, int x_type, const void* y, int64_t ld_y, int y_type,
                     int post_norm, const float* post_weight, const float* gate, int64_t ld_gate, int gate_rows,

@@ -560,7 +560,8 @@ int sdvg_gated_norm(const void* x, int64_t ld_x, int x_type, const void* y, int6
                     const float* shift, int64_t ld_mod, int mod_rows, float eps, void* out, int64_t ld_out, int out_type,
                     int rows, int cols, void* stream) {
   SDVG_RANGE();
-  if (rows < 0 || cols < 1) return SDVG_ERR_BAD_SHAPE;
+  constexpr int kMaxExtent = 0x7fffffff - 1024;                  // a column one step of a CTA further on is still an int
+  if (rows < 0 || cols < 1 || rows > kMaxExtent || cols > kMaxExtent) return SDVG_ERR_BAD_SHAPE;
   if (post_norm < SDVG_NORM_NONE || post_norm > SDVG_NORM_LAYER || norm < SDVG_NORM_NONE || norm > SDVG_NORM_LAYER)
     return SDVG_ERR_INVALID_ARG;
   if (!sdvg::elem_type_ok(x_type) || (y && !sdvg::elem_type_ok(y_type)) || (out && !sdvg::elem_type_ok(out_type)))

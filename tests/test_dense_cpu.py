@@ -244,3 +244,17 @@ def test_the_binding_refuses_a_rotary_table_that_is_too_short(ring):
         with pytest.raises(ValueError, match="table"):
             qk_on_paper(ring, **change)
     assert qk_on_paper(ring, tab_frames=0) == qk_on_paper(ring, grid_h=0) == reached
+
+
+@pytest.mark.parametrize("change", [dict(cols=0x7fffffff), dict(cols=0x7fffffff - 1023), dict(rows=0x7fffffff), dict(rows=0x7fffffff - 1023),
+                                    dict(cols=0x7fffffff - 100, y=W, ld_y=1 << 31)])
+def test_gated_norm_refuses_extents_at_the_end_of_an_int(lib, change):
+    """A column counter that steps by the threads of a CTA, or rows rounded up to whole CTAs, would pass the end of its type."""
+    wide = dict(ld_x=1 << 31, ld_out=1 << 31) if "cols" in change else {}
+    assert lib.sdvg_gated_norm(*norm_args(**{**wide, **change})) == api.SDVG_ERR_BAD_SHAPE
+
+
+def test_gated_norm_takes_extents_just_below(lib):
+    for change in (dict(cols=0x7fffffff - 1024, ld_x=1 << 31, ld_out=1 << 31), dict(rows=0x7fffffff - 1024)):
+        # everything is checked before the pointers' alignment
+        assert lib.sdvg_gated_norm(*norm_args(**change, out=OUT + 1)) == api.SDVG_ERR_MISALIGNED
