@@ -86,7 +86,7 @@ int    sdvg_rope3d_table(float* host_out, int head_dim, int tab_frames, int grid
  * im' = fl(fl(re*s) + fl(im*c)) in IEEE fp32 without fused multiply-add,
  * then round-to-nearest-even to bf16.
  * cos_sin_tab: device copy of the table built for (head_dim, tab_frames, grid_h, grid_w).
- * Errors: BAD_SHAPE (head_dim not 64/128, tokens mismatch), BAD_STATE
+ * Errors: BAD_SHAPE (head_dim not 64/128, tokens mismatch, a table of 2^31 pairs or more), BAD_STATE
  * (frame_offset < 0 or frame_offset+frames > tab_frames), MISALIGNED, INVALID_ARG.
  */
 int sdvg_rope3d_qk(const void* q, const void* k, void* q_out, void* k_out,

@@ -17,9 +17,11 @@ int fill_rope(Params& p, int head_dim, int tokens, const RopeArgs& r) {
   if (!r.tab) return SDVG_ERR_INVALID_ARG;
   if (!sdvg::aligned16(r.tab)) return SDVG_ERR_MISALIGNED;
   if (r.tab_frames <= 0) return SDVG_ERR_BAD_SHAPE;
-  if (r.frame_offset < 0 || (long long)r.frame_offset + r.frames > r.tab_frames) return SDVG_ERR_BAD_STATE;
   int pf, ph, pw;
   sdvg_rope3d_pairs(head_dim, &pf, &ph, &pw);
+  // the kernels' offsets into the table are ints
+  if ((long long)r.tab_frames * pf + (long long)r.grid_h * ph + (long long)r.grid_w * pw > 0x7fffffff) return SDVG_ERR_BAD_SHAPE;
+  if (r.frame_offset < 0 || (long long)r.frame_offset + r.frames > r.tab_frames) return SDVG_ERR_BAD_STATE;
   p.grid_hw = r.grid_h * r.grid_w;
   p.grid_w = r.grid_w;
   p.frame_offset = r.frame_offset;

@@ -258,3 +258,21 @@ def test_gated_norm_takes_extents_just_below(lib):
     for change in (dict(cols=0x7fffffff - 1024, ld_x=1 << 31, ld_out=1 << 31), dict(rows=0x7fffffff - 1024)):
         # everything is checked before the pointers' alignment
         assert lib.sdvg_gated_norm(*norm_args(**change, out=OUT + 1)) == api.SDVG_ERR_MISALIGNED
+
+
+def test_rotary_tables_past_32_bits_are_refused(lib, ring):
+    """Offsets into the table are ints, in (cos, sin) pairs: 12 per frame position and 10 per row and column with head_dim 64."""
+    most = (2 ** 31 - 1 - 8 * 20) // 12
+
+    def commit(tab_frames, offset=0):
+        return lib.sdvg_qk_norm_rope3d_commit(ring, X, 128, W, 128, B, 128, None, None, 0, 1e-6, OUT, None, 1, 8, 8, offset, G, tab_frames, 1,
+                                              api.SDVG_STAGE, None, None)
+
+    def rope(tab_frames, offset=0):
+        return lib.sdvg_rope3d_qk(X, W, OUT, R, 64, 2, 64, 1, 8, 8, offset, G, tab_frames, None)
+
+    for call in (commit, rope):
+        for tab_frames in (most + 1, 1 << 30, 2 ** 31 - 1):
+            assert call(tab_frames) == call(tab_frames, tab_frames - 1) == api.SDVG_ERR_BAD_SHAPE
+        assert call(most, most) == api.SDVG_ERR_BAD_STATE       # past the table's frames: the next check
+    assert commit(most) == api.SDVG_ERR_BAD_STATE               # block 1 before block 0
