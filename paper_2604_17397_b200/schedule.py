@@ -175,6 +175,7 @@ class TransformerLayer:
 
     def _mod(self, mod: torch.Tensor):
         rows = -(-self.tokens // mod.shape[0])
+        mod = mod[:-(-self.tokens // rows)]                      # rows that a token reaches: all, where they divide evenly
         return [mod[:, i * self.width:(i + 1) * self.width] for i in range(6)], rows
 
     def _heads(self, t: torch.Tensor) -> torch.Tensor:

@@ -109,3 +109,17 @@ def test_a_commit_of_its_own_reads_no_status(monkeypatch):
     with pytest.raises(api.SdvgError):
         layer(m).commit(x, mod, 0, check=True)
     assert [c[0] for c in r.calls] == ["norm", "linear", "ring", "norm", "linear"]
+
+
+@pytest.mark.parametrize("groups", [1, 2, 3, 5, 7, 11, 12, 20])
+def test_modulation_rows_of_any_number(monkeypatch, groups):
+    """Token t uses row t // ceil(tokens / groups); the calls get as many rows as that reaches, which is what they ask for."""
+    r, m = Record(monkeypatch), model("drafter")
+    x, _, x_out = provider()
+    mod = torch.arange(groups, dtype=torch.float32)[:, None].expand(groups, 6 * WIDTH).contiguous()
+    layer(m).step(x, mod, 0, x_out)
+    rows = -(-TOKENS // groups)
+    for kw in [c[1] for c in r.calls if c[0] == "norm"]:
+        assert kw["modulate_rows"] == rows
+        assert kw["scale"].shape == kw["shift"].shape == (-(-TOKENS // rows), WIDTH)
+        assert kw["scale"][:, 0].tolist() == [float(i) for i in range(-(-TOKENS // rows))]
