@@ -12,8 +12,6 @@ CSRC = os.path.join(HERE, "csrc")
 LIB_PATH = os.path.join(HERE, "libsdvg.so")
 SOURCES = ["sdvg_host.cu", "rope_commit.cu", "route.cu", "state.cu", "quant.cu", "steps.cu", "attn_fwd.cu",
            "linear.cu", "gated_norm.cu", "qk_norm.cu"]
-
-
 BINDING_PATH = os.path.join(HERE, "_binding.so")
 
 
@@ -50,14 +48,23 @@ def build(force: bool = False, out: str = LIB_PATH, extra_flags=(), verbose: boo
     return out
 
 
-def build_binding(force: bool = False) -> str:
-    """The compiled argument marshalling of the dense operators: links the library and torch's Python types."""
-    sources = [os.path.join(CSRC, "binding.cpp"), os.path.join(ROOT, "include", "sdvg.h")]
-    if not force and os.path.exists(BINDING_PATH) and all(os.path.getmtime(s) <= os.path.getmtime(BINDING_PATH) for s in sources):
-        return BINDING_PATH
+def build_binding(force: bool = False):
+    """The compiled argument marshalling of the dense operators: links the library and torch's Python types, so that it is
+    built again for another torch or Python.  Returns its path, or None where there is no torch to build it for (the library
+    itself needs none)."""
+    try:
+        import torch
+    except ImportError:
+        return None
     import sysconfig
 
-    import torch
+    sources = [os.path.join(CSRC, "binding.cpp"), os.path.join(ROOT, "include", "sdvg.h")]
+    made_for, note = f"torch {torch.__version__} {sys.implementation.cache_tag}", BINDING_PATH + ".made_for"
+    if not force and os.path.exists(BINDING_PATH) and os.path.exists(note):
+        with open(note) as f:
+            same = f.read() == made_for
+        if same and all(os.path.getmtime(s) <= os.path.getmtime(BINDING_PATH) for s in sources):
+            return BINDING_PATH
     torch_dir = os.path.dirname(torch.__file__)
     include = [os.path.join(torch_dir, "include"), os.path.join(torch_dir, "include", "torch", "csrc", "api", "include"),
                sysconfig.get_paths()["include"]]
@@ -67,6 +74,8 @@ def build_binding(force: bool = False) -> str:
                     *[a for d in include for a in ("-isystem", d)], "-I", os.path.join(ROOT, "include"), sources[0], "-o",
                     BINDING_PATH, "-L" + HERE, "-l:libsdvg.so", "-Wl,-rpath,$ORIGIN", "-L" + libs, "-Wl,-rpath," + libs, "-ltorch_python",
                     "-ltorch_cpu", "-lc10"], check=True)
+    with open(note, "w") as f:
+        f.write(made_for)
     return BINDING_PATH
 
 
