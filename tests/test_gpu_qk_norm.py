@@ -178,3 +178,43 @@ def test_binding_refuses_mismatched_tensors():
     with pytest.raises(ValueError):
         call(cache, s, torch.empty((16, 2, 128), device="cuda", dtype=torch.bfloat16)[..., :64], None, 0)
     assert cache.state()[2] == -1                  # nothing was staged
+
+
+@pytest.mark.parametrize("heads,dim", [(80, 128), (81, 128), (96, 128), (128, 128), (160, 64), (161, 64), (255, 64), (256, 64)])
+@pytest.mark.parametrize("scope,fused,weights", [("row", True, True), ("head", False, True), ("head", True, False)])
+def test_parity_of_the_widest_tokens(heads, dim, scope, fused, weights):
+    """Around 10240 elements, where a thread goes from two pieces to four, with whole and partly filled last warps, up to 16384."""
+    grid = (2, 3, 5)
+    s = make(heads, dim, grid, 3, scope, fused, weights, seed=heads)
+    cache = api.Cache(3, heads, 30, dim)
+    guard = Canaries()
+    guard.watch_cache(cache)
+    q_out, k_out = (guard.new((30, heads, dim), torch.bfloat16) for _ in range(2))
+    assert call(cache, s, q_out, k_out, 0) == -1
+    (q_ref, q_tol), (k_ref, k_tol) = expected(s, 0)
+    assert_close(q_out, q_ref, q_tol, "q")
+    assert_close(k_out, k_ref, k_tol, "k")
+    ring_k, ring_v = cache.read_block(0)
+    assert np.array_equal(to_bits(ring_k), to_bits(k_out)) and np.array_equal(to_bits(ring_v), to_bits(s["v"]))
+    guard.check()
+
+
+def test_more_tokens_than_teams_at_the_widest():
+    """Every team walks several tokens, so that its ring wraps."""
+    s = make(128, 128, (3, 20, 20), 2, seed=8)
+    cache = api.Cache(2, 128, 1200, 128)
+    q_out = torch.full((1200, 128, 128), float("nan"), device="cuda", dtype=torch.bfloat16)
+    call(cache, s, q_out, None, 0)
+    (q_ref, q_tol), (k_ref, k_tol) = expected(s, 0)
+    assert_close(q_out, q_ref, q_tol, "q")
+    assert_close(cache.read_block(0)[0], k_ref, k_tol, "k")
+    assert torch.equal(cache.read_block(0)[1], s["v"])
+
+
+@pytest.mark.parametrize("heads,dim", [(129, 128), (257, 64)])
+def test_tokens_past_the_widest_are_refused(heads, dim):
+    s = make(heads, dim, (1, 2, 2), 2, "head")
+    cache = api.Cache(2, heads, 4, dim)
+    with pytest.raises(api.SdvgError) as e:
+        call(cache, s, torch.empty((4, heads, dim), device="cuda", dtype=torch.bfloat16), None, 0)
+    assert e.value.status == api.SDVG_ERR_BAD_SHAPE and cache.state()[2] == -1
