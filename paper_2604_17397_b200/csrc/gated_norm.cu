@@ -481,13 +481,12 @@ int device_sms(int* sms) {
 constexpr int kMostDynamic = 200 * 1024;
 constexpr int kFreeDynamic = 40 * 1024;                // needs no opt-in, with what the kernel has statically: 48 KB in all
 
-// -1: a team's ring does not fit
 template <int XW, int YW, int NI, bool WARP, bool FULL>
 int launch_team_as(const NormParams& p, int threads, int sms, cudaStream_t stream) {
   const int rows_per_cta = WARP ? threads / 32 : 1;
   const int want = (p.rows + rows_per_cta - 1) / rows_per_cta;
   const int dynamic = threads * kSlots * (Ring<XW, NI>::kBytes + Ring<YW, NI>::kBytes);
-  if (dynamic > kMostDynamic) return -1;
+  static_assert((WARP ? 128 : kTeamThreads) * kSlots * (Ring<XW, NI>::kBytes + Ring<YW, NI>::kBytes) <= kMostDynamic, "ring size");
   int grid = want;
   if (want > sms || dynamic > kFreeDynamic) {
     // a grid that the device holds at once: teams walk rows of equal number.  Asked again when the shape changes.
