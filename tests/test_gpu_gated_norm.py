@@ -246,3 +246,15 @@ def test_infinite_scales_travel_as_in_the_formula(cols, norm, affine):
         assert np.isinf(ref[:3, 3]).all() and np.isinf(ref[3:, 5]).all()
         assert np.array_equal(np.isnan(got), np.isnan(ref))
         assert np.array_equal(got[np.isinf(ref)], ref[np.isinf(ref)]) and np.array_equal(np.isinf(got), np.isinf(ref))
+
+
+@pytest.mark.parametrize("cols", [64, 1536, 1537, 20001])
+def test_infinite_scales_with_a_bias_of_zero(cols):
+    s = problem(6, cols, "bf16", "", "fp32", affine=True, mod_rows=3, seed=cols)
+    s["scale"][0, 3], s["scale"][1, 5], s["bias"][3], s["bias"][5] = float("inf"), float("-inf"), 0.0, -0.0
+    out = torch.empty((6, cols), device="cuda")
+    (_, ref), _ = expected(s)
+    call(s, None, out)
+    got = f64(out)
+    assert np.isinf(ref[:3, 3]).all() and np.isinf(ref[3:, 5]).all() and not np.isnan(ref).any()
+    assert np.array_equal(np.isinf(got), np.isinf(ref)) and np.array_equal(got[np.isinf(ref)], ref[np.isinf(ref)])
