@@ -19,6 +19,7 @@ function drives synthetic traces and a real model.
 """
 from __future__ import annotations
 
+import functools
 from dataclasses import dataclass, field
 from typing import Callable, Optional
 
@@ -26,6 +27,19 @@ import numpy as np
 import torch
 
 from . import api
+
+
+def _on_the_models_device(method):
+    """The method of a ModelState or a TransformerLayer with the model's device current.  Some library calls launch on the current
+    device and its stream, others go by their tensors: here all of them go to one stream."""
+    @functools.wraps(method)
+    def run(self, *args, **kw):
+        dev = getattr(self, "m", self).table.device
+        if dev.type != "cuda" or dev.index is None or dev.index == torch.cuda.current_device():
+            return method(self, *args, **kw)
+        with torch.cuda.device(dev):
+            return method(self, *args, **kw)
+    return run
 
 
 @dataclass
@@ -110,6 +124,7 @@ class ModelState:
             api.sdvg_block_steps(self.cache, qs, ks, vs, q_ropeds, outs, self.grid, block * self.frames, self.table,
                                  self.tab_frames, block, self.scale, self.workspace)
 
+    @_on_the_models_device
     def check_status(self, where: str) -> None:
         """Raise if a kernel of this model gave up on a bounded wait since the workspace was last reset
         (the status word is sticky, so one check covers every launch since then); synchronises the stream."""
@@ -220,6 +235,7 @@ class TransformerLayer:
         return api.sdvg_rope3d_qk_commit_e4m3(m.cache, q, k, v, q_roped, None if q is None else m.q_inv_scale, m.k_inv_scale,
                                               m.v_inv_scale, m.grid, block * m.frames, m.table, m.tab_frames, block, flags)
 
+    @_on_the_models_device
     def step(self, x, mod, block: int, x_out) -> None:
         """One denoise step of `block`: the ring's slot of the block is staged, x_out (may be x) receives the stream."""
         m, w = self.m, self.w
@@ -244,6 +260,7 @@ class TransformerLayer:
             api.sdvg_gated_norm(self.x1, None, y=self.y, gate=gate2, gate_rows=rows, post_norm=api.SDVG_NORM_RMS,
                                 post_weight=w.post_ff, x_out=x_out, eps=w.eps)
 
+    @_on_the_models_device
     def commit(self, x, mod, block: int, check: bool = False) -> int:
         """The block's final K/V from its final stream into the ring (SDVG_FINAL); returns the evicted block.  K and V come from
         a product with bounded waits; ``check`` reads the status word (and so synchronises) before the ring is written, and

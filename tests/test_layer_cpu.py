@@ -123,3 +123,36 @@ def test_modulation_rows_of_any_number(monkeypatch, groups):
         assert kw["modulate_rows"] == rows
         assert kw["scale"].shape == kw["shift"].shape == (-(-TOKENS // rows), WIDTH)
         assert kw["scale"][:, 0].tolist() == [float(i) for i in range(-(-TOKENS // rows))]
+
+
+@pytest.mark.parametrize("current", [0, 1])
+def test_a_layer_runs_with_its_own_device_current(monkeypatch, current):
+    """The attention, the ring writes of 8-bit caches and the status read launch on the current device and its stream, whatever
+    their tensors' device; the norms and products go by their tensors.  All of a step has to be in one stream."""
+    r, m = Record(monkeypatch), model("drafter")
+    one = layer(m)
+    at, seen = [current], []
+
+    class Device:
+        def __init__(self, dev):
+            self.dev = torch.device(dev).index
+
+        def __enter__(self):
+            self.before, at[0] = at[0], self.dev
+
+        def __exit__(self, *_):
+            at[0] = self.before
+
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: at[0])
+    monkeypatch.setattr(torch.cuda, "device", Device)
+    for name in ("sdvg_gated_norm", "sdvg_linear", "sdvg_qk_norm_rope3d_commit", "sdvg_block_attn_fwd", "sdvg_block_attn_status"):
+        def call(*args, f=getattr(api, name), **kw):
+            seen.append(at[0])
+            return f(*args, **kw)
+        monkeypatch.setattr(api, name, call)
+    m.table = types.SimpleNamespace(device=torch.device("cuda", 1))
+    x, mod, x_out = provider()
+    one.step(x, mod, 0, x_out)
+    m.check_status("step")
+    one.commit(x, mod, 0, check=True)
+    assert seen == [1] * 13 and at == [current]
