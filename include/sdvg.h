@@ -571,7 +571,7 @@ int sdvg_block_steps_e4m3_tiled(int steps, sdvg_cache* cache, const void* const*
  *             itself (same pointer and stride), otherwise it must not overlap out
  *   out       device, out_type [rows, cols], row stride ld_out >= cols; must not overlap x, w, bias or gate
  * Products of the 16-bit operands on the tensor cores, fp32 accumulation over `inner`, fp32 epilogue.  The order of the sum
- * depends on the three sizes alone: equal calls give equal bits.
+ * depends on the three sizes, the output type and the device's SM count alone: equal calls give equal bits.
  * Strides and alignment: x and w are fetched by TMA, so their base addresses must be 16-byte aligned and ld_x, ld_w
  * multiples of 8 and >= inner (a single row's stride is not read); rows longer than `inner` are padding that is not read
  * into the result.  out, residual, bias and gate need the alignment of their element type only.

@@ -463,8 +463,8 @@ __global__ void __launch_bounds__(kTileThreads) linear_tile_kernel(const __grid_
 // (16 KB of weights and 64 tile_t bytes of tokens, written once and read once, at 128 bytes a clock; measured over `inner`:
 // 167, 190, 240 and 340 ns a stage for 64, 128, 176 and 256 tokens).  So tiles of 256 tokens are balanced and smaller ones
 // wait for shared memory; on long runs the power cap holds both back.  4680 x 5120 x 5120 with gate and residual: tensor
-// pipe active 89% of the time.  Under the power cap, back to back: 4680 x 5120 x 15360 567 us (1298 TFLOP/s; a library product
-// alone 542-557 on one box), x 20480 with GELU 756 (724-733 without).
+// pipe active 89% of the time.  Under the power cap, back to back, over several boxes: 4680 x 5120 x 15360 552 to 595 us (1334 to
+// 1237 TFLOP/s; a library product alone 542 to 560), x 20480 with GELU 737 to 780 (706 to 733).
 constexpr int kEpiWarps = 8;
 constexpr int kPairThreads = 32 * (kEpiWarps + 2);
 constexpr int kPairSmem = 227 * 1024 - 512;          // dynamic shared memory of a CTA; the barriers are static
@@ -767,6 +767,8 @@ int launch(LinearParams& p, const void* x, int64_t ld_x, const void* w, int64_t 
   if ((st = make_map(&p.w_map, w, in_type, inner, p.cols, ld_w, kTileF)) != SDVG_OK) return st;
   if ((st = make_map(&p.x_map, x, in_type, inner, p.rows, ld_x, by_pair ? p.tile_t / 2 : p.tile_t)) != SDVG_OK) return st;
   if (by_pair) {
+    // anything from 2 to 16 is within 3% of the best: 565 to 582 us at 4680 x 5120 x 15360 (4 best), 98 to 101 at 4680 x 6144 x 1536
+    // into fp32 (8 and up best); wider groups run out of L2, 64: 742 us there
     p.group = 8;
     p.stages = std::min(kMaxStages, (kPairSmem - 1024) / (kTileF * 128 + p.tile_t * 64));
     const int grid = 2 * (int)std::min((long long)pairs, p.tiles);

@@ -208,7 +208,8 @@ class TransformerLayer:
         return parts if with_q else [None] + parts
 
     def _rms(self, t, weight, out) -> torch.Tensor:
-        """RMS norm of a column range into a contiguous [tokens, heads, dim] tensor (an 8-bit ring takes such tensors)."""
+        """RMS norm of a column range into a contiguous [tokens, heads, dim] tensor (an 8-bit ring takes such tensors).  Rounded to
+        bf16 before the rotation, which over a bf16 ring is one pass with the norm and rounds once."""
         if self.w.scope == api.SDVG_SCOPE_ROW:
             api.sdvg_gated_norm(t, out, norm=api.SDVG_NORM_RMS, weight=weight, eps=self.w.eps)
         else:
