@@ -169,7 +169,7 @@ def test_overlapped_kernels_do_not_read_through_the_read_only_path():
     csrc = os.path.join(os.path.dirname(build.__file__), "csrc")
     text = {f: re.sub(r"//[^\n]*", "", open(os.path.join(csrc, f)).read()) for f in os.listdir(csrc)}
     overlapped = [f for f, t in text.items() if f.endswith(".cu") and "overlap_wait()" in t]
-    assert sorted(overlapped) == ["gated_norm.cu", "linear.cu", "qk_norm.cu"]
+    assert {"gated_norm.cu", "linear.cu", "qk_norm.cu"} <= set(overlapped)
     for f in overlapped + ["row_team.cuh", "elem_types.cuh"]:
         assert not re.search(r"__ldg\w*\(|ld\.global\S*\.nc|__restrict__", text[f]), f
 
