@@ -555,6 +555,7 @@ int sdvg_block_steps_e4m3_tiled(int steps, sdvg_cache* cache, const void* const*
 #define SDVG_BF16 0
 #define SDVG_F16  1
 #define SDVG_F32  2
+#define SDVG_E4M3 3   /* outputs of sdvg_linear_e4m3 only */
 
 #define SDVG_ACT_NONE      0
 #define SDVG_ACT_SILU      1   /* v / (1 + e^-v) */
@@ -642,6 +643,48 @@ int sdvg_qk_norm_rope3d_commit(sdvg_cache* cache, const void* q, int64_t ld_q, c
                                float eps, void* q_out, void* k_out, int frames, int grid_h, int grid_w,
                                int frame_offset, const float* cos_sin_tab, int tab_frames, int64_t block_index,
                                int flags, int64_t* evicted_block, void* stream);
+
+/* ---- 8-bit rows and weights: the dense operators on E4M3 matrices ------------------- */
+/*
+ * A matrix of E4M3 codes (as above) with POWER-OF-TWO SCALES, one per block of 128 columns and 1 row (activations) or 128 rows
+ * (weights): element [r, c] is code[r, c] * 2^(scale[r / block_rows, c / 128] - 127), scale a byte (255: NaN).  Codes and
+ * scales are row-major bytes with row strides ld_* of their own; a row has ceil(cols / 128) scales, the last block may be short.
+ * Quantising chooses 2^e with the smallest integer e in [-126, 120] for which the block's largest magnitude is at most
+ * 448 * 2^e (NaN elements do not count; an infinite maximum takes 120, an all-zero block -126) and stores e + 127;
+ * codes are e4m3(x / 2^e), round to nearest even, saturating, NaN stays NaN: exact but for that one rounding.
+ */
+
+/*
+ * x: device, x_type [rows, cols] -> out8: codes [rows, cols], scale: bytes [ceil(rows / block_rows), ceil(cols / 128)], block_rows 1
+ * or 128.  Pointers need the alignment of their element type; 16-byte rows are moved in vectors.  rows == 0 or cols == 0 is a
+ * call with nothing to do.  out8 must not overlap x.
+ * Errors: INVALID_ARG, BAD_SHAPE (also more than 2^31 - 1 tiles of 128 x 128), MISALIGNED, UNSUPPORTED_ARCH, CUDA.
+ */
+int sdvg_quant_e4m3_blocks(const void* x, int64_t ld_x, int x_type, void* out8, int64_t ld_out, void* scale,
+                           int64_t ld_scale, int block_rows, int rows, int cols, void* stream);
+
+/* The values back, rounded once to out_type: out[r, c] as above.  Arguments and errors as sdvg_quant_e4m3_blocks. */
+int sdvg_dequant_e4m3_blocks(const void* x8, int64_t ld_x, const void* scale, int64_t ld_scale, int block_rows, void* out,
+                             int64_t ld_out, int out_type, int rows, int cols, void* stream);
+
+/*
+ * sdvg_linear on such matrices: out[r, j] = residual[r, j] + gate[r / gate_rows, j] * act( sum_k x[r, k] w[j, k] + bias[j] )
+ *   x8, x_scale   codes [rows, inner] and scales [rows, ceil(inner / 128)] (block_rows 1)
+ *   w8, w_scale   codes [cols, inner] and scales [ceil(cols / w_scale_rows), ceil(inner / 128)], w_scale_rows 1 or 128
+ *   out           device, out_type: SDVG_BF16, SDVG_F16, SDVG_F32, or SDVG_E4M3: the result quantised (block_rows 1), codes in out and
+ *                 scales in out_scale [rows, ceil(cols / 128)]; residual must be NULL then, and out_scale with the other types
+ * Everything else as in sdvg_linear: products on the tensor cores, which apply the scales, fp32 accumulation and epilogue, one
+ * rounding per output; the order of the sum depends on the sizes, the output type and the SM count alone.
+ * Strides and alignment: x8 and w8 16-byte aligned, ld_x and ld_w multiples of 16 and >= inner; x_scale and w_scale 4-byte aligned,
+ * ld_x_scale and ld_w_scale multiples of 4 (a single row's stride is not read; bytes behind a row's scales are not either).
+ * out, out_scale, residual, bias and gate need the alignment of their element type only.
+ * Errors: those of sdvg_linear; INVALID_ARG also for another w_scale_rows.
+ */
+int sdvg_linear_e4m3(const void* x8, int64_t ld_x, const void* x_scale, int64_t ld_x_scale, const void* w8, int64_t ld_w,
+                     const void* w_scale, int64_t ld_w_scale, int w_scale_rows, const float* bias, int act, const float* gate,
+                     int64_t ld_gate, int gate_rows, const void* residual, int64_t ld_residual, void* out, int64_t ld_out,
+                     void* out_scale, int64_t ld_out_scale, int rows, int cols, int inner, int out_type, void* workspace,
+                     size_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus
 }

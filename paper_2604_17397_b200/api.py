@@ -31,7 +31,7 @@ SDVG_AGG_MIN = 0
 SDVG_AGG_MEAN = 1
 SDVG_SIGNAL_REWARD = 0
 SDVG_SIGNAL_RANDOM = 1
-SDVG_BF16, SDVG_F16, SDVG_F32 = 0, 1, 2
+SDVG_BF16, SDVG_F16, SDVG_F32, SDVG_E4M3 = 0, 1, 2, 3
 SDVG_ACT_NONE, SDVG_ACT_SILU, SDVG_ACT_GELU_TANH, SDVG_ACT_GELU = 0, 1, 2, 3
 SDVG_NORM_NONE, SDVG_NORM_RMS, SDVG_NORM_LAYER = 0, 1, 2
 SDVG_SCOPE_ROW, SDVG_SCOPE_HEAD = 0, 1
@@ -93,6 +93,10 @@ SIGNATURES = {
                              _I64, _I, _F, _VP, _I64, _I, _I, _I, _VP]),
     "sdvg_qk_norm_rope3d_commit": (_I, [_VP, _VP, _I64, _VP, _I64, _VP, _I64, _VP, _VP, _I, _F, _VP, _VP, _I, _I, _I, _I,
                                         _VP, _I, _I64, _I, C.POINTER(_I64), _VP]),
+    "sdvg_quant_e4m3_blocks": (_I, [_VP, _I64, _I, _VP, _I64, _VP, _I64, _I, _I, _I, _VP]),
+    "sdvg_dequant_e4m3_blocks": (_I, [_VP, _I64, _VP, _I64, _I, _VP, _I64, _I, _I, _I, _VP]),
+    "sdvg_linear_e4m3": (_I, [_VP, _I64, _VP, _I64, _VP, _I64, _VP, _I64, _I, _VP, _I, _VP, _I64, _I, _VP, _I64, _VP, _I64,
+                              _VP, _I64, _I, _I, _I, _I, _VP, _SZ, _VP]),
 }
 
 _lib = None
@@ -724,3 +728,50 @@ def sdvg_qk_norm_rope3d_commit(cache: Cache, q, k, v, q_weight, k_weight, scope:
     if evicted < -1:
         raise SdvgError(-1000 - evicted, "sdvg_qk_norm_rope3d_commit")
     return evicted
+
+
+# ---------------------------------------------------------------- 8-bit rows and weights
+
+def e4m3_matrix(rows: int, cols: int, block_rows: int = 1, device="cuda"):
+    """(codes, scales) of an E4M3 matrix, uninitialised uint8 [rows, cols] and [ceil(rows / block_rows), ceil(cols / 128)] with the
+    row strides that sdvg_linear_e4m3 reads."""
+    new = lambda r, c: torch.empty((r, -(-c // 16) * 16), dtype=torch.uint8, device=device)[:, :c]
+    return new(rows, cols), new(-(-rows // block_rows), -(-cols // 128))
+
+
+def sdvg_quant_e4m3_blocks(x, out8, scale, stream=None) -> None:
+    """x [rows, cols] of bf16, fp16 or fp32 -> uint8 codes of the same shape and scale bytes [rows, blocks] (one per 128 columns of a
+    row) or [ceil(rows / 128), blocks] (one per 128 x 128 block), blocks = ceil(cols / 128)."""
+    dev = _device_of(x)
+    if _elsewhere(dev):
+        with torch.cuda.device(dev):
+            return sdvg_quant_e4m3_blocks(x, out8, scale, stream)
+    st = _binding().e4m3_blocks(x, out8, scale, 1, _raw_stream(dev, stream))
+    if st != SDVG_OK:
+        raise SdvgError(st, "sdvg_quant_e4m3_blocks")
+
+
+def sdvg_dequant_e4m3_blocks(x8, scale, out, stream=None) -> None:
+    """The values of such a matrix, rounded once to out's type (bf16, fp16 or fp32)."""
+    dev = _device_of(x8)
+    if _elsewhere(dev):
+        with torch.cuda.device(dev):
+            return sdvg_dequant_e4m3_blocks(x8, scale, out, stream)
+    st = _binding().e4m3_blocks(out, x8, scale, 0, _raw_stream(dev, stream))
+    if st != SDVG_OK:
+        raise SdvgError(st, "sdvg_dequant_e4m3_blocks")
+
+
+def sdvg_linear_e4m3(x8, x_scale, w8, w_scale, out, workspace, bias=None, act: int = SDVG_ACT_NONE, residual=None, gate=None,
+                     gate_rows: int = 0, out_scale=None, stream=None) -> None:
+    """sdvg_linear on E4M3 matrices: x8 [rows, inner] with scales [rows, blocks], w8 [cols, inner] with scales [ceil(cols / 128), blocks]
+    or [cols, blocks]; out [rows, cols] of bf16, fp16 or fp32, or uint8 codes with their scales in out_scale [rows, ceil(cols / 128)]
+    (no residual then).  Row strides: x8 and w8 multiples of 16, their scales' multiples of 4 (``e4m3_matrix`` makes such)."""
+    dev = _device_of(x8)
+    if _elsewhere(dev):
+        with torch.cuda.device(dev):
+            return sdvg_linear_e4m3(x8, x_scale, w8, w_scale, out, workspace, bias, act, residual, gate, gate_rows, out_scale, stream)
+    st = _binding().linear_e4m3(x8, x_scale, w8, w_scale, out, workspace, bias, act, residual, gate, gate_rows, out_scale,
+                                _raw_stream(dev, stream))
+    if st != SDVG_OK:
+        raise SdvgError(st, "sdvg_linear_e4m3")

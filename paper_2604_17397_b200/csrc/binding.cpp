@@ -147,6 +147,84 @@ PyObject* linear(PyObject*, PyObject* const* args, Py_ssize_t n) {
   return PyLong_FromLong(st);
 }
 
+// A matrix of codes and its scales, one per 128 columns and `block_rows` rows.
+struct Coded {
+  Matrix codes, scale;
+};
+Coded coded(Reader& r, const Tensor* codes, const Tensor* scale, int64_t rows, int64_t cols, int64_t block_rows, const char* what,
+            const char* scale_what) {
+  Coded c;
+  c.codes = matrix(r, codes, rows, cols, ScalarType::Byte, what);
+  c.scale = matrix(r, scale, (rows + block_rows - 1) / block_rows, (cols + 127) / 128, ScalarType::Byte, scale_what);
+  return c;
+}
+// Rows per scale of a matrix of `rows` rows: 128 or 1, by the number of rows that its scales have.
+int64_t block_rows_of(const Tensor& scale, int64_t rows) {
+  return scale.dim() == 2 && scale.size(0) == (rows + 127) / 128 ? 128 : 1;
+}
+
+// (x8, x_scale, w8, w_scale, out, workspace, bias, act, residual, gate, gate_rows, out_scale, stream) -> status
+PyObject* linear_e4m3(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  if (n != 13) return PyErr_Format(PyExc_TypeError, "linear_e4m3 takes 13 arguments");
+  Reader r{args};
+  const Tensor *x = r.tensor(0, "x8", false), *xs = r.tensor(1, "x_scale", false), *w = r.tensor(2, "w8", false),
+               *ws = r.tensor(3, "w_scale", false), *out = r.tensor(4, "out", false), *space_t = r.tensor(5, "workspace", false),
+               *os = r.tensor(11, "out_scale", true);
+  if (!r.ok) return nullptr;
+  if (x->dim() != 2 || w->dim() != 2) return r.fail("x8, w8", "expected matrices"), nullptr;
+  const int64_t rows = x->size(0), inner = x->size(1), cols = w->size(0), w_rows = block_rows_of(*ws, cols);
+  const ScalarType to = out->scalar_type();
+  if (os ? to != ScalarType::Byte : elem_type(to) < 0)
+    return r.fail("out", "must be bfloat16, float16 or float32, or uint8 codes with out_scale"), nullptr;
+  if (rows > 0x7fffffff || cols > 0x7fffffff || inner > 0x7fffffff) return r.fail("x8, w8", "too large"), nullptr;
+  const int act = r.small(7), gate_rows = r.small(10);
+  const Coded mx = coded(r, x, xs, rows, inner, 1, "x8", "x_scale"), mw = coded(r, w, ws, cols, inner, w_rows, "w8", "w_scale");
+  Coded mo;
+  if (os) mo = coded(r, out, os, rows, cols, 1, "out", "out_scale");
+  else mo.codes = matrix(r, out, rows, cols, to, "out");
+  const Matrix res = matrix(r, r.tensor(8, "residual", true), rows, cols, to, "residual"),
+               gate = groups(r, 9, rows, cols, gate_rows, "gate");
+  const float* bias = vector(r, 6, cols, "bias");
+  void* stream = r.address(12);
+  if (!r.ok) return nullptr;
+  // whatever may throw is read before the interpreter lock is released
+  void* const space = space_t->data_ptr();
+  const size_t space_bytes = space_t->nbytes();
+  int st;
+  Py_BEGIN_ALLOW_THREADS
+  st = sdvg_linear_e4m3(mx.codes.p, mx.codes.ld, mx.scale.p, mx.scale.ld, mw.codes.p, mw.codes.ld, mw.scale.p, mw.scale.ld,
+                        (int)w_rows, bias, act, static_cast<const float*>(gate.p), gate.ld, gate_rows, res.p, res.ld, mo.codes.p,
+                        mo.codes.ld, mo.scale.p, mo.scale.ld, (int)rows, (int)cols, (int)inner, os ? SDVG_E4M3 : elem_type(to), space,
+                        space_bytes, stream);
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(st);
+}
+
+// (values, codes, scale, to_codes, stream) -> status
+PyObject* e4m3_blocks(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  if (n != 5) return PyErr_Format(PyExc_TypeError, "e4m3_blocks takes 5 arguments");
+  Reader r{args};
+  const Tensor *x = r.tensor(0, "values", false), *c = r.tensor(1, "codes", false), *s = r.tensor(2, "scale", false);
+  if (!r.ok) return nullptr;
+  if (x->dim() != 2 || elem_type(x->scalar_type()) < 0)
+    return r.fail("values", "expected a matrix of bfloat16, float16 or float32"), nullptr;
+  const int64_t rows = x->size(0), cols = x->size(1), block_rows = block_rows_of(*s, rows);
+  if (rows > 0x7fffffff || cols > 0x7fffffff) return r.fail("values", "too large"), nullptr;
+  const Matrix m = matrix(r, x, rows, cols, x->scalar_type(), "values");
+  const Coded q = coded(r, c, s, rows, cols, block_rows, "codes", "scale");
+  const int quantise = r.small(3);
+  void* stream = r.address(4);
+  if (!r.ok) return nullptr;
+  int st;
+  Py_BEGIN_ALLOW_THREADS
+  st = quantise ? sdvg_quant_e4m3_blocks(m.p, m.ld, m.type, q.codes.p, q.codes.ld, q.scale.p, q.scale.ld, (int)block_rows, (int)rows,
+                                         (int)cols, stream)
+                : sdvg_dequant_e4m3_blocks(q.codes.p, q.codes.ld, q.scale.p, q.scale.ld, (int)block_rows, m.p, m.ld, m.type, (int)rows,
+                                           (int)cols, stream);
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(st);
+}
+
 // (x, out, y, gate, gate_rows, post_norm, post_weight, x_out, norm, weight, bias, scale, shift, modulate_rows, eps, stream)
 // -> status
 PyObject* gated_norm(PyObject*, PyObject* const* args, Py_ssize_t n) {
@@ -253,6 +331,7 @@ PyMethodDef method(const char* name) {
 }
 
 PyMethodDef methods[] = {method<linear>("linear"), method<gated_norm>("gated_norm"), method<qk_norm>("qk_norm"),
+                         method<linear_e4m3>("linear_e4m3"), method<e4m3_blocks>("e4m3_blocks"),
                          {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

@@ -1,0 +1,762 @@
+// Linear layer on E4M3 operands with power-of-two block scales: out = residual + gate * act(x W^T + bias), where a row of x has one
+// scale per 128 elements of `inner`, and W one per 128 x 128 block (or per row and 128 elements).
+//
+// The scales never meet the sums in registers: the tensor core takes them itself (tcgen05.mma kind::mxf8f6f4.block_scale, one
+// exponent byte per operand row and step of 32 elements).  Four instructions of 32 elements make a stage of 128, so all
+// four take the same byte, and a 32-bit word of scales serves four stages.  As in linear.cu the weights are the M-side
+// operand, accumulator lanes are features and columns tokens; a stage is the same 128-byte rows with twice the elements.
+//
+// A warp of its own brings the scales: it gathers the words of the tile's rows (row-major bytes, so that whoever made them
+// needs to know no layout), puts them into shared memory in the order of the tensor core and hands them to the issuer, which
+// copies them to tensor memory (tcgen05.cp) in order with its products.
+#include <cuda.h>
+#include <math.h>
+
+#include <algorithm>
+#include <mutex>
+
+#include "e4m3_scale.cuh"
+#include "elem_types.cuh"
+#include "linear_epilogue.cuh"
+#include "overlap.cuh"
+#include "sdvg_internal.h"
+#include "tensor_map.h"
+
+namespace {
+
+using namespace linear;
+
+constexpr int kTileK = 128;                          // elements of `inner` per stage: one 128-byte swizzled row, one scale
+constexpr int kWordStages = 4;                       // stages that a 32-bit word of scales serves
+constexpr int kMaxStages = 8;
+constexpr int kScaleSlots = 4;                       // words of scales on their way
+constexpr int kWorkspaceBytes = 256;
+constexpr int kMaxDevices = 64;
+
+struct alignas(64) Linear8Params : EpilogueParams {
+  CUtensorMap w_map;                                 // box 128 x 128 features
+  CUtensorMap x_map;                                 // box 128 x tile_t tokens (tiles), or half of them (pairs)
+  const uint8_t *x_scale, *w_scale;                  // exponent bytes: of row r and 128-element block b at scale[(r >> shift) * ld + b]
+  long long ld_xs, ld_ws;
+  int w_shift;                                       // 0 or 7
+  uint8_t* out_scale;                                // 8-bit outputs: exponent byte of row r and 128-column block b
+  long long ld_os;
+  int tile_t, tiles_f, tiles_t, k_iters, stages;
+  int split;                                         // CTAs (a cluster) that share a tile's sum; tiles only
+  int group;                                         // feature tiles of a group of the tile order (pairs)
+  long long tiles;
+  uint32_t idesc;
+  unsigned int* status;
+};
+
+// Word `word` (blocks 4 word .. 4 word + 3) of a row of `blocks` exponent bytes; bytes past the row's end are not read.
+__device__ __forceinline__ uint32_t scale_word(const uint8_t* row, int word, int blocks) {
+  const uint8_t* at = row + 4 * word;
+  if (4 * word + 4 <= blocks) return *reinterpret_cast<const uint32_t*>(at);
+  uint32_t v = 0;
+#pragma unroll
+  for (int j = 0; j < 3; ++j)
+    if (4 * word + j < blocks) v |= (uint32_t)at[j] << (8 * j);
+  return v;
+}
+
+// Words of rows r0 + lane, + 32, .. (GROUPS * 128 of them, those from r_end on read as 0) into GROUPS blocks of 512 bytes, [32
+// lanes][4 words] each: the order in which they are copied to tensor memory.
+template <int GROUPS>
+__device__ __forceinline__ void stage_scales(uint4* to, const uint8_t* scale, long long ld, int shift, int r0, int r_end, int word,
+                                             int blocks) {
+  const int lane = threadIdx.x % 32;
+  uint32_t w[4 * GROUPS];
+#pragma unroll
+  for (int c = 0; c < 4 * GROUPS; ++c) {
+    const int r = r0 + 32 * c + lane;
+    w[c] = r < r_end ? scale_word(scale + (long long)(r >> shift) * ld, word, blocks) : 0;
+  }
+#pragma unroll
+  for (int g = 0; g < GROUPS; ++g) to[32 * g + lane] = make_uint4(w[4 * g], w[4 * g + 1], w[4 * g + 2], w[4 * g + 3]);
+}
+
+// fp32 outputs: the tensor core adds products to the accumulator by truncation, so a long sum drifts; there it is cut into chunks
+// that are added with round-to-nearest, as in linear.cu.  A step of the 8-bit kind adds 32 products, twice those of the 16-bit
+// kind, so that chunks are twice as long for the same drift.
+constexpr int kPairChunkIters = 1280 / kTileK;
+constexpr int kTileChunkIters = 512 / kTileK;
+
+// ---- 8-bit outputs ------------------------------------------------------------------------------
+// The four warps that hold the 128 features of a block exchange their largest magnitudes per token through shared memory: 16 tokens
+// at a time, two buffers in turn, one bounded wait.
+struct Exchange {
+  uint4 top[2][16];                                  // [turn][token] of the four warps
+  uint64_t bar;                                      // a warp's arrival
+};
+
+// Rounds 16 tokens of the block (acc: this lane's feature n) to E4M3 and stores them with their scales.  Returns false when a wait gave up.
+__device__ __forceinline__ bool quantise16(const Linear8Params& p, Exchange& x, int& turn, const float (&acc)[16], int n, int quad,
+                                           int m0, int m_end) {
+  const int lane = threadIdx.x % 32;
+  const bool mine = n < p.cols;
+  uint32_t top = 0;
+#pragma unroll
+  for (int j = 0; j < 16; ++j) {
+    const uint32_t m = __reduce_max_sync(0xffffffffu, mine ? sdvg::magnitude_bits(acc[j]) : 0u);
+    if (lane == j) top = m;
+  }
+  const int buffer = turn & 1;
+  if (lane < 16) reinterpret_cast<uint32_t*>(&x.top[buffer][lane])[quad] = top;
+  __syncwarp();
+  if (lane == 0) mbar_arrive(&x.bar);
+  const bool ok = __all_sync(0xffffffffu, wait_for(&x.bar, (uint32_t)buffer, p.status, kWaitLimitNs));
+  ++turn;
+  if (!ok) return false;
+  const uint4 t = x.top[buffer][lane % 16];
+  const int e = sdvg::scale_exponent(max(max(t.x, t.y), max(t.z, t.w)));
+  const int block = n / 128;                         // the same for the warp
+  if (quad == 0 && lane < 16 && m0 + lane < m_end && block * 128 < p.cols)
+    p.out_scale[(long long)(m0 + lane) * p.ld_os + block] = (uint8_t)(e + 127);
+  const float inv = sdvg::power_of_two(-e);
+  const long long ld = stride_here(p.ld_out);
+  uint8_t* o = static_cast<uint8_t*>(p.out) + m0 * ld + n;
+#pragma unroll
+  for (int j = 0; j < 16; j += 4) {
+    const float i0 = __shfl_sync(0xffffffffu, inv, j), i1 = __shfl_sync(0xffffffffu, inv, j + 1),
+                i2 = __shfl_sync(0xffffffffu, inv, j + 2), i3 = __shfl_sync(0xffffffffu, inv, j + 3);
+    const uint32_t c = pack_e4m3x4(acc[j] * i0, acc[j + 1] * i1, acc[j + 2] * i2, acc[j + 3] * i3);
+#pragma unroll
+    for (int i = 0; i < 4; ++i, o += ld)
+      if (mine && m0 + j + i < m_end) *o = (uint8_t)(c >> (8 * i));
+  }
+  return true;
+}
+
+// ---- few tokens: a cluster per tile, which splits `inner` ---------------------------------------
+constexpr int kTileThreads = 224;                    // four epilogue warps, producer, issuer, scales
+constexpr int kMaxTileFew = 64;                      // tokens per tile
+constexpr int kMaxSplit = 8;                         // portable cluster size
+constexpr int kTileSlotBytes = 1024;                 // a word of scales of the tile's features, and of its tokens
+constexpr int kTileScaleCols = 8;                    // and its columns in tensor memory
+
+struct TileSmem {
+  uint64_t full[kMaxStages], empty[kMaxStages], sf_full[kScaleSlots], sf_empty[kScaleSlots], acc_full, acc_empty;
+  Exchange exchange;
+  uint32_t tmem;
+};
+
+// Tensor memory columns: the accumulator (whose place the total of several chunks takes) and two words of scales.
+__host__ __device__ constexpr uint32_t tile_tmem_cols(int tile_t) {
+  uint32_t cols = 32;
+  while (cols < (uint32_t)tile_t + 2 * kTileScaleCols) cols *= 2;
+  return cols;
+}
+
+template <int OutType>
+__global__ void __launch_bounds__(kTileThreads) linear8_tile_kernel(const __grid_constant__ Linear8Params p) {
+  constexpr bool kChunked = OutType == SDVG_F32, kOut8 = OutType == SDVG_E4M3;
+  using T = typename OutElem<OutType>::T;
+  extern __shared__ uint8_t raw[];
+  __shared__ TileSmem sm;
+  uint8_t* buf = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  const int rank = p.split > 1 ? (int)cluster_ctarank() : 0, tile = blockIdx.x / p.split;
+  const int n0 = (tile % p.tiles_f) * kTileF;
+  const int m0 = (tile / p.tiles_f) * p.tile_t, m_end = min(p.rows, m0 + p.tile_t);
+  const int w_bytes = kTileF * 128, stage_bytes = w_bytes + p.tile_t * 128;
+  uint8_t* slots = buf + p.stages * stage_bytes;
+  // this CTA's part of `inner`: never empty
+  const int share = p.k_iters / p.split, rest = p.k_iters % p.split;
+  const int k0 = rank * share + min(rank, rest), iters = share + (rank < rest ? 1 : 0);
+  const int word0 = k0 / kWordStages, words = (k0 + iters - 1) / kWordStages - word0 + 1;
+  const int chunks = kChunked ? (iters + kTileChunkIters - 1) / kTileChunkIters : 1;
+  const uint32_t tmem_cols = tile_tmem_cols(p.tile_t);
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < p.stages; ++s) {
+      mbar_init(&sm.full[s], 1);
+      mbar_init(&sm.empty[s], 1);
+    }
+    for (int s = 0; s < kScaleSlots; ++s) {
+      mbar_init(&sm.sf_full[s], 1);
+      mbar_init(&sm.sf_empty[s], 1);
+    }
+    mbar_init(&sm.acc_full, 1);
+    mbar_init(&sm.acc_empty, 4);
+    mbar_init(&sm.exchange.bar, 4);
+    fence_mbar_init();
+    prefetch_tmap(&p.w_map);
+    prefetch_tmap(&p.x_map);
+  }
+  if (warp == 0) {
+    tmem_alloc(&sm.tmem, tmem_cols);
+    tmem_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = sm.tmem;
+  sdvg::overlap_wait();
+
+  if (warp == 4) {
+    if (elect_one()) {
+      int i = 0;
+      RingPos r;
+      for (; i < iters; ++i, r.next(p.stages)) {
+        const int s = r.stage;
+        if (!wait_for(&sm.empty[s], r.phase ^ 1, p.status, kWaitLimitNs)) break;
+        uint8_t* st = buf + s * stage_bytes;
+        mbar_expect_tx(&sm.full[s], stage_bytes);
+        tma_load_2d(st, &p.w_map, &sm.full[s], (k0 + i) * kTileK, n0);
+        tma_load_2d(st + w_bytes, &p.x_map, &sm.full[s], (k0 + i) * kTileK, m0);
+      }
+      // only now, as in linear.cu: a next grid that starts while SMs still hold several of these CTAs lands on the wrong SMs
+      sdvg::overlap_begin();
+      if (i < iters)                                   // gave up: see the copies in flight land before the CTA may leave
+        for (int j = min(i, p.stages); j > 0; --j) {
+          r.back(p.stages);
+          wait_for(&sm.full[r.stage], r.phase, p.status, kWaitLimitNs);
+        }
+    }
+    __syncwarp();
+  } else if (warp == 5) {
+    if (elect_one()) {
+      bool ok = true;
+      RingPos r, acc, sf;
+      int word = -1;                                   // none yet
+      uint32_t scales = 0;
+      for (int c = 0; ok && c < chunks; ++c, acc.next(1)) {
+        if (!(ok = wait_for(&sm.acc_empty, acc.phase ^ 1, p.status, kWaitLimitNs))) break;
+        tc_fence_after();
+        const int i0 = c * kTileChunkIters, i1 = kChunked ? min(iters, i0 + kTileChunkIters) : iters;
+        for (int i = i0; i < i1; ++i, r.next(p.stages)) {
+          const int s = r.stage, k = k0 + i;
+          if (k / kWordStages != word) {
+            word = k / kWordStages;
+            if (!(ok = wait_for(&sm.sf_full[sf.stage], sf.phase, p.status, kWaitLimitNs))) break;
+            tc_fence_after();
+            // two places in turn: the products of the word before may still read theirs
+            scales = tmem + p.tile_t + (word & 1) * kTileScaleCols;
+            const uint32_t from = smem_u32(slots + sf.stage * kTileSlotBytes);
+            tmem_cp_scales(scales, from);
+            tmem_cp_scales(scales + 4, from + 512);
+            mma_commit(&sm.sf_empty[sf.stage]);
+            sf.next(kScaleSlots);
+          }
+          if (!(ok = wait_for(&sm.full[s], r.phase, p.status, kWaitLimitNs))) break;
+          tc_fence_after();
+          const uint32_t st = smem_u32(buf + s * stage_bytes);
+          const uint64_t a = smem_desc_sw128(st, 16, 1024), b = smem_desc_sw128(st + w_bytes, 16, 1024);
+          const uint32_t idesc = p.idesc | idesc_scale_step(k % kWordStages);
+#pragma unroll
+          for (int kk = 0; kk < 4; ++kk)
+            mma_ss_mx(tmem, a + 2 * kk, b + 2 * kk, idesc, scales, scales + 4, i > i0 || kk > 0);
+          mma_commit(&sm.empty[s]);
+        }
+        if (ok) mma_commit(&sm.acc_full);
+      }
+    }
+    __syncwarp();
+  } else if (warp == 6) {
+    RingPos sf;
+    for (int w = 0; w < words; ++w, sf.next(kScaleSlots)) {
+      if (!__all_sync(0xffffffffu, wait_for(&sm.sf_empty[sf.stage], sf.phase ^ 1, p.status, kWaitLimitNs))) break;
+      uint4* to = reinterpret_cast<uint4*>(slots + sf.stage * kTileSlotBytes);
+      stage_scales<1>(to, p.w_scale, p.ld_ws, p.w_shift, n0, min(p.cols, n0 + kTileF), word0 + w, p.k_iters);
+      stage_scales<1>(to + 32, p.x_scale, p.ld_xs, 0, m0, m_end, word0 + w, p.k_iters);
+      fence_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&sm.sf_full[sf.stage]);
+    }
+  } else {
+    const uint32_t lanes = tmem + ((uint32_t)(warp * 32) << 16);
+    const int n = n0 + warp * 32 + lane;
+    const float b = p.bias && n < p.cols ? p.bias[n] : 0.f;
+    RingPos r;
+    const bool summed = kChunked && chunks > 1;
+    bool ok;
+    if (summed)
+      ok = add_chunks<1, kMaxTileFew / 16>(chunks, lanes, p.tile_t, 0, [](int i) { return 16 * i; }, m_end - m0, r, &sm.acc_full,
+                                           p.status, [&](int) {
+        if (lane == 0) mbar_arrive(&sm.acc_empty);
+      });
+    else
+      ok = __all_sync(0xffffffffu, wait_for(&sm.acc_full, r.phase, p.status, kWaitLimitNs));
+    if (ok) {
+      tc_fence_after();
+      const TileGate gate = tile_gate(p, n, m0, m_end);
+      float* mine = reinterpret_cast<float*>(buf) + warp * 32 + lane;      // [token][128 features]: the ring is read and free
+      int turn = 0;
+#pragma unroll 1
+      for (int c = 0; ok && m0 + c < m_end; c += 16) {
+        float acc[16];
+        T res[16];
+        if (!kOut8 && p.split == 1) load_residual16<OutType>(p, res, n, m0 + c, m_end);
+        tmem_ld16(lanes + c, reinterpret_cast<uint32_t(&)[16]>(acc));
+        tmem_wait_ld();
+        if (p.split > 1) {
+#pragma unroll
+          for (int j = 0; j < 16; ++j) mine[(c + j) * kTileF] = acc[j];
+        } else if constexpr (kOut8) {
+          if (n < p.cols) gated16(p, acc, n, m0 + c, min(16, m_end - m0 - c), b, gate);
+          ok = quantise16(p, sm.exchange, turn, acc, n, warp, m0 + c, m_end);
+        } else {
+          epilogue16<OutType>(p, acc, res, n, m0 + c, m_end, b, gate);
+        }
+      }
+    }
+  }
+  if (p.split > 1) {
+    // a CTA that gave up joins the barriers as well; the status word says that the outputs are undefined
+    cluster_arrive();
+    cluster_wait();
+    if (warp < 4) {
+      const int per = (m_end - m0 + p.split - 1) / p.split, first = rank * per, last = min(m_end - m0, first + per);
+      const int n = n0 + warp * 32 + lane;
+      const float b = p.bias && n < p.cols ? p.bias[n] : 0.f;
+      const uint32_t mine = smem_u32(buf) + (warp * 32 + lane) * 4;
+      const TileGate gate = tile_gate(p, n, m0 + first, m0 + last);
+      int turn = 0;
+#pragma unroll 1
+      for (int c = first; c < last; c += 16) {
+        T res[16];
+        if (!kOut8) load_residual16<OutType>(p, res, n, m0 + c, m0 + last);
+        float acc[16];
+#pragma unroll
+        for (int j = 0; j < 16; ++j) acc[j] = 0.f;
+#pragma unroll 1
+        for (int s = 0; s < p.split; ++s) {
+          const uint32_t from = map_to_rank(mine, s);
+#pragma unroll
+          for (int j = 0; j < 16; ++j)
+            if (c + j < last) acc[j] += ld_cluster_f32(from + (c + j) * kTileF * 4);
+        }
+        if constexpr (kOut8) {
+          if (n < p.cols) gated16(p, acc, n, m0 + c, min(16, last - c), b, gate);
+          if (!quantise16(p, sm.exchange, turn, acc, n, warp, m0 + c, m0 + last)) break;
+        } else {
+          epilogue16<OutType>(p, acc, res, n, m0 + c, m0 + last, b, gate);
+        }
+      }
+    }
+    __syncwarp();
+    cluster_arrive();
+    cluster_wait();                                    // nobody leaves while its sums may still be read
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  if (warp == 0) tmem_dealloc(tmem, tmem_cols);
+}
+
+// ---- many tokens: CTA pairs, persistent ---------------------------------------------------------
+//
+// As in linear.cu: a tile is 256 features x tile_t tokens on two SMs, one tcgen05.mma of the even CTA reads the operands of
+// both.  Each CTA's tensor memory holds the scales of its own features and of all the tile's tokens; the even CTA's copy moves
+// both CTAs' words at once.  The last 32 columns of tensor memory are the scales' (two words in turn), which leaves
+// accumulators of 240 columns for two tiles in flight.
+constexpr int kEpiWarps = 8;
+constexpr int kPairThreads = 32 * (kEpiWarps + 3);
+constexpr int kPairSlotBytes = 512 + 1024;           // a word of scales of the CTA's features, and of the tile's tokens
+constexpr int kPairSmem = 227 * 1024 - 2048;         // dynamic shared memory of a CTA; the barriers and exchanges are static
+constexpr int kMaxTileT = 240, kMaxTileChunked = 112;
+constexpr int kScaleCol = 480, kPairScaleCols = 16;
+template <int OutType>
+constexpr int kAccs = OutType == SDVG_F32 ? 3 : 2;
+template <int OutType>
+constexpr int kAccStride = OutType == SDVG_F32 ? kMaxTileChunked : kMaxTileT;
+static_assert((kAccs<SDVG_F32> + 1) * kAccStride<SDVG_F32> <= kScaleCol && kAccs<SDVG_BF16> * kAccStride<SDVG_BF16> <= kScaleCol);
+static_assert(kScaleCol + 2 * kPairScaleCols <= 512);
+
+struct PairSmem {
+  uint64_t full[kMaxStages], empty[kMaxStages], sf_full[kScaleSlots], sf_empty[kScaleSlots], acc_full[3], acc_empty[3];
+  Exchange exchange[2];
+  uint32_t tmem;
+};
+static_assert(sizeof(PairSmem) <= 2048 - 512);
+
+template <int OutType>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
+    linear8_pair_kernel(const __grid_constant__ Linear8Params p) {
+  constexpr bool kChunked = OutType == SDVG_F32, kOut8 = OutType == SDVG_E4M3;
+  using T = typename OutElem<OutType>::T;
+  extern __shared__ uint8_t raw[];
+  __shared__ PairSmem sm;
+  uint8_t* buf = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  const uint32_t rank = cluster_ctarank();
+  const int pair = blockIdx.x / 2, pairs = gridDim.x / 2;
+  const int w_bytes = kTileF * 128, stage_bytes = w_bytes + p.tile_t * 64;
+  uint8_t* slots = buf + p.stages * stage_bytes;
+  const int chunks = kChunked ? (p.k_iters + kPairChunkIters - 1) / kPairChunkIters : 1;
+  const int words = (p.k_iters + kWordStages - 1) / kWordStages;
+  sdvg::overlap_begin();
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < p.stages; ++s) {
+      mbar_init(&sm.full[s], 1);                     // the even CTA's counts the bytes of both
+      mbar_init(&sm.empty[s], 1);
+    }
+    for (int s = 0; s < kScaleSlots; ++s) {
+      mbar_init(&sm.sf_full[s], 2);                  // the even CTA's: the scale warps of both
+      mbar_init(&sm.sf_empty[s], 1);
+    }
+    for (int b = 0; b < kAccs<OutType>; ++b) {
+      mbar_init(&sm.acc_full[b], 1);
+      mbar_init(&sm.acc_empty[b], 2 * kEpiWarps);    // the even CTA's: the epilogue warps of both
+    }
+    for (int h = 0; h < 2; ++h) mbar_init(&sm.exchange[h].bar, 4);
+    fence_mbar_init();
+    prefetch_tmap(&p.w_map);
+    prefetch_tmap(&p.x_map);
+  }
+  if (warp == 0) {
+    tmem_alloc_pair(&sm.tmem, 512);
+    tmem_relinquish_pair();
+  }
+  tc_fence_before();
+  __syncthreads();
+  cluster_arrive();
+  cluster_wait();                                    // the other CTA's barriers are initialised as well
+  tc_fence_after();
+  const uint32_t tmem = sm.tmem;
+  sdvg::overlap_wait();
+
+  if (warp == kEpiWarps) {
+    // ================= producer: this CTA's features and its half of the token tile =================
+    if (elect_one()) {
+      RingPos r;
+      int issued = 0;                                // up to the number of stages
+      bool ok = true;
+      for (long long t = pair; ok && t < p.tiles; t += pairs) {
+        int ft, tt;
+        tile_of(p, t, &ft, &tt);
+        const int n0 = (2 * ft + (int)rank) * kTileF, m0 = tt * p.tile_t + (int)rank * (p.tile_t / 2);
+        for (int i = 0; i < p.k_iters; ++i, r.next(p.stages)) {
+          const int s = r.stage;
+          if (!(ok = wait_for(&sm.empty[s], r.phase ^ 1, p.status, kWaitLimitNs))) break;
+          issued = min(issued + 1, p.stages);
+          uint8_t* st = buf + s * stage_bytes;
+          const uint32_t full = map_to_rank(smem_u32(&sm.full[s]), 0);
+          if (rank == 0) mbar_expect_tx(&sm.full[s], 2 * stage_bytes);
+          tma_load_2d_pair(st, &p.w_map, full, i * kTileK, n0);
+          tma_load_2d_pair(st + w_bytes, &p.x_map, full, i * kTileK, m0);
+        }
+      }
+      // every stage is read (on a give-up: landed, as far as this CTA can tell) before the CTA may leave
+      for (; issued > 0; --issued) {
+        r.back(p.stages);
+        if (ok) ok = wait_for(&sm.empty[r.stage], r.phase, p.status, kWaitLimitNs);
+        else if (rank == 0) wait_for(&sm.full[r.stage], r.phase, p.status, kWaitLimitNs);
+      }
+    }
+  } else if (warp == kEpiWarps + 1) {
+    // ================= issuer: the even CTA, for both ==============================================
+    if (rank == 0 && elect_one()) {
+      RingPos r, acc, sf;
+      uint32_t scales = 0;
+      bool ok = true;
+      for (long long t = pair; ok && t < p.tiles; t += pairs) {
+        for (int c = 0; ok && c < chunks; ++c, acc.next(kAccs<OutType>)) {
+          const int b = acc.stage;
+          if (!(ok = wait_for(&sm.acc_empty[b], acc.phase ^ 1, p.status, kWaitLimitNs))) break;
+          tc_fence_after();
+          const int i0 = c * kPairChunkIters, i1 = kChunked ? min(p.k_iters, i0 + kPairChunkIters) : p.k_iters;
+          for (int i = i0; i < i1; ++i, r.next(p.stages)) {
+            const int s = r.stage;
+            if (i % kWordStages == 0) {
+              if (!(ok = wait_for(&sm.sf_full[sf.stage], sf.phase, p.status, kWaitLimitNs))) break;
+              tc_fence_after();
+              // two places in turn: the products of the word before may still read theirs
+              scales = tmem + kScaleCol + (sf.stage & 1) * kPairScaleCols;
+              const uint32_t from = smem_u32(slots + sf.stage * kPairSlotBytes);
+              tmem_cp_scales_pair(scales, from);
+              tmem_cp_scales_pair(scales + 4, from + 512);
+              if (p.tile_t > 128) tmem_cp_scales_pair(scales + 8, from + 1024);
+              mma_commit_pair(&sm.sf_empty[sf.stage]);
+              sf.next(kScaleSlots);
+            }
+            if (!(ok = wait_for(&sm.full[s], r.phase, p.status, kWaitLimitNs))) break;
+            tc_fence_after();
+            const uint32_t st = smem_u32(buf + s * stage_bytes);
+            const uint64_t da = smem_desc_sw128(st, 16, 1024), db = smem_desc_sw128(st + w_bytes, 16, 1024);
+            const uint32_t idesc = p.idesc | idesc_scale_step(i % kWordStages);
+#pragma unroll
+            for (int kk = 0; kk < 4; ++kk)
+              mma_ss_mx_pair(tmem + b * kAccStride<OutType>, da + 2 * kk, db + 2 * kk, idesc, scales, scales + 4, i > i0 || kk > 0);
+            mma_commit_pair(&sm.empty[s]);
+          }
+          if (ok) mma_commit_pair(&sm.acc_full[b]);
+        }
+      }
+    }
+  } else if (warp == kEpiWarps + 2) {
+    // ================= scales: of this CTA's features and of all the tile's tokens =================
+    RingPos sf;
+    int issued = 0;
+    bool ok = true;
+    for (long long t = pair; ok && t < p.tiles; t += pairs) {
+      int ft, tt;
+      tile_of(p, t, &ft, &tt);
+      const int n0 = (2 * ft + (int)rank) * kTileF, m0 = tt * p.tile_t, m_end = min(p.rows, m0 + p.tile_t);
+      for (int w = 0; w < words; ++w, sf.next(kScaleSlots)) {
+        if (!(ok = __all_sync(0xffffffffu, wait_for(&sm.sf_empty[sf.stage], sf.phase ^ 1, p.status, kWaitLimitNs)))) break;
+        issued = min(issued + 1, kScaleSlots);
+        uint4* to = reinterpret_cast<uint4*>(slots + sf.stage * kPairSlotBytes);
+        stage_scales<1>(to, p.w_scale, p.ld_ws, p.w_shift, n0, min(p.cols, n0 + kTileF), w, p.k_iters);
+        stage_scales<2>(to + 32, p.x_scale, p.ld_xs, 0, m0, m_end, w, p.k_iters);
+        fence_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive_cluster(map_to_rank(smem_u32(&sm.sf_full[sf.stage]), 0));
+      }
+    }
+    // every word is copied before the CTA may leave
+    for (; ok && issued > 0; --issued) {
+      sf.back(kScaleSlots);
+      ok = __all_sync(0xffffffffu, wait_for(&sm.sf_empty[sf.stage], sf.phase, p.status, kWaitLimitNs));
+    }
+  } else {
+    // ================= epilogue: warps w and w + 4 share 32 features and take 32-token column blocks in turn ==========
+    const int quad = warp % 4, half = warp / 4;
+    const uint32_t lanes = tmem + ((uint32_t)(quad * 32) << 16);
+    const uint32_t empty = map_to_rank(smem_u32(sm.acc_empty), 0);
+    RingPos r;
+    bool ok = true;
+    int turn = 0;
+    for (long long t = pair; ok && t < p.tiles; t += pairs) {
+      int ft, tt;
+      tile_of(p, t, &ft, &tt);
+      const int n = (2 * ft + (int)rank) * kTileF + quad * 32 + lane;
+      const int m0 = tt * p.tile_t, m_end = min(p.rows, m0 + p.tile_t);
+      const float bias = p.bias && n < p.cols ? p.bias[n] : 0.f;
+      // this warp's columns: blocks of 32 from 32 half on, 64 apart, handled as two halves of 16
+      const TileGate gate = tile_gate(p, n, m0, m_end);
+      T ahead0[16], ahead1[16];
+      if (!kOut8) {
+        load_residual16<OutType>(p, ahead0, n, m0 + half * 32, m_end);
+        load_residual16<OutType>(p, ahead1, n, m0 + half * 32 + 16, m_end);
+      }
+      auto release = [&](int stage) {
+        if (lane == 0) mbar_arrive_cluster(empty + 8 * stage);
+      };
+      const bool summed = kChunked && chunks > 1;
+      if (summed)
+        ok = add_chunks<kAccs<OutType>, (kMaxTileChunked + 31) / 32>(
+            chunks, lanes, kAccStride<OutType>, kAccs<OutType> * kAccStride<OutType>,
+            [&](int i) { return (i / 2 * 2 + half) * 32 + (i & 1) * 16; }, m_end - m0, r, sm.acc_full, p.status, release);
+      else
+        ok = __all_sync(0xffffffffu, wait_for(&sm.acc_full[r.stage], r.phase, p.status, kWaitLimitNs));
+      if (!ok) break;
+      tc_fence_after();
+      const uint32_t sums = lanes + (summed ? kAccs<OutType> : r.stage) * kAccStride<OutType>;
+#pragma unroll 1
+      for (int col = half * 32; m0 + col < m_end; col += 64) {
+        float acc0[16], acc1[16];
+        tmem_ld16(sums + col, reinterpret_cast<uint32_t(&)[16]>(acc0));
+        tmem_ld16(sums + col + 16, reinterpret_cast<uint32_t(&)[16]>(acc1));
+        tmem_wait_ld();
+        if constexpr (kOut8) {
+          if (n < p.cols) gated16(p, acc0, n, m0 + col, min(16, m_end - m0 - col), bias, gate);
+          if (!(ok = quantise16(p, sm.exchange[half], turn, acc0, n, quad, m0 + col, m_end))) break;
+          if (m0 + col + 16 < m_end) {
+            if (n < p.cols) gated16(p, acc1, n, m0 + col + 16, min(16, m_end - m0 - col - 16), bias, gate);
+            if (!(ok = quantise16(p, sm.exchange[half], turn, acc1, n, quad, m0 + col + 16, m_end))) break;
+          }
+        } else {
+          epilogue16<OutType>(p, acc0, ahead0, n, m0 + col, m_end, bias, gate);
+          load_residual16<OutType>(p, ahead0, n, m0 + col + 64, m_end);
+          epilogue16<OutType>(p, acc1, ahead1, n, m0 + col + 16, m_end, bias, gate);
+          load_residual16<OutType>(p, ahead1, n, m0 + col + 80, m_end);
+        }
+      }
+      if (!ok) break;
+      if (!summed) {
+        tc_fence_before();
+        __syncwarp();
+        release(r.stage);
+        r.next(kAccs<OutType>);
+      }
+    }
+  }
+  __syncwarp();
+  tc_fence_before();
+  __syncthreads();
+  cluster_arrive();
+  cluster_wait();                                    // neither CTA leaves while the other may still reach into it
+  tc_fence_after();
+  if (warp == 0) tmem_dealloc_pair(tmem, 512);
+}
+
+// ---- host side -------------------------------------------------------------------------------
+
+// Matrix of codes [rows, inner] with a row stride, as (inner, row): box = 128 elements x box_rows, 128-byte swizzle; what lies
+// past either end reads as zero.
+int make_map(CUtensorMap* m, const void* base, int inner, int rows, int64_t ld, int box_rows) {
+  const sdvg::EncodeTiledFn fn = sdvg::encode_tiled_fn();
+  if (!fn) return SDVG_ERR_CUDA;
+  if (rows == 1) ld = ((int64_t)inner + 15) / 16 * 16;           // not read, but the map wants a legal one
+  cuuint64_t dims[2] = {(cuuint64_t)inner, (cuuint64_t)rows};
+  cuuint64_t strides[1] = {(cuuint64_t)ld};
+  cuuint32_t box[2] = {(cuuint32_t)kTileK, (cuuint32_t)box_rows};
+  cuuint32_t estr[2] = {1, 1};
+  const CUresult r = fn(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), dims, strides, box, estr,
+                        CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                        CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? SDVG_OK : SDVG_ERR_CUDA;
+}
+
+std::mutex g_setup_mu;
+
+constexpr int kPairRows = kMaxTileFew;               // more tokens than this go to the pairs
+
+constexpr int kTileStages = 4;
+constexpr int tile_dynamic(int tile_t) { return kTileStages * (kTileF + tile_t) * 128 + kScaleSlots * kTileSlotBytes + 1024; }
+
+// As in linear.cu: no tile takes a larger share of an SM's tensor memory columns than of its shared memory, so that a CTA that an
+// SM can hold finds its columns at once, and clusters never wait for each other's.
+constexpr bool columns_within_share(int tile_t) {
+  return tile_tmem_cols(tile_t) * (228 * 1024 / 512) <= (uint32_t)tile_dynamic(tile_t);
+}
+static_assert(columns_within_share(16) && columns_within_share(32) && columns_within_share(48) && columns_within_share(64));
+static_assert(kMaxTileFew == 64, "the sizes checked above");
+
+// CTAs per tile: as many as it takes to give every SM work, while all of them run at once and each keeps four stages of the sum,
+// or eight where the SMs have more than one CTA then.
+int tile_split(long long tiles, int k_iters, int tile_t, int sms) {
+  const int per_sm = 228 * 1024 / (tile_dynamic(tile_t) + 2 * 1024);
+  int split = 1;
+  while (split < kMaxSplit && tiles * split < sms && tiles * 2 * split <= (long long)sms * per_sm &&
+         k_iters >= (tiles * 2 * split <= sms ? 8 : 16) * split)
+    split *= 2;
+  return split;
+}
+
+// One-time set-up per device and output type: the opt-in to the kernels' dynamic shared memory, and how many CTA pairs
+// the device runs at once.
+template <int OutType>
+int set_up(int* pairs) {
+  static int pairs_of_device[kMaxDevices] = {};
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return sdvg::cuda_status(e);
+  if (dev < 0 || dev >= kMaxDevices) return SDVG_ERR_INVALID_ARG;
+  std::lock_guard<std::mutex> lock(g_setup_mu);
+  if (!pairs_of_device[dev]) {
+    e = cudaFuncSetAttribute(linear8_tile_kernel<OutType>, cudaFuncAttributeMaxDynamicSharedMemorySize, tile_dynamic(kMaxTileFew));
+    if (e != cudaSuccess) return sdvg::cuda_status(e);
+    e = cudaFuncSetAttribute(linear8_pair_kernel<OutType>, cudaFuncAttributeMaxDynamicSharedMemorySize, kPairSmem);
+    if (e != cudaSuccess) return sdvg::cuda_status(e);
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(2);
+    cfg.blockDim = dim3(kPairThreads);
+    cfg.dynamicSmemBytes = kPairSmem;
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = 2;
+    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    int n = 0;
+    e = cudaOccupancyMaxActiveClusters(&n, linear8_pair_kernel<OutType>, &cfg);
+    if (e != cudaSuccess || n < 1) return sdvg::cuda_status(e != cudaSuccess ? e : cudaErrorUnknown);
+    pairs_of_device[dev] = n;
+  }
+  *pairs = pairs_of_device[dev];
+  return SDVG_OK;
+}
+
+template <int OutType>
+int launch(Linear8Params& p, const void* x, int64_t ld_x, const void* w, int64_t ld_w, int inner, cudaStream_t stream) {
+  int pairs = 0;
+  int st = set_up<OutType>(&pairs);
+  if (st != SDVG_OK) return st;
+  const bool by_pair = p.rows > kPairRows;
+  const int feature_tile = by_pair ? 2 * kTileF : kTileF;
+  p.tiles_f = (p.cols + feature_tile - 1) / feature_tile;
+  if (by_pair) p.tile_t = pair_tile(p.rows, p.tiles_f, pairs, OutType == SDVG_F32 ? kMaxTileChunked : kMaxTileT);
+  else p.tile_t = (std::min(p.rows, kMaxTileFew) + 15) / 16 * 16;
+  p.tiles_t = (p.rows + p.tile_t - 1) / p.tile_t;
+  p.tiles = (long long)p.tiles_f * p.tiles_t;
+  if (p.tiles >= 1ll << 28) return SDVG_ERR_BAD_SHAPE;
+  p.idesc = idesc_mx_e4m3(feature_tile, p.tile_t);
+  if ((st = make_map(&p.w_map, w, inner, p.cols, ld_w, kTileF)) != SDVG_OK) return st;
+  if ((st = make_map(&p.x_map, x, inner, p.rows, ld_x, by_pair ? p.tile_t / 2 : p.tile_t)) != SDVG_OK) return st;
+  if (by_pair) {
+    p.group = 8;
+    p.stages = std::min(kMaxStages, (kPairSmem - 1024 - kScaleSlots * kPairSlotBytes) / (kTileF * 128 + p.tile_t * 64));
+    const int grid = 2 * (int)std::min((long long)pairs, p.tiles);
+    return sdvg::cuda_status(
+        sdvg::launch_overlapped(linear8_pair_kernel<OutType>, grid, kPairThreads, kPairSmem, 0, stream, p));
+  }
+  p.split = tile_split(p.tiles, p.k_iters, p.tile_t, 2 * pairs);
+  p.stages = kTileStages;
+  return sdvg::cuda_status(sdvg::launch_overlapped(linear8_tile_kernel<OutType>, (unsigned)p.tiles * p.split, kTileThreads,
+                                                   tile_dynamic(p.tile_t), p.split > 1 ? p.split : 0, stream, p));
+}
+
+bool aligned_to(const void* p, int bytes) { return (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(bytes - 1)) == 0; }
+
+}  // namespace
+
+extern "C" {
+
+int sdvg_linear_e4m3(const void* x8, int64_t ld_x, const void* x_scale, int64_t ld_x_scale, const void* w8, int64_t ld_w,
+                     const void* w_scale, int64_t ld_w_scale, int w_scale_rows, const float* bias, int act, const float* gate,
+                     int64_t ld_gate, int gate_rows, const void* residual, int64_t ld_residual, void* out, int64_t ld_out,
+                     void* out_scale, int64_t ld_out_scale, int rows, int cols, int inner, int out_type, void* workspace,
+                     size_t workspace_bytes, void* stream) {
+  SDVG_RANGE();
+  constexpr int kMaxExtent = 0x7fffffff - 1024;                  // a tile's end past the matrix's is still an int
+  constexpr int kMaxInner = 1 << 26;                             // one sum stays far below the limit of a wait
+  if (rows < 0 || cols < 0 || inner < 1 || rows > kMaxExtent || cols > kMaxExtent || inner > kMaxInner)
+    return SDVG_ERR_BAD_SHAPE;
+  const bool out8 = out_type == SDVG_E4M3;
+  if (!out8 && !sdvg::elem_type_ok(out_type)) return SDVG_ERR_INVALID_ARG;
+  if (act < SDVG_ACT_NONE || act > SDVG_ACT_GELU || (gate && gate_rows < 1)) return SDVG_ERR_INVALID_ARG;
+  if (w_scale_rows != 1 && w_scale_rows != 128) return SDVG_ERR_INVALID_ARG;
+  if (out8 ? residual != nullptr : out_scale != nullptr) return SDVG_ERR_INVALID_ARG;
+  if (rows == 0 || cols == 0) return SDVG_OK;
+  if (!x8 || !x_scale || !w8 || !w_scale || !out || (out8 && !out_scale) || !workspace ||
+      workspace_bytes < (size_t)kWorkspaceBytes)
+    return SDVG_ERR_INVALID_ARG;
+  const int blocks = (inner + 127) / 128, out_blocks = (cols + 127) / 128;
+  const bool w_scales = cols > w_scale_rows;                     // more than one row of them
+  if ((rows > 1 && (ld_x < inner || ld_out < cols || ld_x_scale < blocks)) || (cols > 1 && ld_w < inner) ||
+      (w_scales && ld_w_scale < blocks) || (out8 && rows > 1 && ld_out_scale < out_blocks))
+    return SDVG_ERR_BAD_SHAPE;
+  if (residual && rows > 1 && ld_residual != 0 && ld_residual < cols) return SDVG_ERR_BAD_SHAPE;
+  if (gate && rows > gate_rows && ld_gate < cols) return SDVG_ERR_BAD_SHAPE;
+  // the tensor map's stride is a 40-bit byte count
+  if ((rows > 1 && ld_x >= (int64_t)1 << 40) || (cols > 1 && ld_w >= (int64_t)1 << 40)) return SDVG_ERR_BAD_SHAPE;
+  if (!sdvg::aligned16(x8) || !sdvg::aligned16(w8) || (rows > 1 && (ld_x & 15)) || (cols > 1 && (ld_w & 15)) ||
+      !aligned_to(x_scale, 4) || !aligned_to(w_scale, 4) || (rows > 1 && (ld_x_scale & 3)) || (w_scales && (ld_w_scale & 3)))
+    return SDVG_ERR_MISALIGNED;
+  const int out_bytes = out8 ? 1 : sdvg::elem_bytes(out_type);
+  if (!aligned_to(out, out_bytes) || !aligned_to(residual, out_bytes) || !aligned_to(bias, 4) || !aligned_to(gate, 4) ||
+      !aligned_to(workspace, 256))
+    return SDVG_ERR_MISALIGNED;
+  int st = sdvg::require_sm100();
+  if (st != SDVG_OK) return st;
+  Linear8Params p = {};
+  p.out = out;
+  p.residual = residual;
+  p.bias = bias;
+  p.gate = gate;
+  p.ld_out = ld_out;
+  p.ld_res = ld_residual;
+  p.ld_gate = ld_gate;
+  p.gate_rows = gate_rows;
+  p.rows = rows;
+  p.cols = cols;
+  p.act = act;
+  p.x_scale = (const uint8_t*)x_scale;
+  p.w_scale = (const uint8_t*)w_scale;
+  p.ld_xs = ld_x_scale;
+  p.ld_ws = ld_w_scale;
+  p.w_shift = w_scale_rows == 128 ? 7 : 0;
+  p.out_scale = (uint8_t*)out_scale;
+  p.ld_os = ld_out_scale;
+  p.k_iters = blocks;
+  p.status = (unsigned int*)workspace + 1;
+  const cudaStream_t s = (cudaStream_t)stream;
+  if (out8) return launch<SDVG_E4M3>(p, x8, ld_x, w8, ld_w, inner, s);
+  if (out_type == SDVG_F32) return launch<SDVG_F32>(p, x8, ld_x, w8, ld_w, inner, s);
+  if (out_type == SDVG_F16) return launch<SDVG_F16>(p, x8, ld_x, w8, ld_w, inner, s);
+  return launch<SDVG_BF16>(p, x8, ld_x, w8, ld_w, inner, s);
+}
+
+}  // extern "C"

@@ -285,6 +285,42 @@ __device__ __forceinline__ void tma_load_2d_pair(void* smem_dst, const CUtensorM
       : "memory");
 }
 
+// ---- 8-bit products with a power-of-two scale per row and 128-byte step -------------------
+// Scale factors of a product in tensor memory: one column holds 32 rows (one per lane, the same in every quarter of the lanes),
+// and a row's 32-bit word holds the exponent bytes (2^(byte - 127)) of four steps, of which an instruction takes the one that
+// its descriptor names.  This copies 512 bytes of shared memory, [32 lanes][4 columns] words, to all four quarters; it runs in
+// order with the products issued by the same thread.
+__device__ __forceinline__ uint64_t smem_desc_scales(uint32_t smem_addr) {
+  return (uint64_t)((smem_addr & 0x3ffff) >> 4) | (uint64_t)(128 >> 4) << 32 | (uint64_t)1 << 46;   // 8-row groups of 128 bytes, no swizzle
+}
+__device__ __forceinline__ void tmem_cp_scales(uint32_t taddr, uint32_t smem_addr) {
+  asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(smem_desc_scales(smem_addr)) : "memory");
+}
+// In both CTAs of a pair, each from its own shared memory.
+__device__ __forceinline__ void tmem_cp_scales_pair(uint32_t taddr, uint32_t smem_addr) {
+  asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(smem_desc_scales(smem_addr)) : "memory");
+}
+__device__ __forceinline__ void mma_ss_mx(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t a_scales,
+                                          uint32_t b_scales, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %6, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::"r"(d_tmem),
+      "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(a_scales), "r"(b_scales), "r"(accumulate)
+      : "memory");
+}
+__device__ __forceinline__ void mma_ss_mx_pair(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc,
+                                               uint32_t a_scales, uint32_t b_scales, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %6, 0;\n\t"
+      "tcgen05.mma.cta_group::2.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::"r"(d_tmem),
+      "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(a_scales), "r"(b_scales), "r"(accumulate)
+      : "memory");
+}
+// Shared-memory writes of this thread before it are seen by asynchronous reads (copies, products) ordered after it.
+__device__ __forceinline__ void fence_async_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+
 // ---- descriptors ---------------------------------------------------------
 // Shared-memory matrix descriptor, 128-byte swizzle, tile base 1024-byte aligned.
 //   K-major operand  (rows = M or N, 128 B of K per row: 64 bf16 or 128 bytes): 8-row groups `sbo` bytes apart.
@@ -327,6 +363,15 @@ __host__ __device__ constexpr uint32_t idesc_e4m3_f32(int m, int n, bool b_mn_ma
          | ((uint32_t)(m >> 4) << 24);
 }
 
+// Instruction descriptor of the scaled form: E4M3 x E4M3 -> fp32 with exponent-byte scales, both operands K-major.  scale_step
+// (0 .. 3): which byte of the scale words the instruction takes, for both operands.
+__host__ __device__ constexpr uint32_t idesc_mx_e4m3(int m, int n) {
+  return (uint32_t)(n >> 3) << 17
+         | 1u << 23                      // scales are exponent bytes
+         | (uint32_t)(m >> 4) << 24;
+}
+__host__ __device__ constexpr uint32_t idesc_scale_step(uint32_t scale_step) { return scale_step << 4 | scale_step << 29; }
+
 // Four floats -> four E4M3 bytes (round to nearest even, saturating at +-448), a in the lowest byte.
 __device__ __forceinline__ uint32_t pack_e4m3x4(float a, float b, float c, float d) {
   uint32_t r;
@@ -337,6 +382,20 @@ __device__ __forceinline__ uint32_t pack_e4m3x4(float a, float b, float c, float
       : "=r"(r)
       : "f"(a), "f"(b), "f"(c), "f"(d));
   return r;
+}
+
+// Two E4M3 bytes -> two floats, exactly; the lower byte first.
+__device__ __forceinline__ float2 unpack_e4m3x2(uint16_t codes) {
+  uint32_t h;                                          // every E4M3 value is a half
+  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"(codes));
+  float2 f;
+  asm("{\n\t.reg .b16 lo, hi;\n\t"
+      "mov.b32 {lo, hi}, %2;\n\t"
+      "cvt.f32.f16 %0, lo;\n\t"
+      "cvt.f32.f16 %1, hi;\n\t}"
+      : "=f"(f.x), "=f"(f.y)
+      : "r"(h));
+  return f;
 }
 
 }  // namespace sm100

@@ -1,0 +1,149 @@
+"""Host-side checks of the 8-bit dense operators' C entry points, and pins of their fp64 definitions; no GPU."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import e4m3_blocks_oracle as B
+from oracle import sdvg_oracle as O
+from paper_2604_17397_b200 import api, build
+from test_dense_cpu import OnPaper, without_address
+
+X, XS, W, WS, B_, G, R, OUT, OS, SPACE = (0x10000 * i for i in range(1, 11))
+
+
+@pytest.fixture(scope="module")
+def lib():
+    build.build()
+    return api.lib()
+
+
+def linear_args(**change):
+    a = dict(x=X, ld_x=64, xs=XS, ld_xs=4, w=W, ld_w=64, ws=WS, ld_ws=4, w_rows=128, bias=B_, act=0, gate=None, ld_gate=0, gate_rows=0,
+             residual=None, ld_residual=0, out=OUT, ld_out=32, os=None, ld_os=0, rows=4, cols=32, inner=64, out_type=0, space=SPACE,
+             space_bytes=256, stream=None)
+    assert set(change) <= set(a)
+    return list({**a, **change}.values())
+
+
+OUT8 = dict(out_type=3, os=OS, ld_os=1)
+
+
+@pytest.mark.parametrize("change,status", [
+    (dict(rows=-1), "BAD_SHAPE"), (dict(cols=-1), "BAD_SHAPE"), (dict(inner=0), "BAD_SHAPE"), (dict(rows=0x7fffffff), "BAD_SHAPE"),
+    (dict(inner=(1 << 26) + 1, ld_x=1 << 27, ld_w=1 << 27), "BAD_SHAPE"), (dict(ld_x=48), "BAD_SHAPE"), (dict(ld_w=48), "BAD_SHAPE"),
+    (dict(ld_out=31), "BAD_SHAPE"), (dict(ld_xs=0), "BAD_SHAPE"), (dict(cols=129, ld_out=129, ld_ws=0), "BAD_SHAPE"),
+    (dict(w_rows=1, ld_ws=0), "BAD_SHAPE"), (dict(inner=513, ld_x=528, ld_w=528), "BAD_SHAPE"),
+    (dict(residual=R, ld_residual=31), "BAD_SHAPE"), (dict(gate=G, gate_rows=2, ld_gate=31), "BAD_SHAPE"),
+    (dict(ld_x=1 << 40), "BAD_SHAPE"), (dict(**{**OUT8, "ld_os": 0}), "BAD_SHAPE"),
+    (dict(out_type=4), "INVALID_ARG"), (dict(out_type=-1), "INVALID_ARG"), (dict(act=4), "INVALID_ARG"), (dict(w_rows=64), "INVALID_ARG"),
+    (dict(w_rows=0), "INVALID_ARG"), (dict(gate=G, gate_rows=0, ld_gate=32), "INVALID_ARG"), (dict(out_type=3), "INVALID_ARG"),
+    (dict(os=OS, ld_os=1), "INVALID_ARG"), (dict(residual=R, ld_residual=32, **OUT8), "INVALID_ARG"),
+    (dict(x=None), "INVALID_ARG"), (dict(xs=None), "INVALID_ARG"), (dict(w=None), "INVALID_ARG"), (dict(ws=None), "INVALID_ARG"),
+    (dict(out=None), "INVALID_ARG"), (dict(space=None), "INVALID_ARG"), (dict(space_bytes=255), "INVALID_ARG"),
+    (dict(x=X + 8), "MISALIGNED"), (dict(w=W + 4), "MISALIGNED"), (dict(ld_x=72), "MISALIGNED"), (dict(ld_w=65), "MISALIGNED"),
+    (dict(xs=XS + 2), "MISALIGNED"), (dict(ws=WS + 1), "MISALIGNED"), (dict(ld_xs=5), "MISALIGNED"),
+    (dict(cols=129, ld_out=129, ld_ws=6), "MISALIGNED"), (dict(out=OUT + 1), "MISALIGNED"), (dict(out=OUT + 2, out_type=2), "MISALIGNED"),
+    (dict(bias=B_ + 2), "MISALIGNED"), (dict(gate=G + 1, gate_rows=4), "MISALIGNED"), (dict(space=SPACE + 16), "MISALIGNED"),
+])
+def test_linear_refuses_on_the_host(lib, change, status):
+    assert lib.sdvg_linear_e4m3(*linear_args(**change)) == getattr(api, "SDVG_ERR_" + status)
+
+
+def test_strides_of_single_rows_are_not_looked_at(lib):
+    one = dict(rows=1, cols=1, ld_x=0, ld_xs=0, ld_w=0, ld_ws=0, ld_out=0, space=SPACE + 16)
+    assert lib.sdvg_linear_e4m3(*linear_args(**one)) == api.SDVG_ERR_MISALIGNED          # the workspace, checked last
+    assert lib.sdvg_linear_e4m3(*linear_args(**{**one, **OUT8, "ld_os": 0, "out": OUT + 1})) == api.SDVG_ERR_MISALIGNED
+
+
+def test_nothing_to_do(lib):
+    assert lib.sdvg_linear_e4m3(*linear_args(rows=0, x=None, out=None)) == api.SDVG_OK
+    assert lib.sdvg_linear_e4m3(*linear_args(cols=0, w=None)) == api.SDVG_OK
+    assert lib.sdvg_quant_e4m3_blocks(None, 0, 0, None, 0, None, 0, 1, 0, 8, None) == api.SDVG_OK
+    assert lib.sdvg_dequant_e4m3_blocks(None, 0, None, 0, 128, None, 0, 2, 8, 0, None) == api.SDVG_OK
+
+
+@pytest.mark.parametrize("change,status", [
+    (dict(rows=-1), "BAD_SHAPE"), (dict(cols=-1), "BAD_SHAPE"), (dict(rows=0x7fffffff), "BAD_SHAPE"), (dict(ld_x=199), "BAD_SHAPE"),
+    (dict(ld_8=199), "BAD_SHAPE"), (dict(ld_s=1), "BAD_SHAPE"), (dict(rows=2 ** 31 - 1025, cols=2 ** 20, ld_x=2 ** 20, ld_8=2 ** 20,
+                                                                      ld_s=2 ** 20), "BAD_SHAPE"),
+    (dict(type=3), "INVALID_ARG"), (dict(type=-1), "INVALID_ARG"), (dict(block=2), "INVALID_ARG"), (dict(block=0), "INVALID_ARG"),
+    (dict(x=None), "INVALID_ARG"), (dict(x8=None), "INVALID_ARG"), (dict(scale=None), "INVALID_ARG"),
+    (dict(x=X + 1), "MISALIGNED"), (dict(type=2, x=X + 2), "MISALIGNED"),
+])
+def test_quantisation_refuses_on_the_host(lib, change, status):
+    a = dict(x=X, ld_x=200, type=0, x8=OUT, ld_8=200, scale=OS, ld_s=2, block=1, rows=300, cols=200)
+    assert set(change) <= set(a)
+    x, ld_x, t, x8, ld_8, s, ld_s, block, rows, cols = {**a, **change}.values()
+    want = getattr(api, "SDVG_ERR_" + status)
+    assert lib.sdvg_quant_e4m3_blocks(x, ld_x, t, x8, ld_8, s, ld_s, block, rows, cols, None) == want
+    assert lib.sdvg_dequant_e4m3_blocks(x8, ld_8, s, ld_s, block, x, ld_x, t, rows, cols, None) == want
+
+
+def u8(*shape):
+    return OnPaper(*shape, dtype=torch.uint8)
+
+
+def linear_on_paper(**change):
+    a = dict(x=u8(4, 300), xs=u8(4, 3), w=u8(200, 300), ws=u8(2, 3), out=OnPaper(4, 200), space=u8(256), bias=None, act=0, residual=None,
+             gate=None, gate_rows=0, out_scale=None, stream=0)
+    assert set(change) <= set(a)
+    return api._binding().linear_e4m3(*{**a, **change}.values())
+
+
+def test_the_binding_reads_and_refuses(lib):
+    reached = api.SDVG_ERR_INVALID_ARG                          # the library, which refuses the null addresses
+    assert linear_on_paper() == linear_on_paper(ws=u8(200, 3)) == reached
+    assert linear_on_paper(out=u8(4, 200), out_scale=u8(4, 2)) == reached
+    for change in (dict(xs=u8(4, 2)), dict(xs=u8(3, 3)), dict(ws=u8(3, 3)), dict(ws=u8(2, 4)), dict(ws=u8(6)), dict(x=OnPaper(4, 300)),
+                   dict(w=u8(200, 299)), dict(out=u8(4, 200)), dict(out_scale=u8(4, 2)), dict(out=u8(4, 200), out_scale=u8(4, 3)),
+                   dict(out=u8(4, 199), out_scale=u8(4, 2)), dict(xs=OnPaper(4, 3)), dict(out=OnPaper(4, 201)),
+                   dict(residual=OnPaper(4, 200, dtype=torch.float32)), dict(gate=OnPaper(2, 200, dtype=torch.float32), gate_rows=1),
+                   dict(bias=OnPaper(199, dtype=torch.float32)), dict(x=u8(300))):
+        with pytest.raises(ValueError):
+            linear_on_paper(**change)
+    for change in (dict(ws=without_address(2, 3, dtype=torch.uint8)), dict(space=without_address(256, dtype=torch.uint8))):
+        with pytest.raises(RuntimeError):
+            linear_on_paper(**change)
+    blocks = api._binding().e4m3_blocks
+    for way in (0, 1):
+        assert blocks(OnPaper(200, 300), u8(200, 300), u8(200, 3), way, 0) == reached
+        assert blocks(OnPaper(200, 300, dtype=torch.float32), u8(200, 300), u8(2, 3), way, 0) == reached
+        for bad in ((u8(200, 300), u8(200, 300), u8(2, 3)), (OnPaper(200, 300), u8(200, 299), u8(2, 3)),
+                    (OnPaper(200, 300), u8(200, 300), u8(3, 3)), (OnPaper(200), u8(200), u8(2)),
+                    (torch.zeros(2, 3), torch.zeros(2, 3, dtype=torch.uint8), torch.zeros(1, 1, dtype=torch.uint8))):
+            with pytest.raises(ValueError):
+                blocks(*bad, way, 0)
+    with pytest.raises(TypeError):
+        blocks()
+
+
+# ---- the definitions ------------------------------------------------------------------------------------
+
+def test_scales_are_the_smallest_that_hold_their_block():
+    rng = np.random.default_rng(0)
+    x = rng.standard_normal((200, 300)) * 2.0 ** rng.integers(-30, 30, (200, 1))
+    for block_rows in (1, 128):
+        codes, s = B.quantise(x, block_rows)
+        f = B.of_elements(s, *x.shape, block_rows)
+        assert (np.abs(x) <= 448 * f).all()
+        top = np.array([[np.abs(x[i * block_rows:(i + 1) * block_rows, j * 128:(j + 1) * 128]).max() for j in range(3)]
+                        for i in range(s.shape[0])])
+        assert (top > 224 * 2.0 ** (s.astype(float) - 127)).all()
+        assert (np.abs(B.values(codes, s, block_rows) - x) <= B.half_step(np.abs(x), f)).all()
+
+
+def test_codes_and_scale_bytes_are_torchs_types():
+    x = np.random.default_rng(1).standard_normal((5, 256))
+    codes, s = B.quantise(x, 1)
+    t = torch.from_numpy(codes).view(torch.float8_e4m3fn).double()
+    f = torch.from_numpy(s).view(torch.float8_e8m0fnu).double().repeat_interleave(128, 1)
+    assert np.array_equal((t * f).numpy(), B.values(codes, s, 1))
+    assert torch.equal((torch.from_numpy(x) / f).float().to(torch.float8_e4m3fn).view(torch.uint8), torch.from_numpy(codes))
+
+
+def test_special_values():
+    x = np.zeros((1, 384))
+    x[0, 0], x[0, 128], x[0, 129] = np.nan, np.inf, 3.0
+    codes, s = B.quantise(x, 1)
+    assert s.tolist() == [[1, 247, 1]] and codes[0, 0] == 0x7F and codes[0, 128] == 0x7E and codes[0, 129] == 0
+    assert O.e4m3_tile_scale_exponent(0.0) == -126

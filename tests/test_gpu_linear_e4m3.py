@@ -1,0 +1,269 @@
+"""sdvg_linear_e4m3 and the quantisation of its operands against fp64."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from dense_utils import DTYPES, assert_close, f64, linear_tolerance
+from oracle import dense_oracle as D
+from oracle import e4m3_blocks_oracle as B
+from paper_2604_17397_b200 import api
+
+pytestmark = pytest.mark.gpu
+
+ACTS = {"none": api.SDVG_ACT_NONE, "silu": api.SDVG_ACT_SILU, "gelu_tanh": api.SDVG_ACT_GELU_TANH, "gelu": api.SDVG_ACT_GELU}
+OUTS = {**DTYPES, "e4m3": torch.uint8}
+
+
+def randn(gen, *shape, std=1.0):
+    return torch.randn(shape, generator=gen, device="cuda") * std
+
+
+def coded(x, block_rows, pad=16, more=0, fill=0x7F):
+    """E4M3 codes and scales of x as the oracle quantises them; what lies between the rows is NaN."""
+    codes, scale = B.quantise(f64(x), block_rows)
+    got = []
+    for a, p in ((codes, 16), (scale, 4)):
+        ld = -(-a.shape[1] // p) * p + more * p
+        buf = torch.full((a.shape[0], ld), fill if p == 16 else 255, device="cuda", dtype=torch.uint8)
+        buf[:, :a.shape[1]] = torch.from_numpy(a).cuda()
+        got.append(buf[:, :a.shape[1]])
+    return got
+
+
+def problem(rows, cols, inner, out="bf16", act="none", bias=True, gate_rows=0, residual="", seed=0, w_rows=128, spread=6.0, more=0):
+    """spread: blocks differ in magnitude by up to 2^spread."""
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    sized = lambda n: torch.exp2(spread * torch.rand((n, -(-inner // 128)), generator=gen, device="cuda") - spread / 2
+                                 ).repeat_interleave(128, 1)[:, :inner]
+    x = randn(gen, rows, inner) * sized(rows)
+    w = randn(gen, cols, inner, std=1 / math.sqrt(inner)) * sized(-(-cols // 128)).repeat_interleave(128, 0)[:cols]
+    s = dict(x=coded(x, 1, more=more), w=coded(w, w_rows, more=more), act=act, gate_rows=gate_rows, out=out, w_rows=w_rows)
+    s["bias"] = randn(gen, cols) if bias else None
+    s["gate"] = randn(gen, -(-rows // gate_rows), cols) if gate_rows else None
+    s["residual"] = None
+    if residual:
+        s["residual"] = randn(gen, rows if residual == "rows" else 1, cols, std=2.0).to(OUTS[out]).expand(rows, cols)
+    return s
+
+
+def call(s, out, ws, out_scale=None, stream=None):
+    api.sdvg_linear_e4m3(*s["x"], *s["w"], out, ws, bias=s["bias"], act=ACTS[s["act"]], residual=s["residual"], gate=s["gate"],
+                         gate_rows=s["gate_rows"], out_scale=out_scale, stream=stream)
+
+
+def expected(s, dtype):
+    """(reference, bound) of the result rounded to dtype."""
+    x, w = (B.values(c.cpu().numpy(), e.cpu().numpy(), n) for (c, e), n in ((s["x"], 1), (s["w"], s["w_rows"])))
+    b, g, r = (f64(s[k]) for k in ("bias", "gate", "residual"))
+    ref = D.linear_ref(x, w, b, s["act"], g, s["gate_rows"], r)
+    per_row = None if g is None else D.of_rows(g, x.shape[0], s["gate_rows"])
+    return ref, linear_tolerance(x, w, b, s["act"], per_row, r, ref, dtype)
+
+
+def check_quantised(codes, scale, ref, err):
+    """Rows of codes of values known up to err: the scale is that of some value within it, the codes are within half a step."""
+    e = scale.cpu().numpy().astype(np.int64)
+    lo, hi = (B.scale_bytes(np.maximum(np.abs(ref) + d, 0), 1).astype(np.int64) for d in (-err, err))
+    assert ((lo <= e) & (e <= hi)).all()
+    f = B.of_elements(scale.cpu().numpy(), *ref.shape, 1)
+    tol = err + B.half_step(np.abs(ref) + err, f)
+    assert_close(B.values(codes.cpu().numpy(), scale.cpu().numpy(), 1), ref, tol, "codes")
+
+
+def check(s, ld_out=None, in_place=False):
+    ws = api.attn_workspace()
+    rows, cols = s["x"][0].shape[0], s["w"][0].shape[0]
+    dtype = OUTS[s["out"]]
+    buf = torch.full((rows + 2, ld_out or cols), 77, device="cuda", dtype=dtype)         # a row before, a row after
+    out = buf[1:rows + 1, :cols]
+    if s["out"] == "e4m3":
+        blocks = -(-cols // 128)
+        sbuf = torch.full((rows + 2, blocks + 1), 33, device="cuda", dtype=torch.uint8)
+        call(s, out, ws, sbuf[1:rows + 1, :blocks])
+        assert api.sdvg_block_attn_status(ws) == api.SDVG_OK
+        check_quantised(out, sbuf[1:rows + 1, :blocks], *expected(s, torch.float32))
+        assert bool((sbuf[0] == 33).all()) and bool((sbuf[-1] == 33).all()) and bool((sbuf[:, blocks:] == 33).all())
+    else:
+        ref, tol = expected(s, dtype)
+        if in_place:
+            out.copy_(s["residual"])
+            s["residual"] = out
+        call(s, out, ws)
+        assert api.sdvg_block_attn_status(ws) == api.SDVG_OK
+        assert_close(out, ref, tol)
+    assert bool((buf[0] == 77).all()) and bool((buf[rows + 1] == 77).all()) and bool((buf[:, cols:] == 77).all())
+    return out
+
+
+@pytest.mark.parametrize("rows,cols,inner", [(1, 128, 128), (64, 128, 512), (65, 256, 128), (256, 256, 512)])
+@pytest.mark.parametrize("out", ["fp32", "bf16", "e4m3"])
+def test_plain_tiles(rows, cols, inner, out):
+    check(problem(rows, cols, inner, out, bias=False, seed=1))
+
+
+SHAPES = [(1, 1, 1), (1, 1536, 256), (2, 5, 7), (3, 130, 72), (15, 128, 640), (16, 127, 63), (17, 129, 129), (33, 100, 700),
+          (64, 257, 1100), (127, 64, 640), (128, 300, 130), (129, 260, 515), (241, 129, 1281), (256, 256, 128), (257, 127, 1537),
+          (300, 515, 2000), (513, 70, 64), (1000, 640, 72)]
+
+
+@pytest.mark.parametrize("rows,cols,inner", SHAPES)
+@pytest.mark.parametrize("out", ["bf16", "fp32", "fp16", "e4m3"])
+def test_shapes(rows, cols, inner, out):
+    check(problem(rows, cols, inner, out, gate_rows=max(1, rows // 3), residual="" if out == "e4m3" else "rows",
+                  seed=rows + cols + inner))
+
+
+@pytest.mark.parametrize("rows", [5, 100])
+@pytest.mark.parametrize("act", list(ACTS))
+@pytest.mark.parametrize("out", ["bf16", "fp32", "e4m3"])
+def test_activations(rows, act, out):
+    check(problem(rows, 200, 300, out, act, residual="" if out == "e4m3" else "broadcast", gate_rows=rows, seed=7))
+
+
+@pytest.mark.parametrize("rows,cols,inner", [(3, 300, 1400), (90, 300, 1400), (90, 1, 600)])
+def test_scales_per_row_of_the_weights(rows, cols, inner):
+    check(problem(rows, cols, inner, "fp32", seed=11, w_rows=1, spread=20.0, more=1))
+
+
+@pytest.mark.parametrize("rows,cols,inner", [(3, 520, 9000), (40, 70, 5120), (70, 140, 9000)])
+@pytest.mark.parametrize("out", ["fp32", "bf16", "e4m3"])
+def test_long_sums(rows, cols, inner, out):
+    check(problem(rows, cols, inner, out, act="silu", seed=13, residual="" if out == "e4m3" else "rows"))
+
+
+@pytest.mark.parametrize("rows", [6, 150])
+def test_strides_and_in_place(rows):
+    check(problem(rows, 150, 260, "bf16", residual="rows", seed=17, more=3), ld_out=157, in_place=True)
+    check(problem(rows, 150, 260, "e4m3", seed=17, more=3), ld_out=153)
+
+
+@pytest.mark.parametrize("rows", [2, 80])
+def test_several_tiles_per_pair_and_wide_outputs(rows):
+    check(problem(rows * 12, 5000, 200, "bf16", seed=19, gate_rows=7))
+    check(problem(rows * 12, 5000, 200, "e4m3", act="gelu", seed=19, gate_rows=7))
+
+
+@pytest.mark.parametrize("rows", [4, 70])
+@pytest.mark.parametrize("out", ["fp32", "e4m3"])
+def test_extreme_scales_and_special_codes(rows, out):
+    """Exponents at the ends of the quantiser's range cancel; all-zero blocks (scale 2^-126) add nothing; NaN codes and the NaN scale
+    reach just the elements that they belong to."""
+    s = problem(rows, 256, 512, out, bias=False, seed=23, spread=0.0)
+    (x, xs), (w, ws_) = s["x"], s["w"]
+    xs[:, 0], ws_[:, 0] = 247, 10                          # 2^120 * 2^-117
+    x[:, 128:256], xs[:, 1] = 0, 1
+    w[:, 256:384], ws_[:, 2] = 0, 1
+    xs[1, 2] = 254                                         # 0 times anything finite
+    check(s)
+    x[0, 5] = 0x7F
+    w[7, 400] = 0xFF
+    xs[2, 3] = 255
+    out_t = torch.zeros((rows, 256), device="cuda", dtype=OUTS[out])
+    scale = torch.zeros((rows, 2), device="cuda", dtype=torch.uint8) if out == "e4m3" else None
+    call(s, out_t, api.attn_workspace(), scale)
+    nan = torch.isnan(out_t.view(torch.float8_e4m3fn).float() if out == "e4m3" else out_t)
+    want = torch.zeros_like(nan)
+    want[0], want[2], want[:, 7] = True, True, True
+    assert torch.equal(nan, want)
+
+
+@pytest.mark.parametrize("rows", [4, 200])
+def test_infinities_of_gate_and_residual(rows):
+    s = problem(rows, 130, 128, "bf16", act="silu", gate_rows=1, residual="rows", seed=29)
+    s["residual"] = s["residual"].clone()
+    s["residual"][0, 3] = float("inf")
+    s["gate"][1, 4] = float("-inf")
+    check(s)
+    s = problem(rows, 130, 128, "e4m3", gate_rows=1, seed=29)
+    s["gate"][1, 4], s["bias"][4] = float("inf"), 1e30
+    out, scale = torch.empty((rows, 130), device="cuda", dtype=torch.uint8), torch.empty((rows, 2), device="cuda", dtype=torch.uint8)
+    call(s, out, api.attn_workspace(), scale)
+    assert int(scale[1, 0]) == 247 and int(out[1, 4]) == 0x7E and int(out[1, :4].max() & 0x7F) == 0
+
+
+@pytest.mark.parametrize("rows", [1, 65])
+def test_equal_calls_give_equal_bits_and_streams(rows):
+    s = problem(rows, 700, 1300, "fp32", seed=31)
+    ws = api.attn_workspace()
+    a, b = (torch.empty((rows, 700), device="cuda") for _ in range(2))
+    call(s, a, ws)
+    other = torch.cuda.Stream()
+    other.wait_stream(torch.cuda.current_stream())
+    call(s, b, ws, stream=other)
+    torch.cuda.synchronize()
+    assert torch.equal(a, b)
+    graph = torch.cuda.CUDAGraph()
+    c = torch.empty_like(a)
+    with torch.cuda.graph(graph):
+        call(s, c, ws)
+    for _ in range(3):
+        graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(a, c)
+
+
+def test_nothing_to_do():
+    ws = api.attn_workspace()
+    x, xs = api.e4m3_matrix(4, 64)
+    w, wscale = api.e4m3_matrix(8, 64, 128)
+    api.sdvg_linear_e4m3(x[:0], xs[:0], w, wscale, torch.empty((0, 8), device="cuda"), ws)
+    api.sdvg_linear_e4m3(x, xs, w[:0], wscale[:0], torch.empty((4, 0), device="cuda"), ws)
+
+
+# ---- quantisation and back -------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("rows,cols", [(1, 1), (1, 128), (3, 129), (127, 40), (128, 128), (130, 300), (257, 1000)])
+@pytest.mark.parametrize("dtype", list(DTYPES))
+@pytest.mark.parametrize("block_rows", [1, 128])
+def test_quantised_matrices_equal_the_oracle(rows, cols, dtype, block_rows):
+    gen = torch.Generator(device="cuda").manual_seed(rows * cols)
+    for odd in (0, 1):
+        size = torch.exp2(torch.randint(-40, 40, (rows, 1), generator=gen, device="cuda").float() / (4 if dtype == "fp16" else 1))
+        x = torch.empty((rows, -(-cols // 8) * 8 + odd), device="cuda", dtype=DTYPES[dtype])[:, :cols]
+        x.copy_((randn(gen, rows, cols) * size).to(DTYPES[dtype]))
+        codes, scale = B.quantise(f64(x), block_rows)
+        out = torch.full((rows + 2, -(-cols // 8) * 8 + 8 + odd), 77, device="cuda", dtype=torch.uint8)
+        s = torch.full((scale.shape[0] + 2, scale.shape[1] + 1), 33, device="cuda", dtype=torch.uint8)
+        o, so = out[1:-1, :cols], s[1:-1, :-1]
+        api.sdvg_quant_e4m3_blocks(x, o, so)
+        assert np.array_equal(so.cpu().numpy(), scale)
+        assert np.array_equal(o.cpu().numpy(), codes)
+        assert bool((out[0] == 77).all()) and bool((out[-1] == 77).all()) and bool((out[:, cols:] == 77).all())
+        assert bool((s[0] == 33).all()) and bool((s[-1] == 33).all()) and bool((s[:, -1] == 33).all())
+        for back in DTYPES.values():
+            got = torch.full((rows, cols + 8 - cols % 8 + odd), 5.0, device="cuda", dtype=back)
+            api.sdvg_dequant_e4m3_blocks(o, so, got[:, :cols])
+            want = torch.from_numpy(B.values(codes, scale, block_rows)).to(back)
+            assert torch.equal(got[:, :cols].cpu(), want) and bool((got[:, cols:] == 5).all())
+
+
+@pytest.mark.parametrize("block_rows", [1, 128])
+def test_special_values_are_quantised_as_written(block_rows):
+    x = torch.zeros((130, 260), device="cuda")
+    x[0, 0], x[0, 130], x[1, 3], x[129, 259] = float("nan"), float("inf"), 2.0 ** -140, -float("inf")
+    x[2, 5], x[3, 6], x[128, 0] = 448.0, 450.0, 2.0 ** -149
+    codes, scale = B.quantise(f64(x), block_rows)
+    o, s = api.e4m3_matrix(130, 260, block_rows)
+    api.sdvg_quant_e4m3_blocks(x, o, s)
+    assert np.array_equal(s.cpu().numpy(), scale) and np.array_equal(o.cpu().numpy() & 0x7F, codes & 0x7F)
+    s[0, 0], s[-1, -1] = 0, 255
+    got = torch.empty((130, 260), device="cuda")
+    api.sdvg_dequant_e4m3_blocks(o, s, got)
+    want = torch.from_numpy(B.values(o.cpu().numpy(), s.cpu().numpy(), block_rows)).float()
+    assert torch.equal(torch.isnan(got.cpu()), torch.isnan(want)) and torch.equal(torch.nan_to_num(got.cpu()), torch.nan_to_num(want))
+
+
+def test_the_quantised_operands_of_a_product():
+    """Quantised by the library, multiplied, against the product of what the codes stand for, and near the unquantised one."""
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    x, w = randn(gen, 150, 1000).bfloat16(), randn(gen, 270, 1000, std=1000 ** -0.5).bfloat16()
+    xq, wq = api.e4m3_matrix(150, 1000), api.e4m3_matrix(270, 1000, 128)
+    api.sdvg_quant_e4m3_blocks(x, *xq)
+    api.sdvg_quant_e4m3_blocks(w, *wq)
+    s = dict(x=xq, w=wq, act="none", gate_rows=0, out="fp32", w_rows=128, bias=None, gate=None, residual=None)
+    got = f64(check(s))
+    ref = f64(x) @ f64(w).T
+    # each operand is off by at most 2^-4, 3.6% rms at worst evenly spread; both independent
+    assert np.linalg.norm(got - ref) <= 0.06 * np.linalg.norm(ref)
