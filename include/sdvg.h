@@ -668,6 +668,18 @@ int sdvg_dequant_e4m3_blocks(const void* x8, int64_t ld_x, const void* scale, in
                              int64_t ld_out, int out_type, int rows, int cols, void* stream);
 
 /*
+ * sdvg_gated_norm whose output is such rows (block_rows 1): out8 codes [rows, cols], out_scale bytes [rows, ceil(cols / 128)], both required.
+ * The normed values are quantised from fp32, with no other rounding.  With SDVG_NORM_NONE and nothing else it quantises the rows of x.
+ * out8 and out_scale may not overlap anything and need no alignment; whole vectors want out8 8-byte aligned, ld_out a multiple of 8.
+ * Other arguments and errors as sdvg_gated_norm.
+ */
+int sdvg_gated_norm_e4m3(const void* x, int64_t ld_x, int x_type, const void* y, int64_t ld_y, int y_type,
+                         int post_norm, const float* post_weight, const float* gate, int64_t ld_gate, int gate_rows,
+                         void* x_out, int64_t ld_x_out, int norm, const float* weight, const float* bias,
+                         const float* scale, const float* shift, int64_t ld_mod, int mod_rows, float eps,
+                         void* out8, int64_t ld_out, void* out_scale, int64_t ld_out_scale, int rows, int cols, void* stream);
+
+/*
  * sdvg_linear on such matrices: out[r, j] = residual[r, j] + gate[r / gate_rows, j] * act( sum_k x[r, k] w[j, k] + bias[j] )
  *   x8, x_scale   codes [rows, inner] and scales [rows, ceil(inner / 128)] (block_rows 1)
  *   w8, w_scale   codes [cols, inner] and scales [ceil(cols / w_scale_rows), ceil(inner / 128)], w_scale_rows 1 or 128

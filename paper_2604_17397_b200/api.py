@@ -95,6 +95,8 @@ SIGNATURES = {
                                         _VP, _I, _I64, _I, C.POINTER(_I64), _VP]),
     "sdvg_quant_e4m3_blocks": (_I, [_VP, _I64, _I, _VP, _I64, _VP, _I64, _I, _I, _I, _VP]),
     "sdvg_dequant_e4m3_blocks": (_I, [_VP, _I64, _VP, _I64, _I, _VP, _I64, _I, _I, _I, _VP]),
+    "sdvg_gated_norm_e4m3": (_I, [_VP, _I64, _I, _VP, _I64, _I, _I, _VP, _VP, _I64, _I, _VP, _I64, _I, _VP, _VP, _VP, _VP,
+                                  _I64, _I, _F, _VP, _I64, _VP, _I64, _I, _I, _VP]),
     "sdvg_linear_e4m3": (_I, [_VP, _I64, _VP, _I64, _VP, _I64, _VP, _I64, _I, _VP, _I, _VP, _I64, _I, _VP, _I64, _VP, _I64,
                               _VP, _I64, _I, _I, _I, _I, _VP, _SZ, _VP]),
 }
@@ -775,3 +777,18 @@ def sdvg_linear_e4m3(x8, x_scale, w8, w_scale, out, workspace, bias=None, act: i
                                 _raw_stream(dev, stream))
     if st != SDVG_OK:
         raise SdvgError(st, "sdvg_linear_e4m3")
+
+
+def sdvg_gated_norm_e4m3(x, out8, out_scale, y=None, gate=None, gate_rows: int = 0, post_norm: int = SDVG_NORM_NONE,
+                         post_weight=None, x_out=None, norm: int = SDVG_NORM_LAYER, weight=None, bias=None, scale=None, shift=None,
+                         modulate_rows: int = 0, eps: float = 1e-6, stream=None) -> None:
+    """sdvg_gated_norm whose output is E4M3 rows: uint8 codes [rows, cols] and scales [rows, ceil(cols / 128)]."""
+    dev = _device_of(x)
+    if _elsewhere(dev):
+        with torch.cuda.device(dev):
+            return sdvg_gated_norm_e4m3(x, out8, out_scale, y, gate, gate_rows, post_norm, post_weight, x_out, norm, weight, bias,
+                                        scale, shift, modulate_rows, eps, stream)
+    st = _binding().gated_norm_e4m3(x, out8, y, gate, gate_rows, post_norm, post_weight, x_out, norm, weight, bias, scale, shift,
+                                    modulate_rows, eps, _raw_stream(dev, stream), out_scale)
+    if st != SDVG_OK:
+        raise SdvgError(st, "sdvg_gated_norm_e4m3")

@@ -226,21 +226,26 @@ PyObject* e4m3_blocks(PyObject*, PyObject* const* args, Py_ssize_t n) {
 }
 
 // (x, out, y, gate, gate_rows, post_norm, post_weight, x_out, norm, weight, bias, scale, shift, modulate_rows, eps, stream)
-// -> status
+// -> status; with E4M3 also out_scale, after the stream
+template <bool E4M3>
 PyObject* gated_norm(PyObject*, PyObject* const* args, Py_ssize_t n) {
-  if (n != 16) return PyErr_Format(PyExc_TypeError, "gated_norm takes 16 arguments");
+  if (n != (E4M3 ? 17 : 16))
+    return PyErr_Format(PyExc_TypeError, E4M3 ? "gated_norm_e4m3 takes 17 arguments" : "gated_norm takes 16 arguments");
   Reader r{args};
-  const Tensor *x = r.tensor(0, "x", false), *out = r.tensor(1, "out", true), *y = r.tensor(2, "y", true);
+  const Tensor *x = r.tensor(0, "x", false), *out = r.tensor(1, "out", !E4M3), *y = r.tensor(2, "y", true);
   if (!r.ok) return nullptr;
   if (x->dim() != 2) return r.fail("x", "expected a matrix"), nullptr;
   const int64_t rows = x->size(0), cols = x->size(1);
   if (rows > 0x7fffffff || cols > 0x7fffffff) return r.fail("x", "too large"), nullptr;
-  for (const Tensor* t : {x, out, y})
+  const Tensor* out_scale = E4M3 ? r.tensor(16, "out_scale", false) : nullptr;
+  if (!r.ok) return nullptr;
+  for (const Tensor* t : {x, E4M3 ? nullptr : out, y})
     if (t && elem_type(t->scalar_type()) < 0)
       return r.fail("x, y, out", "expected bfloat16, float16 or float32 tensors"), nullptr;
   const int gate_rows = r.small(4), post = r.small(5), norm = r.small(8), mod_rows = r.small(13);
   const Matrix mx = matrix(r, x, rows, cols, x->scalar_type(), "x"),
-               mo = out ? matrix(r, out, rows, cols, out->scalar_type(), "out") : Matrix(),
+               mo = out ? matrix(r, out, rows, cols, E4M3 ? ScalarType::Byte : out->scalar_type(), "out") : Matrix(),
+               ms = matrix(r, out_scale, rows, (cols + 127) / 128, ScalarType::Byte, "out_scale"),
                my = y ? matrix(r, y, rows, cols, y->scalar_type(), "y") : Matrix(),
                xo = matrix(r, r.tensor(7, "x_out", true), rows, cols, x->scalar_type(), "x_out"),
                gate = groups(r, 3, rows, cols, gate_rows, "gate"), scale = groups(r, 11, rows, cols, mod_rows, "scale"),
@@ -254,8 +259,14 @@ PyObject* gated_norm(PyObject*, PyObject* const* args, Py_ssize_t n) {
   if (!r.ok) return nullptr;
   int st;
   Py_BEGIN_ALLOW_THREADS
-  st = sdvg_gated_norm(mx.p, mx.ld, mx.type, my.p, my.ld, my.type, post, post_weight, static_cast<const float*>(gate.p), gate.ld,
-                       gate_rows, xo.p, xo.ld, norm, weight, bias, static_cast<const float*>(scale.p),
+  if (E4M3)
+    st = sdvg_gated_norm_e4m3(mx.p, mx.ld, mx.type, my.p, my.ld, my.type, post, post_weight, static_cast<const float*>(gate.p),
+                              gate.ld, gate_rows, xo.p, xo.ld, norm, weight, bias, static_cast<const float*>(scale.p),
+                              static_cast<const float*>(shift.p), scale.p ? scale.ld : shift.ld, mod_rows, eps, mo.p, mo.ld, ms.p,
+                              ms.ld, (int)rows, (int)cols, stream);
+  else
+    st = sdvg_gated_norm(mx.p, mx.ld, mx.type, my.p, my.ld, my.type, post, post_weight, static_cast<const float*>(gate.p), gate.ld,
+                         gate_rows, xo.p, xo.ld, norm, weight, bias, static_cast<const float*>(scale.p),
                        static_cast<const float*>(shift.p), scale.p ? scale.ld : shift.ld, mod_rows, eps, mo.p, mo.ld, mo.type,
                        (int)rows, (int)cols, stream);
   Py_END_ALLOW_THREADS
@@ -330,8 +341,8 @@ PyMethodDef method(const char* name) {
   return {name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(guarded<F>)), METH_FASTCALL, nullptr};
 }
 
-PyMethodDef methods[] = {method<linear>("linear"), method<gated_norm>("gated_norm"), method<qk_norm>("qk_norm"),
-                         method<linear_e4m3>("linear_e4m3"), method<e4m3_blocks>("e4m3_blocks"),
+PyMethodDef methods[] = {method<linear>("linear"), method<gated_norm<false>>("gated_norm"), method<qk_norm>("qk_norm"),
+                         method<linear_e4m3>("linear_e4m3"), method<gated_norm<true>>("gated_norm_e4m3"), method<e4m3_blocks>("e4m3_blocks"),
                          {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

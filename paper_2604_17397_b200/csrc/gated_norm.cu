@@ -13,10 +13,12 @@
 
 #include <algorithm>
 
+#include "e4m3_scale.cuh"
 #include "elem_types.cuh"
 #include "overlap.cuh"
 #include "row_team.cuh"
 #include "sdvg_internal.h"
+#include "sm100_ptx.cuh"
 
 namespace {
 
@@ -29,13 +31,14 @@ struct NormParams {
   const void* y;               // null: no sublayer output
   void* x_out;                 // null: not wanted
   void* out;                   // null: not wanted
+  uint8_t* out_scale;          // 8-bit outputs: the scale byte of row r and 128-column block b at r * ld_out_scale + b
   const float* post_weight;
   const float* gate;
   const float* weight;
   const float* bias;
   const float* scale;
   const float* shift;
-  long long ld_x, ld_y, ld_x_out, ld_out, ld_gate, ld_mod;
+  long long ld_x, ld_y, ld_x_out, ld_out, ld_out_scale, ld_gate, ld_mod;
   int x_type, y_type, out_type;
   int post, norm;
   int gate_rows, mod_rows;
@@ -134,8 +137,9 @@ __device__ __forceinline__ void apply_norm(Vec8 (&v)[NI], float mean, float rstd
 
 // Rows of aligned vectors.  XW and YW: bytes of x's and y's elements (YW = 0: no y).  A thread holds NI pieces of 8 columns; the
 // pieces of a warp are 32 vectors apart, so that they are a constant distance from one address per row, which moves on by the
-// row stride.  FULL: the team's pieces are all inside the row.
-template <int XW, int YW, int NI, bool WARP, bool FULL>
+// row stride.  FULL: the team's pieces are all inside the row.  OUT8: the output is E4M3 codes with a scale per 128 columns, which are
+// half a warp's piece.
+template <int XW, int YW, int NI, bool WARP, bool FULL, bool OUT8>
 __global__ void __launch_bounds__(WARP ? 128 : kTeamThreads) gated_norm_kernel(const __grid_constant__ NormParams p) {
   extern __shared__ uint4 s_ring[];
   __shared__ Moments s_part[2][32];
@@ -159,11 +163,12 @@ __global__ void __launch_bounds__(WARP ? 128 : kTeamThreads) gated_norm_kernel(c
   uint4* ring = s_ring + warp * 32 * (kSlots * (Ring<XW, NI>::kBytes + Ring<YW, NI>::kBytes) / 16) + lane;
   const Ring<XW, NI> rx{ring};
   const Ring<YW, NI> ry{ring + kSlots * Ring<XW, NI>::kBytes / 16 * 32};
-  const int out_bytes = p.out_type == SDVG_F32 ? 4 : 2;
+  const int out_bytes = OUT8 ? 1 : p.out_type == SDVG_F32 ? 4 : 2;
   const char* x = static_cast<const char*>(p.x) + (begin * p.ld_x + c0) * XW;
   const char* y = static_cast<const char*>(p.y) + (begin * p.ld_y + c0) * YW;
   char* x_out = static_cast<char*>(p.x_out) + (begin * p.ld_x_out + c0) * XW;
   char* out = static_cast<char*>(p.out) + (begin * p.ld_out + c0) * out_bytes;
+  uint8_t* out_scale = OUT8 ? p.out_scale + begin * p.ld_out_scale + c0 / 128 : nullptr;
   const long long step_x = p.ld_x * XW, step_y = p.ld_y * YW, step_x_out = p.ld_x_out * XW, step_out = p.ld_out * out_bytes;
   int asked = 0;                                       // rows requested so far; x and y point at the next one
   const int total = (int)(end - begin);
@@ -277,8 +282,31 @@ __global__ void __launch_bounds__(WARP ? 128 : kTeamThreads) gated_norm_kernel(c
     for (int i = 0; i < NI; ++i) {
 #pragma unroll
       for (int j = 0; j < 4; ++j) s[i].p[j] = fma2(s[i].p[j], A[i].p[j], B[i].p[j]);
-      if (valid(i)) store8(out + 256 * out_bytes * i, p.out_type, s[i]);
+      if constexpr (OUT8) {
+        float f[8];
+        uint32_t top = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float2 a = floats_of(s[i].p[j]);
+          f[2 * j] = a.x;
+          f[2 * j + 1] = a.y;
+          if (valid(i)) top = max(top, max(sdvg::magnitude_bits(a.x), sdvg::magnitude_bits(a.y)));
+        }
+#pragma unroll
+        for (int o = 8; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+        const int e = sdvg::scale_exponent(top);
+        const float inv = sdvg::power_of_two(-e);
+        if (valid(i)) {
+          __stcs(reinterpret_cast<uint2*>(out + 256 * i),
+                 make_uint2(sm100::pack_e4m3x4(f[0] * inv, f[1] * inv, f[2] * inv, f[3] * inv),
+                            sm100::pack_e4m3x4(f[4] * inv, f[5] * inv, f[6] * inv, f[7] * inv)));
+          if (lane % 16 == 0) out_scale[2 * i] = (uint8_t)(e + 127);
+        }
+      } else {
+        if (valid(i)) store8(out + 256 * out_bytes * i, p.out_type, s[i]);
+      }
     }
+    if (OUT8) out_scale += p.ld_out_scale;
     out += step_out;
   }
   copy_wait<0>();
@@ -330,7 +358,8 @@ __device__ __forceinline__ void store_singles(const float (&v)[NI], void* base, 
 
 // Rows that are not made of aligned vectors: one CTA per row, NI single columns per thread; what is in flight comes from the
 // CTAs of an SM.
-template <int NI>
+// OUT8: four pieces of a warp are a block of 128 columns.
+template <int NI, bool OUT8>
 __global__ void __launch_bounds__(NI == 16 ? 512 : 256) gated_norm_single_kernel(const __grid_constant__ NormParams p) {
   __shared__ Moments s_part[2][32];
   __shared__ float s_count[32];
@@ -396,7 +425,24 @@ __global__ void __launch_bounds__(NI == 16 ? 512 : 256) gated_norm_single_kernel
   with_vector(p.bias, [&](int i, float f) { s[i] += f; });
   with_vector(p.scale ? p.scale + group * p.ld_mod : nullptr, [&](int i, float f) { s[i] = fmaf(s[i], f, s[i]); });
   with_vector(p.shift ? p.shift + group * p.ld_mod : nullptr, [&](int i, float f) { s[i] += f; });
-  store_singles<NI>(s, p.out, r * p.ld_out + c0, p.out_type, valid);
+  if constexpr (OUT8) {
+    uint8_t* o = static_cast<uint8_t*>(p.out) + r * p.ld_out + c0;
+#pragma unroll
+    for (int b = 0; b < NI / 4; ++b) {
+      uint32_t top = 0;
+#pragma unroll
+      for (int i = 4 * b; i < 4 * b + 4; ++i) top = max(top, valid(i) ? sdvg::magnitude_bits(s[i]) : 0u);
+      const int e = sdvg::scale_exponent(__reduce_max_sync(0xffffffffu, top));
+      const float inv = sdvg::power_of_two(-e);
+      const uint32_t codes = sm100::pack_e4m3x4(s[4 * b] * inv, s[4 * b + 1] * inv, s[4 * b + 2] * inv, s[4 * b + 3] * inv);
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (valid(4 * b + i)) o[32 * (4 * b + i)] = (uint8_t)(codes >> (8 * i));
+      if (lane == 0 && valid(4 * b)) p.out_scale[r * p.ld_out_scale + c0 / 128 + b] = (uint8_t)(e + 127);
+    }
+  } else {
+    store_singles<NI>(s, p.out, r * p.ld_out + c0, p.out_type, valid);
+  }
 }
 
 // ---- rows that no team can hold: one CTA per row, which reads it once per statistic -----------------------------
@@ -432,6 +478,7 @@ __device__ __forceinline__ void row_stats(const NormParams& p, int kind, Value v
   *rstd = 1.f / sqrtf(block_sum(q, buf) * p.inv_cols + p.eps);
 }
 
+template <bool OUT8>
 __global__ void __launch_bounds__(kLongThreads) gated_norm_long_kernel(const __grid_constant__ NormParams p) {
   __shared__ float buf[kLongThreads / 32];
   sdvg::overlap_begin();
@@ -453,16 +500,46 @@ __global__ void __launch_bounds__(kLongThreads) gated_norm_long_kernel(const __g
   };
   float mean = 0.f, rstd = 1.f;
   if (p.out) row_stats(p, p.norm, sum, buf, &mean, &rstd);
-  for (int c = threadIdx.x; c < p.cols; c += kLongThreads) {
-    const float s = sum(c);                          // read before either output is written: both may be in place
-    if (p.x_out) store_elem(p.x_out, r * p.ld_x_out + c, p.x_type, s);
-    if (!p.out) continue;
+  auto normed = [&](float s, int c) {
     float o = (s - mean) * rstd;
     if (p.weight) o *= p.weight[c];
     if (p.bias) o += p.bias[c];
     if (scale) o *= 1.f + scale[c];
     if (shift) o += shift[c];
-    store_elem(p.out, r * p.ld_out + c, p.out_type, o);
+    return o;
+  };
+  if constexpr (OUT8) {
+    // a warp takes whole blocks of 128 columns, a lane four of them 32 apart
+    const int lane = threadIdx.x % 32, blocks = p.cols / 128 + (p.cols % 128 ? 1 : 0);
+    uint8_t* out = static_cast<uint8_t*>(p.out) + r * p.ld_out;
+    for (int b = threadIdx.x / 32; b < blocks; b += kLongThreads / 32) {
+      const int c0 = 128 * b + lane;
+      float o[4];
+      uint32_t top = 0;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int c = c0 + 32 * i;
+        o[i] = 0.f;
+        if (c >= p.cols) continue;
+        const float s = sum(c);                      // read before either output is written: both may be in place
+        if (p.x_out) store_elem(p.x_out, r * p.ld_x_out + c, p.x_type, s);
+        o[i] = normed(s, c);
+        top = max(top, sdvg::magnitude_bits(o[i]));
+      }
+      const int e = sdvg::scale_exponent(__reduce_max_sync(0xffffffffu, top));
+      const float inv = sdvg::power_of_two(-e);
+      const uint32_t codes = sm100::pack_e4m3x4(o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv);
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (c0 + 32 * i < p.cols) out[c0 + 32 * i] = (uint8_t)(codes >> (8 * i));
+      if (lane == 0) p.out_scale[r * p.ld_out_scale + b] = (uint8_t)(e + 127);
+    }
+  } else {
+    for (int c = threadIdx.x; c < p.cols; c += kLongThreads) {
+      const float s = sum(c);                        // read before either output is written: both may be in place
+      if (p.x_out) store_elem(p.x_out, r * p.ld_x_out + c, p.x_type, s);
+      if (p.out) store_elem(p.out, r * p.ld_out + c, p.out_type, normed(s, c));
+    }
   }
 }
 
@@ -483,7 +560,7 @@ int device_sms(int* sms) {
 constexpr int kMostDynamic = 200 * 1024;
 constexpr int kFreeDynamic = 40 * 1024;                // needs no opt-in, with what the kernel has statically: 48 KB in all
 
-template <int XW, int YW, int NI, bool WARP, bool FULL>
+template <int XW, int YW, int NI, bool WARP, bool FULL, bool OUT8>
 int launch_team_as(const NormParams& p, int threads, int sms, cudaStream_t stream) {
   const int rows_per_cta = WARP ? threads / 32 : 1;
   const int want = (p.rows + rows_per_cta - 1) / rows_per_cta;
@@ -497,7 +574,7 @@ int launch_team_as(const NormParams& p, int threads, int sms, cudaStream_t strea
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return sdvg::cuda_status(e);
     if (dev != known_dev || dynamic != known_dynamic) {
-      auto kernel = gated_norm_kernel<XW, YW, NI, WARP, FULL>;
+      auto kernel = gated_norm_kernel<XW, YW, NI, WARP, FULL, OUT8>;
       known_dev = -1;
       if (dynamic > kFreeDynamic) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostDynamic);
       if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&resident, kernel, threads, dynamic);
@@ -507,24 +584,25 @@ int launch_team_as(const NormParams& p, int threads, int sms, cudaStream_t strea
     }
     grid = std::min(want, sms * std::max(resident, 1));
   }
-  return sdvg::cuda_status(sdvg::launch_overlapped(gated_norm_kernel<XW, YW, NI, WARP, FULL>, grid, threads, dynamic, 0, stream, p));
+  return sdvg::cuda_status(sdvg::launch_overlapped(gated_norm_kernel<XW, YW, NI, WARP, FULL, OUT8>, grid, threads, dynamic, 0, stream, p));
 }
 
-template <int XW, int YW, int NI, bool WARP>
+template <int XW, int YW, int NI, bool WARP, bool OUT8>
 int launch_team(const NormParams& p, int threads, int sms, cudaStream_t stream) {
-  return p.cols == (WARP ? 32 : threads) * NI * 8 ? launch_team_as<XW, YW, NI, WARP, true>(p, threads, sms, stream)
-                                                  : launch_team_as<XW, YW, NI, WARP, false>(p, threads, sms, stream);
+  return p.cols == (WARP ? 32 : threads) * NI * 8 ? launch_team_as<XW, YW, NI, WARP, true, OUT8>(p, threads, sms, stream)
+                                                  : launch_team_as<XW, YW, NI, WARP, false, OUT8>(p, threads, sms, stream);
 }
 
-template <int XW, int YW>
+template <int XW, int YW, bool OUT8>
 int launch_vec(const NormParams& p, int sms, cudaStream_t stream) {
   const int vecs = p.cols / 8;
-  if (vecs <= 32) return launch_team<XW, YW, 1, true>(p, 128, sms, stream);
-  if (vecs <= 64) return launch_team<XW, YW, 2, true>(p, 128, sms, stream);
-  if (vecs <= 2 * kTeamThreads) return launch_team<XW, YW, 2, false>(p, (vecs + 63) / 64 * 32, sms, stream);
+  if (vecs <= 32) return launch_team<XW, YW, 1, true, OUT8>(p, 128, sms, stream);
+  if (vecs <= 64) return launch_team<XW, YW, 2, true, OUT8>(p, 128, sms, stream);
+  if (vecs <= 2 * kTeamThreads) return launch_team<XW, YW, 2, false, OUT8>(p, (vecs + 63) / 64 * 32, sms, stream);
   return -1;
 }
 
+template <bool OUT8>
 int launch(const NormParams& p, bool vec, cudaStream_t stream) {
   int sms = 0;
   int st = device_sms(&sms);
@@ -532,52 +610,52 @@ int launch(const NormParams& p, bool vec, cudaStream_t stream) {
   st = -1;                                             // -1: a row does not fit the team
   if (vec) {
     const bool x4 = p.x_type == SDVG_F32, y4 = p.y && p.y_type == SDVG_F32;
-    if (!p.y) st = x4 ? launch_vec<4, 0>(p, sms, stream) : launch_vec<2, 0>(p, sms, stream);
-    else if (y4) st = x4 ? launch_vec<4, 4>(p, sms, stream) : launch_vec<2, 4>(p, sms, stream);
-    else st = x4 ? launch_vec<4, 2>(p, sms, stream) : launch_vec<2, 2>(p, sms, stream);
+    if (!p.y) st = x4 ? launch_vec<4, 0, OUT8>(p, sms, stream) : launch_vec<2, 0, OUT8>(p, sms, stream);
+    else if (y4) st = x4 ? launch_vec<4, 4, OUT8>(p, sms, stream) : launch_vec<2, 4, OUT8>(p, sms, stream);
+    else st = x4 ? launch_vec<4, 2, OUT8>(p, sms, stream) : launch_vec<2, 2, OUT8>(p, sms, stream);
     if (st != -1) return st;
   } else if (p.cols <= 512 * 16) {
     auto single = [&](void (*kernel)(NormParams), int pieces) {
       const int threads = ((p.cols + pieces - 1) / pieces + 31) / 32 * 32;
       return sdvg::cuda_status(sdvg::launch_overlapped(kernel, p.rows, threads, 0, 0, stream, p));
     };
-    if (p.cols <= 256) return single(gated_norm_single_kernel<1>, 1);
-    if (p.cols <= 1024) return single(gated_norm_single_kernel<4>, 4);
-    if (p.cols <= 2048) return single(gated_norm_single_kernel<8>, 8);
-    return single(gated_norm_single_kernel<16>, 16);
+    if constexpr (!OUT8) {
+      if (p.cols <= 256) return single(gated_norm_single_kernel<1, false>, 1);
+    }
+    if (p.cols <= 1024) return single(gated_norm_single_kernel<4, OUT8>, 4);
+    if (p.cols <= 2048) return single(gated_norm_single_kernel<8, OUT8>, 8);
+    return single(gated_norm_single_kernel<16, OUT8>, 16);
   }
-  return sdvg::cuda_status(sdvg::launch_overlapped(gated_norm_long_kernel, p.rows, kLongThreads, 0, 0, stream, p));
+  return sdvg::cuda_status(sdvg::launch_overlapped(gated_norm_long_kernel<OUT8>, p.rows, kLongThreads, 0, 0, stream, p));
 }
 
 bool aligned_to(const void* p, int bytes) { return (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(bytes - 1)) == 0; }
 
-}  // namespace
-
-extern "C" {
-
-int sdvg_gated_norm(const void* x, int64_t ld_x, int x_type, const void* y, int64_t ld_y, int y_type, int post_norm,
+// Both entry points: out_type SDVG_E4M3 with out_scale, or another type without.
+int gated_norm(const void* x, int64_t ld_x, int x_type, const void* y, int64_t ld_y, int y_type, int post_norm,
                     const float* post_weight, const float* gate, int64_t ld_gate, int gate_rows, void* x_out,
                     int64_t ld_x_out, int norm, const float* weight, const float* bias, const float* scale,
                     const float* shift, int64_t ld_mod, int mod_rows, float eps, void* out, int64_t ld_out, int out_type,
-                    int rows, int cols, void* stream) {
-  SDVG_RANGE();
+                    void* out_scale, int64_t ld_out_scale, int rows, int cols, void* stream) {
+  const bool out8 = out_type == SDVG_E4M3;
   constexpr int kMaxExtent = 0x7fffffff - 1024;                  // a column one step of a CTA further on is still an int
   if (rows < 0 || cols < 1 || rows > kMaxExtent || cols > kMaxExtent) return SDVG_ERR_BAD_SHAPE;
   if (post_norm < SDVG_NORM_NONE || post_norm > SDVG_NORM_LAYER || norm < SDVG_NORM_NONE || norm > SDVG_NORM_LAYER)
     return SDVG_ERR_INVALID_ARG;
-  if (!sdvg::elem_type_ok(x_type) || (y && !sdvg::elem_type_ok(y_type)) || (out && !sdvg::elem_type_ok(out_type)))
+  if (!sdvg::elem_type_ok(x_type) || (y && !sdvg::elem_type_ok(y_type)) || (out && !out8 && !sdvg::elem_type_ok(out_type)))
     return SDVG_ERR_INVALID_ARG;
   if (!(eps >= 0.f) || !isfinite(eps)) return SDVG_ERR_INVALID_ARG;
   if (!y && (post_norm != SDVG_NORM_NONE || post_weight || gate)) return SDVG_ERR_INVALID_ARG;
   if ((gate && gate_rows < 1) || ((scale || shift) && mod_rows < 1)) return SDVG_ERR_INVALID_ARG;
   if (rows == 0) return SDVG_OK;
-  if (!x || (!x_out && !out)) return SDVG_ERR_INVALID_ARG;
+  if (!x || (!x_out && !out) || (out8 && (!out || !out_scale))) return SDVG_ERR_INVALID_ARG;
   if (rows > 1 && (ld_x < cols || (y && ld_y < cols) || (x_out && ld_x_out < cols) || (out && ld_out < cols)))
     return SDVG_ERR_BAD_SHAPE;
+  if (out8 && rows > 1 && ld_out_scale < (cols + 127) / 128) return SDVG_ERR_BAD_SHAPE;
   if ((gate && rows > gate_rows && ld_gate < cols) || ((scale || shift) && rows > mod_rows && ld_mod < cols))
     return SDVG_ERR_BAD_SHAPE;
   if (!aligned_to(x, sdvg::elem_bytes(x_type)) || (y && !aligned_to(y, sdvg::elem_bytes(y_type))) ||
-      !aligned_to(x_out, sdvg::elem_bytes(x_type)) || (out && !aligned_to(out, sdvg::elem_bytes(out_type))) ||
+      !aligned_to(x_out, sdvg::elem_bytes(x_type)) || (out && !out8 && !aligned_to(out, sdvg::elem_bytes(out_type))) ||
       !aligned_to(post_weight, 4) || !aligned_to(gate, 4) || !aligned_to(weight, 4) || !aligned_to(bias, 4) ||
       !aligned_to(scale, 4) || !aligned_to(shift, 4))
     return SDVG_ERR_MISALIGNED;
@@ -598,6 +676,8 @@ int sdvg_gated_norm(const void* x, int64_t ld_x, int x_type, const void* y, int6
   p.ld_y = ld_y;
   p.ld_x_out = ld_x_out;
   p.ld_out = ld_out;
+  p.out_scale = (uint8_t*)out_scale;
+  p.ld_out_scale = ld_out_scale;
   p.ld_gate = ld_gate;
   p.ld_mod = ld_mod;
   p.x_type = x_type;
@@ -612,7 +692,7 @@ int sdvg_gated_norm(const void* x, int64_t ld_x, int x_type, const void* y, int6
   p.eps = eps;
   p.inv_cols = 1.f / (float)cols;
   p.num_cols = (float)cols;
-  // whole vectors: every address a row or a vector is read or written at is a multiple of 16 bytes
+  // whole vectors: every address a row or a vector is read or written at is a multiple of 16 bytes (of codes: 8)
   auto rows_ok = [&](const void* base, int64_t ld, int type) {
     return !base || (sdvg::aligned16(base) && (rows == 1 || ld * sdvg::elem_bytes(type) % 16 == 0));
   };
@@ -620,10 +700,37 @@ int sdvg_gated_norm(const void* x, int64_t ld_x, int x_type, const void* y, int6
     return !base || (sdvg::aligned16(base) && (rows <= group_rows || ld % 4 == 0));
   };
   const bool vec = cols % 8 == 0 && rows_ok(x, ld_x, x_type) && rows_ok(y, ld_y, y_type) && rows_ok(x_out, ld_x_out, x_type) &&
-                   rows_ok(out, ld_out, out_type) && groups_ok(gate, ld_gate, gate_rows) && groups_ok(scale, ld_mod, mod_rows) &&
+                   (out8 ? aligned_to(out, 8) && (rows == 1 || ld_out % 8 == 0) : rows_ok(out, ld_out, out_type)) && groups_ok(gate, ld_gate, gate_rows) && groups_ok(scale, ld_mod, mod_rows) &&
                    groups_ok(shift, ld_mod, mod_rows) && sdvg::aligned16(post_weight) && sdvg::aligned16(weight) &&
                    sdvg::aligned16(bias);
-  return launch(p, vec, (cudaStream_t)stream);
+  return out8 ? launch<true>(p, vec, (cudaStream_t)stream) : launch<false>(p, vec, (cudaStream_t)stream);
+}
+
+}  // namespace
+
+extern "C" {
+
+int sdvg_gated_norm(const void* x, int64_t ld_x, int x_type, const void* y, int64_t ld_y, int y_type, int post_norm,
+                    const float* post_weight, const float* gate, int64_t ld_gate, int gate_rows, void* x_out,
+                    int64_t ld_x_out, int norm, const float* weight, const float* bias, const float* scale,
+                    const float* shift, int64_t ld_mod, int mod_rows, float eps, void* out, int64_t ld_out, int out_type,
+                    int rows, int cols, void* stream) {
+  SDVG_RANGE();
+  if (out && out_type == SDVG_E4M3 && rows >= 0 && cols >= 1) return SDVG_ERR_INVALID_ARG;
+  return gated_norm(x, ld_x, x_type, y, ld_y, y_type, post_norm, post_weight, gate, ld_gate, gate_rows, x_out, ld_x_out, norm,
+                    weight, bias, scale, shift, ld_mod, mod_rows, eps, out, ld_out, out ? out_type : SDVG_F32, nullptr, 0, rows, cols,
+                    stream);
+}
+
+int sdvg_gated_norm_e4m3(const void* x, int64_t ld_x, int x_type, const void* y, int64_t ld_y, int y_type, int post_norm,
+                         const float* post_weight, const float* gate, int64_t ld_gate, int gate_rows, void* x_out,
+                         int64_t ld_x_out, int norm, const float* weight, const float* bias, const float* scale,
+                         const float* shift, int64_t ld_mod, int mod_rows, float eps, void* out8, int64_t ld_out,
+                         void* out_scale, int64_t ld_out_scale, int rows, int cols, void* stream) {
+  SDVG_RANGE();
+  return gated_norm(x, ld_x, x_type, y, ld_y, y_type, post_norm, post_weight, gate, ld_gate, gate_rows, x_out, ld_x_out, norm,
+                    weight, bias, scale, shift, ld_mod, mod_rows, eps, out8, ld_out, SDVG_E4M3, out_scale, ld_out_scale, rows,
+                    cols, stream);
 }
 
 }  // extern "C"

@@ -79,6 +79,34 @@ def test_quantisation_refuses_on_the_host(lib, change, status):
     assert lib.sdvg_dequant_e4m3_blocks(x8, ld_8, s, ld_s, block, x, ld_x, t, rows, cols, None) == want
 
 
+def norm_args(**change):
+    a = dict(x=X, ld_x=200, x_type=0, y=None, ld_y=0, y_type=0, post=0, post_weight=None, gate=None, ld_gate=0, gate_rows=0, x_out=None,
+             ld_x_out=0, norm=2, weight=None, bias=None, scale=None, shift=None, ld_mod=0, mod_rows=0, eps=1e-6, out=OUT, ld_out=200, os=OS,
+             ld_os=2, rows=4, cols=200, stream=None)
+    assert set(change) <= set(a)
+    return list({**a, **change}.values())
+
+
+@pytest.mark.parametrize("change,status", [
+    (dict(rows=-1), "BAD_SHAPE"), (dict(cols=0), "BAD_SHAPE"), (dict(rows=0x7fffffff), "BAD_SHAPE"), (dict(ld_x=199), "BAD_SHAPE"),
+    (dict(ld_out=199), "BAD_SHAPE"), (dict(ld_os=1), "BAD_SHAPE"), (dict(x_out=R, ld_x_out=199), "BAD_SHAPE"),
+    (dict(scale=G, mod_rows=2, ld_mod=199), "BAD_SHAPE"), (dict(norm=3), "INVALID_ARG"), (dict(x_type=3), "INVALID_ARG"),
+    (dict(y=W, ld_y=200, y_type=3), "INVALID_ARG"), (dict(post=1), "INVALID_ARG"), (dict(eps=float("nan")), "INVALID_ARG"),
+    (dict(shift=G, mod_rows=0), "INVALID_ARG"), (dict(x=None), "INVALID_ARG"), (dict(out=None), "INVALID_ARG"), (dict(os=None), "INVALID_ARG"),
+    (dict(out=None, x_out=R, ld_x_out=200), "INVALID_ARG"), (dict(os=None, x_out=R, ld_x_out=200), "INVALID_ARG"),
+    (dict(x=X + 1), "MISALIGNED"), (dict(weight=B_ + 2), "MISALIGNED"), (dict(x_out=R + 1, ld_x_out=200), "MISALIGNED"),
+])
+def test_gated_norm_refuses_on_the_host(lib, change, status):
+    assert lib.sdvg_gated_norm_e4m3(*norm_args(**change)) == getattr(api, "SDVG_ERR_" + status)
+
+
+def test_gated_norm_with_nothing_to_do_and_codes_of_any_alignment(lib):
+    assert lib.sdvg_gated_norm_e4m3(*norm_args(rows=0, x=None, out=None, os=None)) == api.SDVG_OK
+    assert lib.sdvg_gated_norm_e4m3(*norm_args(out=OUT + 1, os=OS + 1, weight=B_ + 1)) == api.SDVG_ERR_MISALIGNED
+    assert lib.sdvg_gated_norm(X, 200, 0, None, 0, 0, 0, None, None, 0, 0, None, 0, 2, None, None, None, None, 0, 0, 1e-6, OUT, 200, 3, 4, 200,
+                               None) == api.SDVG_ERR_INVALID_ARG
+
+
 def u8(*shape):
     return OnPaper(*shape, dtype=torch.uint8)
 
@@ -104,6 +132,12 @@ def test_the_binding_reads_and_refuses(lib):
     for change in (dict(ws=without_address(2, 3, dtype=torch.uint8)), dict(space=without_address(256, dtype=torch.uint8))):
         with pytest.raises(RuntimeError):
             linear_on_paper(**change)
+    norm = lambda x, out, scale: api._binding().gated_norm_e4m3(x, out, None, None, 0, 0, None, None, 2, None, None, None, None, 0, 1e-6, 0, scale)
+    assert norm(OnPaper(4, 200), u8(4, 200), u8(4, 2)) == reached
+    for bad in ((OnPaper(4, 200), OnPaper(4, 200), u8(4, 2)), (OnPaper(4, 200), u8(4, 200), u8(4, 3)), (OnPaper(4, 200), u8(4, 201), u8(4, 2)),
+                (u8(4, 200), u8(4, 200), u8(4, 2)), (OnPaper(4, 200), None, u8(4, 2)), (OnPaper(4, 200), u8(4, 200), None)):
+        with pytest.raises(ValueError):
+            norm(*bad)
     blocks = api._binding().e4m3_blocks
     for way in (0, 1):
         assert blocks(OnPaper(200, 300), u8(200, 300), u8(200, 3), way, 0) == reached

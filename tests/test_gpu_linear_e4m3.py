@@ -6,6 +6,7 @@ import pytest
 import torch
 
 from dense_utils import DTYPES, assert_close, f64, linear_tolerance
+from e4m3_utils import check_quantised
 from oracle import dense_oracle as D
 from oracle import e4m3_blocks_oracle as B
 from paper_2604_17397_b200 import api
@@ -60,16 +61,6 @@ def expected(s, dtype):
     ref = D.linear_ref(x, w, b, s["act"], g, s["gate_rows"], r)
     per_row = None if g is None else D.of_rows(g, x.shape[0], s["gate_rows"])
     return ref, linear_tolerance(x, w, b, s["act"], per_row, r, ref, dtype)
-
-
-def check_quantised(codes, scale, ref, err):
-    """Rows of codes of values known up to err: the scale is that of some value within it, the codes are within half a step."""
-    e = scale.cpu().numpy().astype(np.int64)
-    lo, hi = (B.scale_bytes(np.maximum(np.abs(ref) + d, 0), 1).astype(np.int64) for d in (-err, err))
-    assert ((lo <= e) & (e <= hi)).all()
-    f = B.of_elements(scale.cpu().numpy(), *ref.shape, 1)
-    tol = err + B.half_step(np.abs(ref) + err, f)
-    assert_close(B.values(codes.cpu().numpy(), scale.cpu().numpy(), 1), ref, tol, "codes")
 
 
 def check(s, ld_out=None, in_place=False):
