@@ -644,6 +644,49 @@ int sdvg_qk_norm_rope3d_commit(sdvg_cache* cache, const void* q, int64_t ld_q, c
                                int frame_offset, const float* cos_sin_tab, int tab_frames, int64_t block_index,
                                int flags, int64_t* evicted_block, void* stream);
 
+/*
+ * The same for an 8-bit ring with static scales (head_dim 128): q8_out = e4m3(rope(rms(q) * q_weight) * q_inv_scale[head]), and
+ * e4m3(rope(rms(k) * k_weight) * k_inv_scale[head]) and e4m3(v * v_inv_scale[head]) into the ring.  Everything before the conversion
+ * is fp32: nothing is rounded to bf16 between (sdvg_rope3d_qk_commit_e4m3 rounds the rotated values to bf16 first).
+ * q8_out: device codes [block_tokens, heads, 128], contiguous; inverse scales device fp32 [heads].  q, q8_out and q_inv_scale
+ * may be NULL together.  Other arguments and errors as sdvg_qk_norm_rope3d_commit; BAD_SHAPE for a bf16 ring.
+ */
+int sdvg_qk_norm_rope3d_commit_e4m3(sdvg_cache* cache, const void* q, int64_t ld_q, const void* k, int64_t ld_k,
+                                    const void* v, int64_t ld_v, const float* q_weight, const float* k_weight, int scope,
+                                    float eps, void* q8_out, const float* q_inv_scale, const float* k_inv_scale,
+                                    const float* v_inv_scale, int frames, int grid_h, int grid_w, int frame_offset,
+                                    const float* cos_sin_tab, int tab_frames, int64_t block_index, int flags,
+                                    int64_t* evicted_block, void* stream);
+
+/* Bytes of the workspace of the next call: 256 and two floats per token; 0 for block_tokens < 1. */
+size_t sdvg_qk_norm_workspace_bytes(int block_tokens);
+
+/*
+ * And for an 8-bit ring with tile scales: the fp32 values of rope(rms(q) * q_weight), rope(rms(k) * k_weight) and v, quantised with
+ * the scale of their tile and head as sdvg_quant_e4m3_tiled chooses it; q8_out with q_tile_scale [heads][tiles] (NULL together
+ * with q), k and v into the ring and its scale arrays.
+ *   workspace   with SDVG_SCOPE_ROW: device memory of sdvg_qk_norm_workspace_bytes(block_tokens), 256-byte aligned, written and read
+ *               within the call (calls that may overlap on the device need one each; so do graphs that may run at the same
+ *               time); its first 256 bytes are not touched.  Not looked at with SDVG_SCOPE_HEAD.
+ * Other arguments and errors as above; BAD_STATE also when no scale arrays are attached.
+ */
+int sdvg_qk_norm_rope3d_commit_e4m3_tiled(sdvg_cache* cache, const void* q, int64_t ld_q, const void* k, int64_t ld_k,
+                                          const void* v, int64_t ld_v, const float* q_weight, const float* k_weight, int scope,
+                                          float eps, void* q8_out, float* q_tile_scale, int frames, int grid_h, int grid_w,
+                                          int frame_offset, const float* cos_sin_tab, int tab_frames, int64_t block_index,
+                                          int flags, int64_t* evicted_block, void* workspace, size_t workspace_bytes,
+                                          void* stream);
+
+/*
+ * A slot of an 8-bit ring read back as values: k_out and v_out (either may be NULL), device bf16 [block_tokens, heads, 128], receive
+ * code * scale, rounded once.  k_descale, v_descale: device fp32 [heads], the scales of a ring with static ones (of what is read);
+ * both NULL: the ring's tile scales.  Like sdvg_cache_read_block it reads whatever the slot holds.
+ * Errors: INVALID_ARG (slot, missing scales), BAD_SHAPE (bf16 ring), BAD_STATE (no scales given and no scale arrays attached),
+ * MISALIGNED, UNSUPPORTED_ARCH, CUDA.
+ */
+int sdvg_cache_read_block_e4m3(const sdvg_cache* cache, int slot, const float* k_descale, const float* v_descale, void* k_out,
+                               void* v_out, void* stream);
+
 /* ---- 8-bit rows and weights: the dense operators on E4M3 matrices ------------------- */
 /*
  * A matrix of E4M3 codes (as above) with POWER-OF-TWO SCALES, one per block of 128 columns and 1 row (activations) or 128 rows

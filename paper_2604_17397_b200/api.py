@@ -93,6 +93,12 @@ SIGNATURES = {
                              _I64, _I, _F, _VP, _I64, _I, _I, _I, _VP]),
     "sdvg_qk_norm_rope3d_commit": (_I, [_VP, _VP, _I64, _VP, _I64, _VP, _I64, _VP, _VP, _I, _F, _VP, _VP, _I, _I, _I, _I,
                                         _VP, _I, _I64, _I, C.POINTER(_I64), _VP]),
+    "sdvg_qk_norm_rope3d_commit_e4m3": (_I, [_VP, _VP, _I64, _VP, _I64, _VP, _I64, _VP, _VP, _I, _F, _VP, _VP, _VP, _VP, _I, _I, _I,
+                                             _I, _VP, _I, _I64, _I, C.POINTER(_I64), _VP]),
+    "sdvg_qk_norm_workspace_bytes": (_SZ, [_I]),
+    "sdvg_qk_norm_rope3d_commit_e4m3_tiled": (_I, [_VP, _VP, _I64, _VP, _I64, _VP, _I64, _VP, _VP, _I, _F, _VP, _VP, _I, _I, _I, _I,
+                                                   _VP, _I, _I64, _I, C.POINTER(_I64), _VP, _SZ, _VP]),
+    "sdvg_cache_read_block_e4m3": (_I, [_VP, _I, _VP, _VP, _VP, _VP, _VP]),
     "sdvg_quant_e4m3_blocks": (_I, [_VP, _I64, _I, _VP, _I64, _VP, _I64, _I, _I, _I, _VP]),
     "sdvg_dequant_e4m3_blocks": (_I, [_VP, _I64, _VP, _I64, _I, _VP, _I64, _I, _I, _I, _VP]),
     "sdvg_gated_norm_e4m3": (_I, [_VP, _I64, _I, _VP, _I64, _I, _I, _VP, _VP, _I64, _I, _VP, _I64, _I, _VP, _VP, _VP, _VP,
@@ -730,6 +736,68 @@ def sdvg_qk_norm_rope3d_commit(cache: Cache, q, k, v, q_weight, k_weight, scope:
     if evicted < -1:
         raise SdvgError(-1000 - evicted, "sdvg_qk_norm_rope3d_commit")
     return evicted
+
+
+def _qk_norm_e4m3(call, name, cache, q, k, v, q_weight, k_weight, scope, eps, q8_out, grid, frame_offset, table, tab_frames,
+                  block_index, flags, stream, more):
+    dev = cache._k_raw.get_device()
+    if _elsewhere(dev):
+        with torch.cuda.device(dev):
+            return _qk_norm_e4m3(call, name, cache, q, k, v, q_weight, k_weight, scope, eps, q8_out, grid, frame_offset, table,
+                                 tab_frames, block_index, flags, stream, more)
+    if k.get_device() != dev:
+        raise ValueError("k must be on the cache's device")
+    frames, grid_h, grid_w = grid
+    evicted = call(cache.handle.value or 0, cache.block_tokens, cache.heads, cache.head_dim, q, k, v, q_weight, k_weight, scope,
+                   eps, q8_out, None, frames, grid_h, grid_w, frame_offset, table, tab_frames, block_index, flags,
+                   _raw_stream(dev, stream), *more)
+    if evicted < -1:
+        raise SdvgError(-1000 - evicted, name)
+    return evicted
+
+
+def sdvg_qk_norm_rope3d_commit_e4m3(cache: Cache, q, k, v, q_weight, k_weight, scope: int, eps: float, q8_out, q_inv_scale,
+                                    k_inv_scale, v_inv_scale, grid, frame_offset: int, table, tab_frames: int, block_index: int,
+                                    flags: int, stream=None) -> int:
+    """sdvg_qk_norm_rope3d_commit into an 8-bit ring with static scales: q8_out uint8 codes, inverse scales fp32 [heads]; no rounding
+    before the one to 8 bits.  Returns the evicted block."""
+    return _qk_norm_e4m3(_binding().qk_norm_e4m3, "sdvg_qk_norm_rope3d_commit_e4m3", cache, q, k, v, q_weight, k_weight, scope, eps,
+                         q8_out, grid, frame_offset, table, tab_frames, block_index, flags, stream,
+                         (q_inv_scale, k_inv_scale, v_inv_scale))
+
+
+def qk_norm_workspace(block_tokens: int, device="cuda") -> torch.Tensor:
+    """A workspace of sdvg_qk_norm_rope3d_commit_e4m3_tiled for blocks of this many tokens."""
+    n = lib().sdvg_qk_norm_workspace_bytes(block_tokens)
+    raw = torch.empty(n + 256, dtype=torch.uint8, device=device)
+    off = (-raw.data_ptr()) % 256
+    return raw[off:off + n]
+
+
+def sdvg_qk_norm_rope3d_commit_e4m3_tiled(cache: Cache, q, k, v, q_weight, k_weight, scope: int, eps: float, q8_out, q_tile_scale,
+                                          grid, frame_offset: int, table, tab_frames: int, block_index: int, flags: int,
+                                          workspace=None, stream=None) -> int:
+    """The same into a ring with tile scales: q8_out and q_tile_scale (fp32 [heads, tiles]) receive q; ``workspace`` (of
+    ``qk_norm_workspace``) is needed with SDVG_SCOPE_ROW.  Returns the evicted block."""
+    return _qk_norm_e4m3(_binding().qk_norm_e4m3_tiled, "sdvg_qk_norm_rope3d_commit_e4m3_tiled", cache, q, k, v, q_weight, k_weight,
+                         scope, eps, q8_out, grid, frame_offset, table, tab_frames, block_index, flags, stream,
+                         (q_tile_scale, workspace))
+
+
+def sdvg_cache_read_block_e4m3(cache: Cache, slot: int, k_out, v_out, k_descale=None, v_descale=None, stream=None) -> None:
+    """The values that a slot of an 8-bit ring holds, bf16 [tokens, heads, 128] (k_out or v_out may be None).  Scales fp32 [heads] for a
+    ring with static ones; without them the ring's tile scales."""
+    dev = cache._k_raw.get_device()
+    if dev >= 0 and _elsewhere(dev):
+        with torch.cuda.device(dev):
+            return sdvg_cache_read_block_e4m3(cache, slot, k_out, v_out, k_descale, v_descale, stream)
+    shape = (cache.block_tokens, cache.heads, cache.head_dim)
+    for t in (k_out, v_out, k_descale, v_descale):
+        if t is not None and t.get_device() != dev:
+            raise ValueError("on another device than the ring")
+    sc = lambda t: None if t is None else _scales(t, cache.heads)
+    _check(lib().sdvg_cache_read_block_e4m3(cache.handle, slot, sc(k_descale), sc(v_descale), _bf16(k_out, shape), _bf16(v_out, shape),
+                                            _raw_stream(dev, stream)), "sdvg_cache_read_block_e4m3")
 
 
 # ---------------------------------------------------------------- 8-bit rows and weights

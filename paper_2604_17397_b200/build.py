@@ -11,7 +11,8 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB_PATH = os.path.join(HERE, "libsdvg.so")
 SOURCES = ["sdvg_host.cu", "rope_commit.cu", "route.cu", "state.cu", "quant.cu", "steps.cu", "attn_fwd.cu",
-           "linear.cu", "gated_norm.cu", "qk_norm.cu", "linear_e4m3.cu", "e4m3_blocks.cu"]
+           "linear.cu", "gated_norm.cu", "qk_norm.cu", "linear_e4m3.cu", "e4m3_blocks.cu",
+           "qk_norm_tiled.cu", "ring_read.cu"]
 BINDING_PATH = os.path.join(HERE, "_binding.so")
 
 

@@ -275,8 +275,13 @@ PyObject* gated_norm(PyObject*, PyObject* const* args, Py_ssize_t n) {
 
 // (handle, block_tokens, heads, head_dim, q, k, v, q_weight, k_weight, scope, eps, q_out, k_out, frames, grid_h, grid_w,
 // frame_offset, table, tab_frames, block_index, flags, stream) -> evicted block, or -1000 - status
+// For an 8-bit ring q_out is codes and k_out None, and further arguments follow: (q_inv_scale, k_inv_scale, v_inv_scale) with static
+// scales, (q_tile_scale, workspace) with tile scales.
+enum Ring { kBf16, kStatic, kTiled };
+template <Ring RING>
 PyObject* qk_norm(PyObject*, PyObject* const* args, Py_ssize_t n) {
-  if (n != 22) return PyErr_Format(PyExc_TypeError, "qk_norm takes 22 arguments");
+  constexpr int kArgs = RING == kBf16 ? 22 : RING == kStatic ? 25 : 24;
+  if (n != kArgs) return PyErr_Format(PyExc_TypeError, "qk_norm takes %d arguments", kArgs);
   Reader r{args};
   sdvg_cache* cache = static_cast<sdvg_cache*>(r.address(0));
   const int64_t tokens = r.integer(1), heads = r.integer(2), dim = r.integer(3);
@@ -284,14 +289,13 @@ PyObject* qk_norm(PyObject*, PyObject* const* args, Py_ssize_t n) {
   const int64_t width = scope == SDVG_SCOPE_ROW ? heads * dim : dim;
   const float eps = r.number(10);
   // [tokens, heads, dim], contiguous within a token
-  auto block = [&](int i, const char* what, bool optional, bool contiguous) {
+  auto block = [&](int i, const char* what, bool optional, bool contiguous, ScalarType type = ScalarType::BFloat16) {
     Matrix m;
     const Tensor* t = r.tensor(i, what, optional);
     if (!t) return m;
-    if (t->scalar_type() != ScalarType::BFloat16 || t->dim() != 3 || t->size(0) != tokens || t->size(1) != heads ||
-        t->size(2) != dim) {
-      PyErr_Format(PyExc_ValueError, "%s: expected bfloat16 [%lld, %lld, %lld]", what, (long long)tokens, (long long)heads,
-                   (long long)dim);
+    if (t->scalar_type() != type || t->dim() != 3 || t->size(0) != tokens || t->size(1) != heads || t->size(2) != dim) {
+      PyErr_Format(PyExc_ValueError, "%s: expected %s [%lld, %lld, %lld]", what, type == ScalarType::Byte ? "uint8" : "bfloat16",
+                   (long long)tokens, (long long)heads, (long long)dim);
       r.ok = false;
       return m;
     }
@@ -302,7 +306,8 @@ PyObject* qk_norm(PyObject*, PyObject* const* args, Py_ssize_t n) {
     return m;
   };
   const Matrix k = block(5, "k", false, false), q = block(4, "q", true, false), v = block(6, "v", false, false),
-               q_out = block(11, "q_out", true, true), k_out = block(12, "k_out", true, true);
+               q_out = block(11, "q_out", true, true, RING == kBf16 ? ScalarType::BFloat16 : ScalarType::Byte),
+               k_out = RING == kBf16 ? block(12, "k_out", true, true) : Matrix();
   const float *qw = vector(r, 7, width, "q_weight"), *kw = vector(r, 8, width, "k_weight");
   const int frames = r.small(13), grid_h = r.small(14), grid_w = r.small(15), offset = r.small(16), tab_frames = r.small(18),
             flags = r.small(20);
@@ -314,13 +319,38 @@ PyObject* qk_norm(PyObject*, PyObject* const* args, Py_ssize_t n) {
     r.fail("table", "shorter than that of the block's grid and tab_frames");
   const int64_t index = r.integer(19);
   void* stream = r.address(21);
+  const float *q_inv = nullptr, *k_inv = nullptr, *v_inv = nullptr;
+  Matrix q_scale;
+  void* space = nullptr;
+  size_t space_bytes = 0;
+  if (RING == kStatic) {
+    q_inv = vector(r, 22, heads, "q_inv_scale");
+    k_inv = vector(r, 23, heads, "k_inv_scale");
+    v_inv = vector(r, 24, heads, "v_inv_scale");
+  } else if (RING == kTiled) {
+    const int64_t tiles = (tokens + 127) / 128;
+    q_scale = matrix(r, r.tensor(22, "q_tile_scale", true), heads, tiles, ScalarType::Float, "q_tile_scale");
+    if (r.ok && q_scale.p && heads > 1 && q_scale.ld != tiles) r.fail("q_tile_scale", "must be contiguous");
+    if (const Tensor* t = r.tensor(23, "workspace", true)) {
+      space = t->data_ptr();
+      space_bytes = t->nbytes();
+    }
+  }
   if (!r.ok) return nullptr;
   const float* const tab = static_cast<const float*>(table->data_ptr());      // may throw: before the lock is released
   int64_t evicted = -1;
   int st;
   Py_BEGIN_ALLOW_THREADS
-  st = sdvg_qk_norm_rope3d_commit(cache, q.p, q.ld, k.p, k.ld, v.p, v.ld, qw, kw, scope, eps, q_out.p, k_out.p, frames, grid_h,
-                                  grid_w, offset, tab, tab_frames, index, flags, &evicted, stream);
+  if (RING == kBf16)
+    st = sdvg_qk_norm_rope3d_commit(cache, q.p, q.ld, k.p, k.ld, v.p, v.ld, qw, kw, scope, eps, q_out.p, k_out.p, frames, grid_h,
+                                    grid_w, offset, tab, tab_frames, index, flags, &evicted, stream);
+  else if (RING == kStatic)
+    st = sdvg_qk_norm_rope3d_commit_e4m3(cache, q.p, q.ld, k.p, k.ld, v.p, v.ld, qw, kw, scope, eps, q_out.p, q_inv, k_inv, v_inv,
+                                         frames, grid_h, grid_w, offset, tab, tab_frames, index, flags, &evicted, stream);
+  else
+    st = sdvg_qk_norm_rope3d_commit_e4m3_tiled(cache, q.p, q.ld, k.p, k.ld, v.p, v.ld, qw, kw, scope, eps, q_out.p,
+                                               static_cast<float*>(q_scale.p), frames, grid_h, grid_w, offset, tab, tab_frames, index,
+                                               flags, &evicted, space, space_bytes, stream);
   Py_END_ALLOW_THREADS
   return PyLong_FromLongLong(st == SDVG_OK ? evicted : -1000 - st);
 }
@@ -341,7 +371,8 @@ PyMethodDef method(const char* name) {
   return {name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(guarded<F>)), METH_FASTCALL, nullptr};
 }
 
-PyMethodDef methods[] = {method<linear>("linear"), method<gated_norm<false>>("gated_norm"), method<qk_norm>("qk_norm"),
+PyMethodDef methods[] = {method<linear>("linear"), method<gated_norm<false>>("gated_norm"), method<qk_norm<kBf16>>("qk_norm"),
+                         method<qk_norm<kStatic>>("qk_norm_e4m3"), method<qk_norm<kTiled>>("qk_norm_e4m3_tiled"),
                          method<linear_e4m3>("linear_e4m3"), method<gated_norm<true>>("gated_norm_e4m3"), method<e4m3_blocks>("e4m3_blocks"),
                          {nullptr, nullptr, 0, nullptr}};
 

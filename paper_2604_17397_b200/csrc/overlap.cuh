@@ -17,10 +17,10 @@ __device__ __forceinline__ void overlap_wait() { cudaGridDependencySynchronize()
 
 // cluster: CTAs per cluster where the kernel does not fix it itself, else 0.
 template <class Params>
-cudaError_t launch_overlapped(void (*kernel)(Params), unsigned grid, int threads, size_t dynamic_bytes, int cluster,
+cudaError_t launch_overlapped(void (*kernel)(Params), dim3 grid, int threads, size_t dynamic_bytes, int cluster,
                               cudaStream_t stream, const Params& params) {
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(grid);
+  cfg.gridDim = grid;
   cfg.blockDim = dim3(threads);
   cfg.dynamicSmemBytes = dynamic_bytes;
   cfg.stream = stream;

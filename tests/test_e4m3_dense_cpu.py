@@ -181,3 +181,90 @@ def test_special_values():
     codes, s = B.quantise(x, 1)
     assert s.tolist() == [[1, 247, 1]] and codes[0, 0] == 0x7F and codes[0, 128] == 0x7E and codes[0, 129] == 0
     assert O.e4m3_tile_scale_exponent(0.0) == -126
+
+
+# ---- ring write and read-back ---------------------------------------------------------------------------
+
+@pytest.fixture
+def rings(lib):
+    """(static, tiled, bf16, too wide) with 2 heads (129) and 64 tokens."""
+    import ctypes as C
+    made = []
+    for heads, e4m3, tiles in ((2, True, False), (2, True, True), (2, False, False), (129, True, True)):
+        h = C.c_void_p()
+        create = lib.sdvg_cache_create_e4m3 if e4m3 else lib.sdvg_cache_create
+        assert create(C.byref(h), 0x10000, 0x20000, 3, heads, 64, 128) == api.SDVG_OK
+        if tiles:
+            assert lib.sdvg_cache_set_tile_scales(h, 0x30000, 0x40000) == api.SDVG_OK
+        made.append(h)
+    yield made
+    for h in made:
+        lib.sdvg_cache_destroy(h)
+
+
+def test_qk_norm_refuses_on_the_host(lib, rings):
+    static, tiled, bf16, wide = rings
+    base = dict(cache=None, q=X, ld_q=256, k=W, ld_k=256, v=B_, ld_v=768, q_weight=G, k_weight=None, scope=0, eps=1e-6, q8=OUT)
+    pos = dict(frames=1, grid_h=8, grid_w=8, frame_offset=0, tab=0x80000, tab_frames=4, block=0, flags=api.SDVG_STAGE, evicted=None)
+    calls = {"static": ({**base, "cache": static, "qi": XS, "ki": XS, "vi": XS, **pos, "stream": None}, lib.sdvg_qk_norm_rope3d_commit_e4m3),
+             "tiled": ({**base, "cache": tiled, "qs": XS, **pos, "ws": 0x90000, "ws_bytes": 256 + 64 * 8, "stream": None},
+                       lib.sdvg_qk_norm_rope3d_commit_e4m3_tiled)}
+    shared = [
+        (dict(cache=None), "INVALID_ARG"), (dict(k=None), "INVALID_ARG"), (dict(v=None), "INVALID_ARG"), (dict(q=None), "INVALID_ARG"),
+        (dict(q8=None), "INVALID_ARG"), (dict(scope=2), "INVALID_ARG"), (dict(eps=-1.0), "INVALID_ARG"), (dict(eps=float("nan")), "INVALID_ARG"),
+        (dict(tab=None), "INVALID_ARG"), (dict(flags=3), "INVALID_ARG"), (dict(cache=bf16), "BAD_SHAPE"), (dict(ld_q=248), "BAD_SHAPE"),
+        (dict(ld_k=128), "BAD_SHAPE"), (dict(ld_v=0), "BAD_SHAPE"), (dict(grid_w=7), "BAD_SHAPE"),
+        (dict(cache=wide, ld_q=20000, ld_k=20000, ld_v=20000), "BAD_SHAPE"), (dict(ld_k=260), "MISALIGNED"), (dict(q=X + 8), "MISALIGNED"),
+        (dict(q_weight=G + 4), "MISALIGNED"), (dict(q8=OUT + 2), "MISALIGNED"), (dict(block=1), "BAD_STATE"), (dict(frame_offset=4), "BAD_STATE"),
+        (dict(tab_frames=1 << 30), "BAD_SHAPE")]
+    own = {"static": [(dict(ki=None), "INVALID_ARG"), (dict(vi=None), "INVALID_ARG"), (dict(qi=None), "INVALID_ARG"), (dict(ki=XS + 2), "MISALIGNED")],
+           "tiled": [(dict(qs=None), "INVALID_ARG"), (dict(qs=XS + 2), "MISALIGNED"), (dict(cache=static), "BAD_STATE"),
+                     (dict(ws=None), "INVALID_ARG"), (dict(ws_bytes=256 + 64 * 8 - 1), "INVALID_ARG"), (dict(ws=0x90010), "MISALIGNED")]}
+    for kind, (args, call) in calls.items():
+        for change, status in shared + own[kind]:
+            assert set(change) <= set(args)
+            assert call(*{**args, **change}.values()) == getattr(api, "SDVG_ERR_" + status), (kind, change)
+    assert lib.sdvg_qk_norm_workspace_bytes(0) == 0 and lib.sdvg_qk_norm_workspace_bytes(4680) == 256 + 8 * 4680
+
+
+def test_read_back_refuses_on_the_host(lib, rings):
+    static, tiled, bf16, _ = rings
+    f = lib.sdvg_cache_read_block_e4m3
+    for args, status in [((None, 0, XS, XS, OUT, OS), "INVALID_ARG"), ((static, 0, XS, XS, None, None), "INVALID_ARG"),
+                         ((static, 3, XS, XS, OUT, OS), "INVALID_ARG"), ((static, -1, XS, XS, OUT, OS), "INVALID_ARG"),
+                         ((static, 0, XS, None, OUT, OS), "INVALID_ARG"), ((static, 0, None, XS, OUT, None), "INVALID_ARG"),
+                         ((static, 0, None, None, OUT, OS), "BAD_STATE"), ((bf16, 0, XS, XS, OUT, OS), "BAD_SHAPE"),
+                         ((tiled, 0, None, None, OUT + 8, OS), "MISALIGNED"), ((static, 0, XS + 1, XS, OUT, OS), "MISALIGNED")]:
+        assert f(*args, None) == getattr(api, "SDVG_ERR_" + status), args
+
+
+def test_the_binding_of_the_ring_writes(lib, rings):
+    static, tiled, _, _ = rings
+    block = lambda *shape: OnPaper(*(shape or (64, 2, 128)))
+    n = lib.sdvg_rope3d_table_floats(128, 4, 8, 8)
+    f32 = lambda *shape: OnPaper(*shape, dtype=torch.float32)
+
+    def call(ring, fn, more, **change):
+        a = dict(handle=ring.value, tokens=64, heads=2, dim=128, q=block(), k=block(), v=block(), q_weight=None, k_weight=None, scope=0,
+                 eps=1e-6, q8=u8(64, 2, 128), k_out=None, frames=1, grid_h=8, grid_w=8, offset=0, table=f32(n), tab_frames=4, block=0,
+                 flags=api.SDVG_STAGE, stream=0)
+        assert set(change) <= set(a)
+        return fn(*{**a, **change}.values(), *more)
+
+    b, reached = api._binding(), -1000 - api.SDVG_ERR_INVALID_ARG
+    inv = (f32(2), f32(2), f32(2))
+    scales = (f32(2, 1), u8(256 + 64 * 8))
+    assert call(static, b.qk_norm_e4m3, inv) == call(tiled, b.qk_norm_e4m3_tiled, scales) == reached
+    assert call(static, b.qk_norm_e4m3, inv, q=None, q8=None) == call(tiled, b.qk_norm_e4m3_tiled, (None, None)) == reached
+    for ring, fn, more in ((static, b.qk_norm_e4m3, inv), (tiled, b.qk_norm_e4m3_tiled, scales)):
+        for change in (dict(q8=block()), dict(q8=u8(64, 2, 64)), dict(k=u8(64, 2, 128)), dict(table=f32(n - 1)), dict(q_weight=f32(255))):
+            with pytest.raises(ValueError):
+                call(ring, fn, more, **change)
+        with pytest.raises(TypeError):
+            fn()
+    for more in ((f32(3), f32(2), f32(2)), (f32(2), f32(2), block()), (f32(2), f32(2, 1), f32(2))):
+        with pytest.raises(ValueError):
+            call(static, b.qk_norm_e4m3, more)
+    for more in ((f32(2, 2), None), (f32(1, 2), None), (u8(2, 1), None), (f32(2, 1), 5)):
+        with pytest.raises(ValueError):
+            call(tiled, b.qk_norm_e4m3_tiled, more)
