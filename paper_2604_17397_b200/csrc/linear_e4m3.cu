@@ -79,7 +79,7 @@ __device__ __forceinline__ void stage_scales(uint4* to, const uint8_t* scale, lo
 // fp32 outputs: the tensor core adds products to the accumulator by truncation, so a long sum drifts; there it is cut into chunks
 // that are added with round-to-nearest, as in linear.cu.  A step of the 8-bit kind adds 32 products, twice those of the 16-bit
 // kind, so that chunks are twice as long for the same drift.
-constexpr int kPairChunkIters = 1280 / kTileK;
+constexpr int kPairChunkIters = 2560 / kTileK;
 constexpr int kTileChunkIters = 512 / kTileK;
 
 // ---- 8-bit outputs ------------------------------------------------------------------------------
@@ -346,34 +346,49 @@ __global__ void __launch_bounds__(kTileThreads) linear8_tile_kernel(const __grid
 
 // ---- many tokens: CTA pairs, persistent ---------------------------------------------------------
 //
-// As in linear.cu: a tile is 256 features x tile_t tokens on two SMs, one tcgen05.mma of the even CTA reads the operands of
-// both.  Each CTA's tensor memory holds the scales of its own features and of all the tile's tokens; the even CTA's copy moves
-// both CTAs' words at once.  The last 32 columns of tensor memory are the scales' (two words in turn), which leaves
-// accumulators of 240 columns for two tiles in flight.
-constexpr int kEpiWarps = 8;
+// A pair of CTAs (two SMs) works on a tile of SUBS x 256 features x tile_t tokens: each CTA holds SUBS x 128 of the features and fetches half
+// of the token tile, and one tcgen05.mma of the even CTA reads the operands of both.  Each CTA's tensor memory holds the
+// scales of its own features and of all the tile's tokens; the even CTA's copy moves both CTAs' words at once.
+//
+// What bounds it is how fast operand tiles come from L2: an SM gets 41 to 46 bytes a clock (measured with the products left out),
+// while its tensor core, twice as fast on a byte as on a half, would take 66 with tiles of 256 x 240.  So where there are
+// features enough a CTA takes 256 of them (SUBS = 2), which share each token tile: 50 bytes a clock.  The two accumulators
+// of 240 columns then belong to one tile, and the next tile cannot run under its epilogue.  What hides most of that: at
+// a tile's end the first half's last kSkew stages are multiplied before the second half's, and at its begin again, so that
+// one half's epilogue runs under the other's products; and operands of the next tile arrive meanwhile.
+// With SUBS = 1 the two accumulators belong to neighbouring tiles, and the epilogue of one runs under the products of the next.
+// The last 32 columns of tensor memory are the scales' (two words in turn).
+constexpr int kEpiWarps = 16;
 constexpr int kPairThreads = 32 * (kEpiWarps + 3);
-constexpr int kPairSlotBytes = 512 + 1024;           // a word of scales of the CTA's features, and of the tile's tokens
-constexpr int kPairSmem = 227 * 1024 - 2048;         // dynamic shared memory of a CTA; the barriers and exchanges are static
-constexpr int kMaxTileT = 240, kMaxTileChunked = 112;
+constexpr int kPairSmem = 227 * 1024 - 3072;         // dynamic shared memory of a CTA; the barriers and exchanges are static
+constexpr int kMaxTileT = 240, kMaxTileChunked = 160;
 constexpr int kScaleCol = 480, kPairScaleCols = 16;
-template <int OutType>
-constexpr int kAccs = OutType == SDVG_F32 ? 3 : 2;
+constexpr int kAccs = 2;
+constexpr int kSkew = 3;
 template <int OutType>
 constexpr int kAccStride = OutType == SDVG_F32 ? kMaxTileChunked : kMaxTileT;
-static_assert((kAccs<SDVG_F32> + 1) * kAccStride<SDVG_F32> <= kScaleCol && kAccs<SDVG_BF16> * kAccStride<SDVG_BF16> <= kScaleCol);
+// A chunked sum has its total behind the accumulators.
+static_assert((kAccs + 1) * kAccStride<SDVG_F32> <= kScaleCol && kAccs * kAccStride<SDVG_BF16> <= kScaleCol);
 static_assert(kScaleCol + 2 * kPairScaleCols <= 512);
 
+// A word of scales of the CTA's features, and of the tile's tokens.
+template <int SUBS>
+constexpr int kPairSlotBytes = SUBS * 512 + 1024;
+template <int SUBS>
+__host__ __device__ constexpr int pair_stage_bytes(int tile_t) { return SUBS * kTileF * 128 + tile_t * 64; }
+
 struct PairSmem {
-  uint64_t full[kMaxStages], empty[kMaxStages], sf_full[kScaleSlots], sf_empty[kScaleSlots], acc_full[3], acc_empty[3];
-  Exchange exchange[2];
+  uint64_t full[kMaxStages], empty[kMaxStages], sf_full[kScaleSlots], sf_empty[kScaleSlots], acc_full[kAccs], acc_empty[kAccs];
+  Exchange exchange[kEpiWarps / 4];
   uint32_t tmem;
 };
-static_assert(sizeof(PairSmem) <= 2048 - 512);
+static_assert(sizeof(PairSmem) <= 3072 - 512);
 
-template <int OutType>
+template <int OutType, int SUBS>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
     linear8_pair_kernel(const __grid_constant__ Linear8Params p) {
   constexpr bool kChunked = OutType == SDVG_F32, kOut8 = OutType == SDVG_E4M3;
+  static_assert(!kChunked || SUBS == 1);
   using T = typename OutElem<OutType>::T;
   extern __shared__ uint8_t raw[];
   __shared__ PairSmem sm;
@@ -381,7 +396,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
   const uint32_t rank = cluster_ctarank();
   const int pair = blockIdx.x / 2, pairs = gridDim.x / 2;
-  const int w_bytes = kTileF * 128, stage_bytes = w_bytes + p.tile_t * 64;
+  constexpr int kFeatures = SUBS * kTileF, w_bytes = kFeatures * 128;  // of a CTA
+  const int stage_bytes = pair_stage_bytes<SUBS>(p.tile_t);
   uint8_t* slots = buf + p.stages * stage_bytes;
   const int chunks = kChunked ? (p.k_iters + kPairChunkIters - 1) / kPairChunkIters : 1;
   const int words = (p.k_iters + kWordStages - 1) / kWordStages;
@@ -395,11 +411,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
       mbar_init(&sm.sf_full[s], 2);                  // the even CTA's: the scale warps of both
       mbar_init(&sm.sf_empty[s], 1);
     }
-    for (int b = 0; b < kAccs<OutType>; ++b) {
+    for (int b = 0; b < kAccs; ++b) {
       mbar_init(&sm.acc_full[b], 1);
       mbar_init(&sm.acc_empty[b], 2 * kEpiWarps);    // the even CTA's: the epilogue warps of both
     }
-    for (int h = 0; h < 2; ++h) mbar_init(&sm.exchange[h].bar, 4);
+    for (int g = 0; g < kEpiWarps / 4; ++g) mbar_init(&sm.exchange[g].bar, 4);
     fence_mbar_init();
     prefetch_tmap(&p.w_map);
     prefetch_tmap(&p.x_map);
@@ -425,7 +441,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
       for (long long t = pair; ok && t < p.tiles; t += pairs) {
         int ft, tt;
         tile_of(p, t, &ft, &tt);
-        const int n0 = (2 * ft + (int)rank) * kTileF, m0 = tt * p.tile_t + (int)rank * (p.tile_t / 2);
+        const int n0 = (2 * ft + (int)rank) * kFeatures, m0 = tt * p.tile_t + (int)rank * (p.tile_t / 2);
         for (int i = 0; i < p.k_iters; ++i, r.next(p.stages)) {
           const int s = r.stage;
           if (!(ok = wait_for(&sm.empty[s], r.phase ^ 1, p.status, kWaitLimitNs))) break;
@@ -447,40 +463,78 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
   } else if (warp == kEpiWarps + 1) {
     // ================= issuer: the even CTA, for both ==============================================
     if (rank == 0 && elect_one()) {
-      RingPos r, acc, sf;
-      uint32_t scales = 0;
+      RingPos sf;
+      int word_slot = 0;                             // words copied so far: two places of tensor memory in turn
+      // a stage's operands are there, and its scales, whose word is copied when its first stage comes
+      auto arrived = [&](int i, const RingPos& r) {
+        if (i % kWordStages == 0) {
+          if (!wait_for(&sm.sf_full[sf.stage], sf.phase, p.status, kWaitLimitNs)) return false;
+          tc_fence_after();
+          const uint32_t to = tmem + kScaleCol + (word_slot & 1) * kPairScaleCols;
+          const uint32_t from = smem_u32(slots + sf.stage * kPairSlotBytes<SUBS>);
+#pragma unroll
+          for (int g = 0; g < SUBS; ++g) tmem_cp_scales_pair(to + 4 * g, from + 512 * g);
+          tmem_cp_scales_pair(to + 4 * SUBS, from + 512 * SUBS);
+          if (p.tile_t > 128) tmem_cp_scales_pair(to + 4 * SUBS + 4, from + 512 * SUBS + 512);
+          mma_commit_pair(&sm.sf_empty[sf.stage]);
+          sf.next(kScaleSlots);
+          ++word_slot;
+        }
+        if (!wait_for(&sm.full[r.stage], r.phase, p.status, kWaitLimitNs)) return false;
+        tc_fence_after();
+        return true;
+      };
+      // the products of stage i of half `sub` into accumulator b; `behind`: words copied after this stage's
+      auto multiply = [&](int i, const RingPos& r, int sub, int b, bool onto, int behind) {
+        const uint32_t st = smem_u32(buf + r.stage * stage_bytes);
+        const uint64_t da = smem_desc_sw128(st + sub * kTileF * 128, 16, 1024), db = smem_desc_sw128(st + w_bytes, 16, 1024);
+        const uint32_t idesc = p.idesc | idesc_scale_step(i % kWordStages);
+        const uint32_t scales = tmem + kScaleCol + ((word_slot - 1 - behind) & 1) * kPairScaleCols;
+#pragma unroll
+        for (int kk = 0; kk < 4; ++kk)
+          mma_ss_mx_pair(tmem + b * kAccStride<OutType>, da + 2 * kk, db + 2 * kk, idesc, scales + 4 * sub, scales + 4 * SUBS, onto || kk > 0);
+      };
+      RingPos r, acc;
       bool ok = true;
       for (long long t = pair; ok && t < p.tiles; t += pairs) {
-        for (int c = 0; ok && c < chunks; ++c, acc.next(kAccs<OutType>)) {
-          const int b = acc.stage;
-          if (!(ok = wait_for(&sm.acc_empty[b], acc.phase ^ 1, p.status, kWaitLimitNs))) break;
-          tc_fence_after();
-          const int i0 = c * kPairChunkIters, i1 = kChunked ? min(p.k_iters, i0 + kPairChunkIters) : p.k_iters;
-          for (int i = i0; i < i1; ++i, r.next(p.stages)) {
-            const int s = r.stage;
-            if (i % kWordStages == 0) {
-              if (!(ok = wait_for(&sm.sf_full[sf.stage], sf.phase, p.status, kWaitLimitNs))) break;
-              tc_fence_after();
-              // two places in turn: the products of the word before may still read theirs
-              scales = tmem + kScaleCol + (sf.stage & 1) * kPairScaleCols;
-              const uint32_t from = smem_u32(slots + sf.stage * kPairSlotBytes);
-              tmem_cp_scales_pair(scales, from);
-              tmem_cp_scales_pair(scales + 4, from + 512);
-              if (p.tile_t > 128) tmem_cp_scales_pair(scales + 8, from + 1024);
-              mma_commit_pair(&sm.sf_empty[sf.stage]);
-              sf.next(kScaleSlots);
+        if constexpr (SUBS == 1) {
+          for (int c = 0; ok && c < chunks; ++c, acc.next(kAccs)) {
+            if (!(ok = wait_for(&sm.acc_empty[acc.stage], acc.phase ^ 1, p.status, kWaitLimitNs))) break;
+            const int i0 = c * kPairChunkIters, i1 = kChunked ? min(p.k_iters, i0 + kPairChunkIters) : p.k_iters;
+            for (int i = i0; i < i1; ++i, r.next(p.stages)) {
+              if (!(ok = arrived(i, r))) break;
+              multiply(i, r, 0, acc.stage, i > i0, 0);
+              mma_commit_pair(&sm.empty[r.stage]);
             }
-            if (!(ok = wait_for(&sm.full[s], r.phase, p.status, kWaitLimitNs))) break;
-            tc_fence_after();
-            const uint32_t st = smem_u32(buf + s * stage_bytes);
-            const uint64_t da = smem_desc_sw128(st, 16, 1024), db = smem_desc_sw128(st + w_bytes, 16, 1024);
-            const uint32_t idesc = p.idesc | idesc_scale_step(i % kWordStages);
-#pragma unroll
-            for (int kk = 0; kk < 4; ++kk)
-              mma_ss_mx_pair(tmem + b * kAccStride<OutType>, da + 2 * kk, db + 2 * kk, idesc, scales, scales + 4, i > i0 || kk > 0);
-            mma_commit_pair(&sm.empty[s]);
+            if (ok) mma_commit_pair(&sm.acc_full[acc.stage]);
           }
-          if (ok) mma_commit_pair(&sm.acc_full[b]);
+        } else {
+          // stages [0, head) and [tail, k_iters) go first through the first half and then through the second
+          const int head = min(kSkew, p.k_iters), tail = max(head, p.k_iters - kSkew);
+          int i = 0;
+          while (ok && i < p.k_iters) {
+            const int run = i == 0 ? head : i < tail ? 1 : p.k_iters - tail;
+            RingPos second = r;
+            if (i == 0 && !(ok = wait_for(&sm.acc_empty[0], acc.phase ^ 1, p.status, kWaitLimitNs))) break;
+            const int words_before = word_slot;
+            for (int k = i; ok && k < i + run; ++k, r.next(p.stages)) {
+              if (!(ok = arrived(k, r))) break;
+              multiply(k, r, 0, 0, k > 0, 0);
+            }
+            if (!ok) break;
+            if (i + run == p.k_iters) mma_commit_pair(&sm.acc_full[0]);
+            if (i == 0 && !(ok = wait_for(&sm.acc_empty[1], acc.phase ^ 1, p.status, kWaitLimitNs))) break;
+            tc_fence_after();
+            // the first stage that begins a word within the run: those before it use the word before
+            const int turn = (i + kWordStages - 1) / kWordStages * kWordStages;
+            for (int k = i; k < i + run; ++k, second.next(p.stages)) {
+              multiply(k, second, 1, 1, k > 0, word_slot != words_before && k < turn ? 1 : 0);
+              mma_commit_pair(&sm.empty[second.stage]);
+            }
+            if (i + run == p.k_iters) mma_commit_pair(&sm.acc_full[1]);
+            i += run;
+          }
+          acc.phase ^= 1;
         }
       }
     }
@@ -492,13 +546,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
     for (long long t = pair; ok && t < p.tiles; t += pairs) {
       int ft, tt;
       tile_of(p, t, &ft, &tt);
-      const int n0 = (2 * ft + (int)rank) * kTileF, m0 = tt * p.tile_t, m_end = min(p.rows, m0 + p.tile_t);
+      const int n0 = (2 * ft + (int)rank) * kFeatures, m0 = tt * p.tile_t, m_end = min(p.rows, m0 + p.tile_t);
       for (int w = 0; w < words; ++w, sf.next(kScaleSlots)) {
         if (!(ok = __all_sync(0xffffffffu, wait_for(&sm.sf_empty[sf.stage], sf.phase ^ 1, p.status, kWaitLimitNs)))) break;
         issued = min(issued + 1, kScaleSlots);
-        uint4* to = reinterpret_cast<uint4*>(slots + sf.stage * kPairSlotBytes);
-        stage_scales<1>(to, p.w_scale, p.ld_ws, p.w_shift, n0, min(p.cols, n0 + kTileF), w, p.k_iters);
-        stage_scales<2>(to + 32, p.x_scale, p.ld_xs, 0, m0, m_end, w, p.k_iters);
+        uint4* to = reinterpret_cast<uint4*>(slots + sf.stage * kPairSlotBytes<SUBS>);
+        stage_scales<SUBS>(to, p.w_scale, p.ld_ws, p.w_shift, n0, min(p.cols, n0 + kFeatures), w, p.k_iters);
+        stage_scales<2>(to + 32 * SUBS, p.x_scale, p.ld_xs, 0, m0, m_end, w, p.k_iters);
         fence_async_smem();
         __syncwarp();
         if (lane == 0) mbar_arrive_cluster(map_to_rank(smem_u32(&sm.sf_full[sf.stage]), 0));
@@ -510,8 +564,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
       ok = __all_sync(0xffffffffu, wait_for(&sm.sf_empty[sf.stage], sf.phase, p.status, kWaitLimitNs));
     }
   } else {
-    // ================= epilogue: warps w and w + 4 share 32 features and take 32-token column blocks in turn ==========
-    const int quad = warp % 4, half = warp / 4;
+    // ================= epilogue: warps w, w + 4, .. share 32 features and take 16-token column blocks in turn ==========
+    const int quad = warp % 4, part = warp / 4;
+    constexpr int kParts = kEpiWarps / 4;
     const uint32_t lanes = tmem + ((uint32_t)(quad * 32) << 16);
     const uint32_t empty = map_to_rank(smem_u32(sm.acc_empty), 0);
     RingPos r;
@@ -520,55 +575,47 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
     for (long long t = pair; ok && t < p.tiles; t += pairs) {
       int ft, tt;
       tile_of(p, t, &ft, &tt);
-      const int n = (2 * ft + (int)rank) * kTileF + quad * 32 + lane;
       const int m0 = tt * p.tile_t, m_end = min(p.rows, m0 + p.tile_t);
-      const float bias = p.bias && n < p.cols ? p.bias[n] : 0.f;
-      // this warp's columns: blocks of 32 from 32 half on, 64 apart, handled as two halves of 16
-      const TileGate gate = tile_gate(p, n, m0, m_end);
-      T ahead0[16], ahead1[16];
-      if (!kOut8) {
-        load_residual16<OutType>(p, ahead0, n, m0 + half * 32, m_end);
-        load_residual16<OutType>(p, ahead1, n, m0 + half * 32 + 16, m_end);
-      }
-      auto release = [&](int stage) {
-        if (lane == 0) mbar_arrive_cluster(empty + 8 * stage);
-      };
-      const bool summed = kChunked && chunks > 1;
-      if (summed)
-        ok = add_chunks<kAccs<OutType>, (kMaxTileChunked + 31) / 32>(
-            chunks, lanes, kAccStride<OutType>, kAccs<OutType> * kAccStride<OutType>,
-            [&](int i) { return (i / 2 * 2 + half) * 32 + (i & 1) * 16; }, m_end - m0, r, sm.acc_full, p.status, release);
-      else
-        ok = __all_sync(0xffffffffu, wait_for(&sm.acc_full[r.stage], r.phase, p.status, kWaitLimitNs));
-      if (!ok) break;
-      tc_fence_after();
-      const uint32_t sums = lanes + (summed ? kAccs<OutType> : r.stage) * kAccStride<OutType>;
 #pragma unroll 1
-      for (int col = half * 32; m0 + col < m_end; col += 64) {
-        float acc0[16], acc1[16];
-        tmem_ld16(sums + col, reinterpret_cast<uint32_t(&)[16]>(acc0));
-        tmem_ld16(sums + col + 16, reinterpret_cast<uint32_t(&)[16]>(acc1));
-        tmem_wait_ld();
-        if constexpr (kOut8) {
-          if (n < p.cols) gated16(p, acc0, n, m0 + col, min(16, m_end - m0 - col), bias, gate);
-          if (!(ok = quantise16(p, sm.exchange[half], turn, acc0, n, quad, m0 + col, m_end))) break;
-          if (m0 + col + 16 < m_end) {
-            if (n < p.cols) gated16(p, acc1, n, m0 + col + 16, min(16, m_end - m0 - col - 16), bias, gate);
-            if (!(ok = quantise16(p, sm.exchange[half], turn, acc1, n, quad, m0 + col + 16, m_end))) break;
+      for (int sub = 0; sub < SUBS; ++sub) {
+        const int n = (2 * ft + (int)rank) * kFeatures + sub * kTileF + quad * 32 + lane;
+        const float bias = p.bias && n < p.cols ? p.bias[n] : 0.f;
+        const TileGate gate = tile_gate(p, n, m0, m_end);
+        T ahead[16];
+        if (!kOut8) load_residual16<OutType>(p, ahead, n, m0 + part * 16, m_end);
+        auto release = [&](int stage) {
+          if (lane == 0) mbar_arrive_cluster(empty + 8 * stage);
+        };
+        const bool summed = kChunked && chunks > 1;
+        if (summed)
+          ok = add_chunks<kAccs, (kMaxTileChunked / 16 + kParts - 1) / kParts>(
+              chunks, lanes, kAccStride<OutType>, kAccs * kAccStride<OutType>, [&](int i) { return (i * kParts + part) * 16; }, m_end - m0, r,
+              sm.acc_full, p.status, release);
+        else
+          ok = __all_sync(0xffffffffu, wait_for(&sm.acc_full[r.stage], r.phase, p.status, kWaitLimitNs));
+        if (!ok) break;
+        tc_fence_after();
+        const uint32_t sums = lanes + (summed ? kAccs : r.stage) * kAccStride<OutType>;
+#pragma unroll 1
+        for (int col = part * 16; m0 + col < m_end; col += 16 * kParts) {
+          float acc[16];
+          tmem_ld16(sums + col, reinterpret_cast<uint32_t(&)[16]>(acc));
+          tmem_wait_ld();
+          if constexpr (kOut8) {
+            if (n < p.cols) gated16(p, acc, n, m0 + col, min(16, m_end - m0 - col), bias, gate);
+            if (!(ok = quantise16(p, sm.exchange[part], turn, acc, n, quad, m0 + col, m_end))) break;
+          } else {
+            epilogue16<OutType>(p, acc, ahead, n, m0 + col, m_end, bias, gate);
+            load_residual16<OutType>(p, ahead, n, m0 + col + 16 * kParts, m_end);
           }
-        } else {
-          epilogue16<OutType>(p, acc0, ahead0, n, m0 + col, m_end, bias, gate);
-          load_residual16<OutType>(p, ahead0, n, m0 + col + 64, m_end);
-          epilogue16<OutType>(p, acc1, ahead1, n, m0 + col + 16, m_end, bias, gate);
-          load_residual16<OutType>(p, ahead1, n, m0 + col + 80, m_end);
         }
-      }
-      if (!ok) break;
-      if (!summed) {
-        tc_fence_before();
-        __syncwarp();
-        release(r.stage);
-        r.next(kAccs<OutType>);
+        if (!ok) break;
+        if (!summed) {
+          tc_fence_before();
+          __syncwarp();
+          release(r.stage);
+          r.next(kAccs);
+        }
       }
     }
   }
@@ -627,6 +674,23 @@ int tile_split(long long tiles, int k_iters, int tile_t, int sms) {
 
 // One-time set-up per device and output type: the opt-in to the kernels' dynamic shared memory, and how many CTA pairs
 // the device runs at once.
+template <int OutType, int SUBS>
+cudaError_t set_up_pair(int* pairs) {
+  cudaError_t e = cudaFuncSetAttribute(linear8_pair_kernel<OutType, SUBS>, cudaFuncAttributeMaxDynamicSharedMemorySize, kPairSmem);
+  if (e != cudaSuccess) return e;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(2);
+  cfg.blockDim = dim3(kPairThreads);
+  cfg.dynamicSmemBytes = kPairSmem;
+  cudaLaunchAttribute attr;
+  attr.id = cudaLaunchAttributeClusterDimension;
+  attr.val.clusterDim.x = 2;
+  attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  return cudaOccupancyMaxActiveClusters(pairs, linear8_pair_kernel<OutType, SUBS>, &cfg);
+}
+
 template <int OutType>
 int set_up(int* pairs) {
   static int pairs_of_device[kMaxDevices] = {};
@@ -638,20 +702,13 @@ int set_up(int* pairs) {
   if (!pairs_of_device[dev]) {
     e = cudaFuncSetAttribute(linear8_tile_kernel<OutType>, cudaFuncAttributeMaxDynamicSharedMemorySize, tile_dynamic(kMaxTileFew));
     if (e != cudaSuccess) return sdvg::cuda_status(e);
-    e = cudaFuncSetAttribute(linear8_pair_kernel<OutType>, cudaFuncAttributeMaxDynamicSharedMemorySize, kPairSmem);
-    if (e != cudaSuccess) return sdvg::cuda_status(e);
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(2);
-    cfg.blockDim = dim3(kPairThreads);
-    cfg.dynamicSmemBytes = kPairSmem;
-    cudaLaunchAttribute attr;
-    attr.id = cudaLaunchAttributeClusterDimension;
-    attr.val.clusterDim.x = 2;
-    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
-    cfg.attrs = &attr;
-    cfg.numAttrs = 1;
     int n = 0;
-    e = cudaOccupancyMaxActiveClusters(&n, linear8_pair_kernel<OutType>, &cfg);
+    e = set_up_pair<OutType, 1>(&n);
+    if constexpr (OutType != SDVG_F32) {
+      int wide = 0;
+      if (e == cudaSuccess) e = set_up_pair<OutType, 2>(&wide);
+      n = std::min(n, wide);
+    }
     if (e != cudaSuccess || n < 1) return sdvg::cuda_status(e != cudaSuccess ? e : cudaErrorUnknown);
     pairs_of_device[dev] = n;
   }
@@ -659,29 +716,66 @@ int set_up(int* pairs) {
   return SDVG_OK;
 }
 
+// Features (SUBS x 256) and tokens of a pair's tile: the sizes whose waves of tiles cost least.  A stage costs the bytes it brings to an
+// SM, those of SUBS x 128 features and half the tokens; a tile's end costs about kTileEnd stages' worth of a token.
+constexpr int kTileEnd = 1500;
+struct PairTile {
+  int subs, tile_t;
+};
+PairTile choose_tile(int rows, int cols, int k_iters, int pairs, bool chunked) {
+  PairTile best{1, 0};
+  long long best_cost = 0;
+  for (int subs = 1; subs <= (chunked ? 1 : 2); ++subs)
+    for (int nt = chunked ? kMaxTileChunked : kMaxTileT; nt >= 64; nt -= 16) {
+      const long long tiles = (long long)((cols + 256 * subs - 1) / (256 * subs)) * ((rows + nt - 1) / nt);
+      const long long cost = (tiles + pairs - 1) / pairs * ((long long)k_iters * (nt + 256 * subs) + kTileEnd * subs);
+      if (!best_cost || cost < best_cost) {
+        best = PairTile{subs, nt};
+        best_cost = cost;
+      }
+    }
+  return best;
+}
+
+template <int OutType, int SUBS>
+int launch_pair(Linear8Params& p, const void* x, int64_t ld_x, const void* w, int64_t ld_w, int inner, int pairs, cudaStream_t stream) {
+  p.tiles_f = (p.cols + 2 * SUBS * kTileF - 1) / (2 * SUBS * kTileF);
+  p.tiles_t = (p.rows + p.tile_t - 1) / p.tile_t;
+  p.tiles = (long long)p.tiles_f * p.tiles_t;
+  if (p.tiles >= 1ll << 28) return SDVG_ERR_BAD_SHAPE;
+  p.idesc = idesc_mx_e4m3(2 * kTileF, p.tile_t);
+  int st = make_map(&p.w_map, w, inner, p.cols, ld_w, SUBS * kTileF);
+  if (st != SDVG_OK) return st;
+  if ((st = make_map(&p.x_map, x, inner, p.rows, ld_x, p.tile_t / 2)) != SDVG_OK) return st;
+  p.group = 8 / SUBS;
+  p.stages = std::min(kMaxStages, (kPairSmem - 1024 - kScaleSlots * kPairSlotBytes<SUBS>) / pair_stage_bytes<SUBS>(p.tile_t));
+  const int grid = 2 * (int)std::min((long long)pairs, p.tiles);
+  return sdvg::cuda_status(
+      sdvg::launch_overlapped(linear8_pair_kernel<OutType, SUBS>, grid, kPairThreads, kPairSmem, 0, stream, p));
+}
+// The skewed stages of both ends are all in the ring at once.
+static_assert((kPairSmem - 1024 - kScaleSlots * kPairSlotBytes<2>) / pair_stage_bytes<2>(kMaxTileT) > kSkew);
+
 template <int OutType>
 int launch(Linear8Params& p, const void* x, int64_t ld_x, const void* w, int64_t ld_w, int inner, cudaStream_t stream) {
   int pairs = 0;
   int st = set_up<OutType>(&pairs);
   if (st != SDVG_OK) return st;
-  const bool by_pair = p.rows > kPairRows;
-  const int feature_tile = by_pair ? 2 * kTileF : kTileF;
-  p.tiles_f = (p.cols + feature_tile - 1) / feature_tile;
-  if (by_pair) p.tile_t = pair_tile(p.rows, p.tiles_f, pairs, OutType == SDVG_F32 ? kMaxTileChunked : kMaxTileT);
-  else p.tile_t = (std::min(p.rows, kMaxTileFew) + 15) / 16 * 16;
-  p.tiles_t = (p.rows + p.tile_t - 1) / p.tile_t;
-  p.tiles = (long long)p.tiles_f * p.tiles_t;
-  if (p.tiles >= 1ll << 28) return SDVG_ERR_BAD_SHAPE;
-  p.idesc = idesc_mx_e4m3(feature_tile, p.tile_t);
-  if ((st = make_map(&p.w_map, w, inner, p.cols, ld_w, kTileF)) != SDVG_OK) return st;
-  if ((st = make_map(&p.x_map, x, inner, p.rows, ld_x, by_pair ? p.tile_t / 2 : p.tile_t)) != SDVG_OK) return st;
-  if (by_pair) {
-    p.group = 8;
-    p.stages = std::min(kMaxStages, (kPairSmem - 1024 - kScaleSlots * kPairSlotBytes) / (kTileF * 128 + p.tile_t * 64));
-    const int grid = 2 * (int)std::min((long long)pairs, p.tiles);
-    return sdvg::cuda_status(
-        sdvg::launch_overlapped(linear8_pair_kernel<OutType>, grid, kPairThreads, kPairSmem, 0, stream, p));
+  if (p.rows > kPairRows) {
+    const PairTile tile = choose_tile(p.rows, p.cols, p.k_iters, pairs, OutType == SDVG_F32);
+    p.tile_t = tile.tile_t;
+    if constexpr (OutType != SDVG_F32) {
+      if (tile.subs == 2) return launch_pair<OutType, 2>(p, x, ld_x, w, ld_w, inner, pairs, stream);
+    }
+    return launch_pair<OutType, 1>(p, x, ld_x, w, ld_w, inner, pairs, stream);
   }
+  p.tile_t = (p.rows + 15) / 16 * 16;
+  p.tiles_f = (p.cols + kTileF - 1) / kTileF;
+  p.tiles_t = 1;
+  p.tiles = p.tiles_f;
+  p.idesc = idesc_mx_e4m3(kTileF, p.tile_t);
+  if ((st = make_map(&p.w_map, w, inner, p.cols, ld_w, kTileF)) != SDVG_OK) return st;
+  if ((st = make_map(&p.x_map, x, inner, p.rows, ld_x, p.tile_t)) != SDVG_OK) return st;
   p.split = tile_split(p.tiles, p.k_iters, p.tile_t, 2 * pairs);
   p.stages = kTileStages;
   return sdvg::cuda_status(sdvg::launch_overlapped(linear8_tile_kernel<OutType>, (unsigned)p.tiles * p.split, kTileThreads,

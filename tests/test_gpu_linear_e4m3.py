@@ -258,3 +258,43 @@ def test_the_quantised_operands_of_a_product():
     ref = f64(x) @ f64(w).T
     # each operand is off by at most 2^-4, 3.6% rms at worst evenly spread; both independent
     assert np.linalg.norm(got - ref) <= 0.06 * np.linalg.norm(ref)
+
+
+def values_on_gpu(codes, scale, block_rows):
+    f = torch.exp2(scale.double() - 127).repeat_interleave(128, 1)[:, :codes.shape[1]].repeat_interleave(block_rows, 0)[:codes.shape[0]]
+    return codes.view(torch.float8_e4m3fn).double() * f
+
+
+@pytest.mark.parametrize("rows,cols,inner", [(2500, 10000, 130), (2333, 9999, 1150), (4680, 5120, 512), (1111, 20480, 900), (4680, 1536, 2816)])
+@pytest.mark.parametrize("out", ["bf16", "fp32", "e4m3"])
+def test_many_tiles(rows, cols, inner, out):
+    """Rounds of tiles of every width, all outputs, in 64 bits on the GPU; the bound is that of linear_tolerance without an activation."""
+    gen = torch.Generator(device="cuda").manual_seed(rows)
+    x, w = api.e4m3_matrix(rows, inner), api.e4m3_matrix(cols, inner, 128)
+    api.sdvg_quant_e4m3_blocks(randn(gen, rows, inner) * torch.exp2(4 * torch.rand((rows, 1), generator=gen, device="cuda")), *x)
+    api.sdvg_quant_e4m3_blocks(randn(gen, cols, inner, std=inner ** -0.5), *w)
+    gate, bias = randn(gen, 3, cols), randn(gen, cols)
+    per = -(-rows // 3)
+    o = torch.full((rows + 1, cols), 77, device="cuda", dtype=OUTS[out])
+    scale = torch.zeros((rows, -(-cols // 128)), device="cuda", dtype=torch.uint8) if out == "e4m3" else None
+    ws = api.attn_workspace()
+    for _ in range(3):
+        api.sdvg_linear_e4m3(*x, *w, o[:rows], ws, bias=bias, gate=gate, gate_rows=per, out_scale=scale)
+    assert api.sdvg_block_attn_status(ws) == api.SDVG_OK
+    xv, wv = values_on_gpu(*x, 1), values_on_gpu(*w, 128)
+    g = gate.double().repeat_interleave(per, 0)[:rows]
+    v = xv @ wv.t() + bias.double()
+    err = ((inner + 2) * 2 * 2.0 ** -24 * (xv.abs() @ wv.abs().t() + bias.double().abs()) + 4 * 2.0 ** -24 * v.abs()) * g.abs()
+    ref = v * g
+    if out == "e4m3":
+        f = torch.exp2(scale.double() - 127).repeat_interleave(128, 1)[:, :cols]
+        got = o[:rows].view(torch.float8_e4m3fn).double() * f
+        tol = err + torch.maximum((ref.abs() + err) / 16, f / 1024)
+        # the scale is the smallest for a block's largest magnitude, which is known up to err
+        top = lambda a: torch.nn.functional.pad(a, (0, -cols % 128)).unflatten(1, (-1, 128)).amax(2)
+        assert bool((top(ref.abs() - err) <= 448 * f[:, ::128]).all()) and bool((top(ref.abs() + err) > 224 * f[:, ::128]).all())
+    else:
+        got = o[:rows].double()
+        tol = err + (ref.abs() + err) * torch.finfo(OUTS[out]).eps / 2
+    assert bool(((got - ref).abs() <= tol).all())
+    assert bool((o[rows] == 77).all())
