@@ -273,6 +273,109 @@ class TransformerLayer:
 
 
 @dataclass
+class E4M3Matrix:
+    """A matrix in E4M3 with power-of-two scales: codes [rows, cols] and scales [rows / 1 or 128, ceil(cols / 128)], both uint8."""
+    codes: torch.Tensor
+    scale: torch.Tensor
+
+    @classmethod
+    def empty(cls, rows: int, cols: int, block_rows: int = 1, device="cuda") -> "E4M3Matrix":
+        return cls(*api.e4m3_matrix(rows, cols, block_rows, device))
+
+    @classmethod
+    def of_weight(cls, w: torch.Tensor, block_rows: int = 128) -> "E4M3Matrix":
+        """A weight matrix quantised with one scale per 128 x 128 block (block_rows 1: per row and 128 columns)."""
+        m = cls.empty(w.shape[0], w.shape[1], block_rows, w.device)
+        api.sdvg_quant_e4m3_blocks(w, m.codes, m.scale)
+        return m
+
+    def rows_from(self, first: int) -> "E4M3Matrix":
+        """The rows from `first` on: a multiple of the rows of a scale."""
+        if first == 0:
+            return self
+        per = 1 if self.scale.shape[0] == self.codes.shape[0] else 128
+        if first % per:
+            raise ValueError("rows must begin with a scale's")
+        return E4M3Matrix(self.codes[first:], self.scale[first // per:])
+
+
+def _linear8(x: E4M3Matrix, w: E4M3Matrix, out, workspace, **kw) -> None:
+    codes, scale = (out.codes, out.scale) if isinstance(out, E4M3Matrix) else (out, None)
+    api.sdvg_linear_e4m3(x.codes, x.scale, w.codes, w.scale, codes, workspace, out_scale=scale, **kw)
+
+
+class TransformerLayerE4M3(TransformerLayer):
+    """The same layer with its matrices in E4M3, quantised here once, and 8-bit rows between its operators: both norms, the attention's
+    output and the hidden rows of the feed-forward pair are written (or quantised) with a scale per 128 elements, and all
+    four products run on the 8-bit tensor cores.  Over an 8-bit ring q, k and v go from the product's rows into the ring in one
+    call, rounded once.  The residual stream, the modulation and the sums stay what they are.
+    """
+
+    def __init__(self, weights: LayerWeights, m: ModelState, x_dtype: torch.dtype = torch.bfloat16):
+        c = m.cache
+        self.w, self.m, self.width, self.tokens = weights, m, c.heads * c.head_dim, c.block_tokens
+        hidden, dev = weights.w_up.shape[0], m.table.device
+        new = lambda cols, dtype=torch.bfloat16: torch.empty((self.tokens, cols), dtype=dtype, device=dev)
+        rows = lambda cols: E4M3Matrix.empty(self.tokens, cols, device=dev)
+        self.h, self.attn, self.ff, self.qkv = rows(self.width), rows(self.width), rows(hidden), new(3 * self.width)
+        self.x1 = new(self.width, x_dtype)                       # the stream between the two halves
+        post = weights.post_attn is not None or weights.post_ff is not None
+        self.y = new(self.width) if post else None
+        self.norms = api.qk_norm_workspace(self.tokens, dev) if m.tiled and weights.scope == api.SDVG_SCOPE_ROW else None
+        # a commit takes the rows of k and v alone, which must not begin within a scale's
+        self.w_qkv = E4M3Matrix.of_weight(weights.w_qkv, 128 if self.width % 128 == 0 else 1)
+        self.w_out, self.w_up, self.w_down = (E4M3Matrix.of_weight(w) for w in (weights.w_out, weights.w_up, weights.w_down))
+
+    def _norm8(self, x, out: E4M3Matrix, **kw) -> None:
+        api.sdvg_gated_norm_e4m3(x, out.codes, out.scale, eps=self.w.eps, **kw)
+
+    def _qkv(self, x, mod, with_q: bool = True):
+        w, n = self.w, self.width
+        (shift, scale, *_), rows = self._mod(mod)
+        self._norm8(x, self.h, scale=scale, shift=shift, modulate_rows=rows)
+        first = 0 if with_q else n
+        out = self.qkv[:, first:]
+        _linear8(self.h, self.w_qkv.rows_from(first), out, self.m.workspace, bias=None if w.b_qkv is None else w.b_qkv[first:])
+        parts = [out[:, i:i + n] for i in range(0, 3 * n - first, n)]
+        return parts if with_q else [None] + parts
+
+    def _write_kv(self, q, k, v, block: int, flags: int, q_roped=None) -> int:
+        m, w = self.m, self.w
+        if not m.e4m3:
+            return super()._write_kv(q, k, v, block, flags, q_roped)
+        q, k, v = (None if t is None else self._heads(t) for t in (q, k, v))
+        head = (m.cache, q, k, v, w.q_norm, w.k_norm, w.scope, w.eps, q_roped)
+        at = (m.grid, block * m.frames, m.table, m.tab_frames, block, flags)
+        if m.tiled:
+            return api.sdvg_qk_norm_rope3d_commit_e4m3_tiled(*head, None if q is None else m.q_tile_scale, *at, self.norms)
+        return api.sdvg_qk_norm_rope3d_commit_e4m3(*head, None if q is None else m.q_inv_scale, m.k_inv_scale, m.v_inv_scale, *at)
+
+    @_on_the_models_device
+    def step(self, x, mod, block: int, x_out) -> None:
+        m, w = self.m, self.w
+        q, k, v = self._qkv(x, mod)
+        self._write_kv(q, k, v, block, api.SDVG_STAGE, m.q_roped)
+        m.attend(m.q_roped, block, m.out)
+        (_, _, gate1, shift2, scale2, gate2), rows = self._mod(mod)
+        second = dict(scale=scale2, shift=shift2, modulate_rows=rows)
+        self._norm8(m.out.view(self.tokens, self.width), self.attn, norm=api.SDVG_NORM_NONE)
+        if w.post_attn is None:
+            _linear8(self.attn, self.w_out, self.x1, m.workspace, bias=w.b_out, gate=gate1, gate_rows=rows, residual=x)
+            self._norm8(self.x1, self.h, **second)
+        else:
+            _linear8(self.attn, self.w_out, self.y, m.workspace, bias=w.b_out)
+            self._norm8(x, self.h, y=self.y, gate=gate1, gate_rows=rows, post_norm=api.SDVG_NORM_RMS, post_weight=w.post_attn,
+                        x_out=self.x1, **second)
+        _linear8(self.h, self.w_up, self.ff, m.workspace, bias=w.b_up, act=w.act)
+        if w.post_ff is None:
+            _linear8(self.ff, self.w_down, x_out, m.workspace, bias=w.b_down, gate=gate2, gate_rows=rows, residual=self.x1)
+        else:
+            _linear8(self.ff, self.w_down, self.y, m.workspace, bias=w.b_down)
+            api.sdvg_gated_norm(self.x1, None, y=self.y, gate=gate2, gate_rows=rows, post_norm=api.SDVG_NORM_RMS,
+                                post_weight=w.post_ff, x_out=x_out, eps=w.eps)
+
+
+@dataclass
 class TimeModulation:
     """The modulation of a step from its time features (Sec. 4.1: the sampler's time steps): fp32 [groups, 6 * width] =
     offsets + W_mod silu(W2 silu(W1 features + b1) + b2) + b_mod, features bf16 [groups, ...]."""
@@ -293,6 +396,25 @@ class TimeModulation:
         api.sdvg_linear(a, self.w2, e, workspace, bias=self.b2, act=api.SDVG_ACT_SILU)
         api.sdvg_linear(e, self.w_mod, out, workspace, bias=self.b_mod,
                         residual=None if self.offsets is None else self.offsets.expand(rows, -1))
+        return out
+
+
+class TimeModulationE4M3:
+    """TimeModulation with its matrices in E4M3, quantised here once: half the bytes, which is what a few rows pay for."""
+
+    def __init__(self, tm: TimeModulation):
+        self.tm = tm
+        self.w1, self.w2, self.w_mod = (E4M3Matrix.of_weight(w) for w in (tm.w1, tm.w2, tm.w_mod))
+
+    def __call__(self, features, workspace, out=None) -> torch.Tensor:
+        tm, rows, dev = self.tm, features.shape[0], features.device
+        f, a, e = (E4M3Matrix.empty(rows, n, device=dev) for n in (features.shape[1], self.w1.codes.shape[0], self.w2.codes.shape[0]))
+        out = torch.empty((rows, self.w_mod.codes.shape[0]), dtype=torch.float32, device=dev) if out is None else out
+        api.sdvg_quant_e4m3_blocks(features, f.codes, f.scale)
+        _linear8(f, self.w1, a, workspace, bias=tm.b1, act=api.SDVG_ACT_SILU)
+        _linear8(a, self.w2, e, workspace, bias=tm.b2, act=api.SDVG_ACT_SILU)
+        _linear8(e, self.w_mod, out, workspace, bias=tm.b_mod,
+                 residual=None if tm.offsets is None else tm.offsets.expand(rows, -1))
         return out
 
 
