@@ -788,16 +788,16 @@ def sdvg_cache_read_block_e4m3(cache: Cache, slot: int, k_out, v_out, k_descale=
     """The values that a slot of an 8-bit ring holds, bf16 [tokens, heads, 128] (k_out or v_out may be None).  Scales fp32 [heads] for a
     ring with static ones; without them the ring's tile scales."""
     dev = cache._k_raw.get_device()
-    if dev >= 0 and _elsewhere(dev):
+    if _elsewhere(dev):
         with torch.cuda.device(dev):
             return sdvg_cache_read_block_e4m3(cache, slot, k_out, v_out, k_descale, v_descale, stream)
-    shape = (cache.block_tokens, cache.heads, cache.head_dim)
-    for t in (k_out, v_out, k_descale, v_descale):
+    for t in (k_out, v_out):
         if t is not None and t.get_device() != dev:
             raise ValueError("on another device than the ring")
-    sc = lambda t: None if t is None else _scales(t, cache.heads)
-    _check(lib().sdvg_cache_read_block_e4m3(cache.handle, slot, sc(k_descale), sc(v_descale), _bf16(k_out, shape), _bf16(v_out, shape),
-                                            _raw_stream(dev, stream)), "sdvg_cache_read_block_e4m3")
+    st = _binding().read_block_e4m3(cache.handle.value or 0, cache.block_tokens, cache.heads, slot, k_out, v_out, k_descale, v_descale,
+                                    _raw_stream(dev, stream))
+    if st != SDVG_OK:
+        raise SdvgError(st, "sdvg_cache_read_block_e4m3")
 
 
 # ---------------------------------------------------------------- 8-bit rows and weights

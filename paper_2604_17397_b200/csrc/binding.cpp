@@ -355,6 +355,35 @@ PyObject* qk_norm(PyObject*, PyObject* const* args, Py_ssize_t n) {
   return PyLong_FromLongLong(st == SDVG_OK ? evicted : -1000 - st);
 }
 
+// (handle, block_tokens, heads, slot, k_out, v_out, k_descale, v_descale, stream) -> status
+PyObject* read_block_e4m3(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  if (n != 9) return PyErr_Format(PyExc_TypeError, "read_block_e4m3 takes 9 arguments");
+  Reader r{args};
+  const sdvg_cache* cache = static_cast<sdvg_cache*>(r.address(0));
+  const int64_t tokens = r.integer(1), heads = r.integer(2);
+  const int slot = r.small(3);
+  void* outs[2] = {nullptr, nullptr};
+  for (int i = 0; i < 2; ++i) {
+    const char* const what = i ? "v_out" : "k_out";
+    const Tensor* t = r.tensor(4 + i, what, true);
+    if (!t) continue;
+    if (t->scalar_type() != ScalarType::BFloat16 || t->dim() != 3 || t->size(0) != tokens || t->size(1) != heads || t->size(2) != 128 ||
+        !t->is_contiguous()) {
+      PyErr_Format(PyExc_ValueError, "%s: expected contiguous bfloat16 [%lld, %lld, 128]", what, (long long)tokens, (long long)heads);
+      return nullptr;
+    }
+    outs[i] = t->data_ptr();
+  }
+  const float *ks = vector(r, 6, heads, "k_descale"), *vs = vector(r, 7, heads, "v_descale");
+  void* stream = r.address(8);
+  if (!r.ok) return nullptr;
+  int st;
+  Py_BEGIN_ALLOW_THREADS
+  st = sdvg_cache_read_block_e4m3(cache, slot, ks, vs, outs[0], outs[1], stream);
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(st);
+}
+
 // A C++ exception (a tensor without storage, say) becomes a Python one.
 template <PyObject* (*F)(PyObject*, PyObject* const*, Py_ssize_t)>
 PyObject* guarded(PyObject* self, PyObject* const* args, Py_ssize_t n) {
@@ -373,7 +402,7 @@ PyMethodDef method(const char* name) {
 
 PyMethodDef methods[] = {method<linear>("linear"), method<gated_norm<false>>("gated_norm"), method<qk_norm<kBf16>>("qk_norm"),
                          method<qk_norm<kStatic>>("qk_norm_e4m3"), method<qk_norm<kTiled>>("qk_norm_e4m3_tiled"),
-                         method<linear_e4m3>("linear_e4m3"), method<gated_norm<true>>("gated_norm_e4m3"), method<e4m3_blocks>("e4m3_blocks"),
+                         method<linear_e4m3>("linear_e4m3"), method<gated_norm<true>>("gated_norm_e4m3"), method<e4m3_blocks>("e4m3_blocks"), method<read_block_e4m3>("read_block_e4m3"),
                          {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

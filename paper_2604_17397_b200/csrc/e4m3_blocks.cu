@@ -55,14 +55,14 @@ __device__ __forceinline__ void load8(float (&v)[8], const BlockParams& p, long 
 
 template <bool VEC>
 __global__ void __launch_bounds__(kThreads) quant_blocks_kernel(const __grid_constant__ BlockParams p) {
-  __shared__ uint32_t s_top[kThreads / 32];
+  __shared__ float s_top[kThreads / 32];
   sdvg::overlap_begin();
   sdvg::overlap_wait();
   const int tile = blockIdx.x / p.col_blocks, block = blockIdx.x % p.col_blocks;
   const int lane = threadIdx.x % 16, c = block * 128 + lane * 8;
   const long long r0 = (long long)tile * 128 + threadIdx.x / 16;
   float v[kRows][8];
-  uint32_t top[kRows];
+  float top[kRows];
 #pragma unroll
   for (int i = 0; i < kRows; ++i) {
     if (r0 + 32 * i < p.rows) {
@@ -74,20 +74,20 @@ __global__ void __launch_bounds__(kThreads) quant_blocks_kernel(const __grid_con
   }
 #pragma unroll
   for (int i = 0; i < kRows; ++i) {
-    top[i] = 0;
+    top[i] = 0.f;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) top[i] = max(top[i], sdvg::magnitude_bits(v[i][j]));
+    for (int j = 0; j < 8; j += 2) top[i] = sdvg::larger(top[i], v[i][j], v[i][j + 1]);
   }
   if (p.block_rows == 1) {
 #pragma unroll
     for (int i = 0; i < kRows; ++i)
 #pragma unroll
-      for (int o = 8; o > 0; o >>= 1) top[i] = max(top[i], __shfl_xor_sync(0xffffffffu, top[i], o));
+      for (int o = 8; o > 0; o >>= 1) top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], o));
   } else {
-    uint32_t m = __reduce_max_sync(0xffffffffu, max(max(top[0], top[1]), max(top[2], top[3])));
+    float m = sdvg::warp_largest(fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])));
     if (threadIdx.x % 32 == 0) s_top[threadIdx.x / 32] = m;
     __syncthreads();
-    m = __reduce_max_sync(0xffffffffu, s_top[threadIdx.x % (kThreads / 32)]);
+    m = sdvg::warp_largest(s_top[threadIdx.x % (kThreads / 32)]);
 #pragma unroll
     for (int i = 0; i < kRows; ++i) top[i] = m;
     if (threadIdx.x == 0) p.scale[tile * p.ld_scale + block] = (uint8_t)(sdvg::scale_exponent(m) + 127);

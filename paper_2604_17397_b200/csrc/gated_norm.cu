@@ -283,17 +283,16 @@ __global__ void __launch_bounds__(WARP ? 128 : kTeamThreads) gated_norm_kernel(c
 #pragma unroll
       for (int j = 0; j < 4; ++j) s[i].p[j] = fma2(s[i].p[j], A[i].p[j], B[i].p[j]);
       if constexpr (OUT8) {
-        float f[8];
-        uint32_t top = 0;
+        float f[8], top = 0.f;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           const float2 a = floats_of(s[i].p[j]);
           f[2 * j] = a.x;
           f[2 * j + 1] = a.y;
-          if (valid(i)) top = max(top, max(sdvg::magnitude_bits(a.x), sdvg::magnitude_bits(a.y)));
+          if (valid(i)) top = sdvg::larger(top, a.x, a.y);
         }
 #pragma unroll
-        for (int o = 8; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+        for (int o = 8; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
         const int e = sdvg::scale_exponent(top);
         const float inv = sdvg::power_of_two(-e);
         if (valid(i)) {
@@ -429,10 +428,10 @@ __global__ void __launch_bounds__(NI == 16 ? 512 : 256) gated_norm_single_kernel
     uint8_t* o = static_cast<uint8_t*>(p.out) + r * p.ld_out + c0;
 #pragma unroll
     for (int b = 0; b < NI / 4; ++b) {
-      uint32_t top = 0;
+      float top = 0.f;
 #pragma unroll
-      for (int i = 4 * b; i < 4 * b + 4; ++i) top = max(top, valid(i) ? sdvg::magnitude_bits(s[i]) : 0u);
-      const int e = sdvg::scale_exponent(__reduce_max_sync(0xffffffffu, top));
+      for (int i = 4 * b; i < 4 * b + 4; ++i) top = valid(i) ? sdvg::larger(top, s[i]) : top;
+      const int e = sdvg::scale_exponent(sdvg::warp_largest(top));
       const float inv = sdvg::power_of_two(-e);
       const uint32_t codes = sm100::pack_e4m3x4(s[4 * b] * inv, s[4 * b + 1] * inv, s[4 * b + 2] * inv, s[4 * b + 3] * inv);
 #pragma unroll
@@ -514,8 +513,7 @@ __global__ void __launch_bounds__(kLongThreads) gated_norm_long_kernel(const __g
     uint8_t* out = static_cast<uint8_t*>(p.out) + r * p.ld_out;
     for (int b = threadIdx.x / 32; b < blocks; b += kLongThreads / 32) {
       const int c0 = 128 * b + lane;
-      float o[4];
-      uint32_t top = 0;
+      float o[4], top = 0.f;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int c = c0 + 32 * i;
@@ -524,9 +522,9 @@ __global__ void __launch_bounds__(kLongThreads) gated_norm_long_kernel(const __g
         const float s = sum(c);                      // read before either output is written: both may be in place
         if (p.x_out) store_elem(p.x_out, r * p.ld_x_out + c, p.x_type, s);
         o[i] = normed(s, c);
-        top = max(top, sdvg::magnitude_bits(o[i]));
+        top = sdvg::larger(top, o[i]);
       }
-      const int e = sdvg::scale_exponent(__reduce_max_sync(0xffffffffu, top));
+      const int e = sdvg::scale_exponent(sdvg::warp_largest(top));
       const float inv = sdvg::power_of_two(-e);
       const uint32_t codes = sm100::pack_e4m3x4(o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv);
 #pragma unroll

@@ -268,3 +268,19 @@ def test_the_binding_of_the_ring_writes(lib, rings):
     for more in ((f32(2, 2), None), (f32(1, 2), None), (u8(2, 1), None), (f32(2, 1), 5)):
         with pytest.raises(ValueError):
             call(tiled, b.qk_norm_e4m3_tiled, more)
+
+
+def test_the_binding_of_the_read_back(lib, rings):
+    static = rings[0]
+    read = lambda k, v, ks=OnPaper(2, dtype=torch.float32), vs=OnPaper(2, dtype=torch.float32), slot=0: api._binding().read_block_e4m3(
+        static.value, 64, 2, slot, k, v, ks, vs, 0)
+    block = lambda: OnPaper(64, 2, 128)
+    assert read(block(), block()) == read(None, None) == read(block(), block(), slot=5) == api.SDVG_ERR_INVALID_ARG
+    for bad in ((OnPaper(64, 2, 64), None), (u8(64, 2, 128), None), (OnPaper(63, 2, 128), None), (None, OnPaper(64, 256))):
+        with pytest.raises(ValueError):
+            read(*bad)
+    for scale in (OnPaper(3, dtype=torch.float32), OnPaper(2), OnPaper(2, 1, dtype=torch.float32)):
+        with pytest.raises(ValueError):
+            read(block(), block(), ks=scale)
+    with pytest.raises(TypeError):
+        api._binding().read_block_e4m3()
