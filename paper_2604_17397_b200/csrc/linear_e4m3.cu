@@ -19,6 +19,7 @@
 #include "elem_types.cuh"
 #include "linear_epilogue.cuh"
 #include "overlap.cuh"
+#include "row_team.cuh"
 #include "sdvg_internal.h"
 #include "tensor_map.h"
 
@@ -125,6 +126,192 @@ __device__ __forceinline__ bool quantise16(const Linear8Params& p, Exchange& x, 
     for (int i = 0; i < 4; ++i, o += ld)
       if (mine && m0 + j + i < m_end) *o = (uint8_t)(c >> (8 * i));
   }
+  return true;
+}
+
+// ---- outputs by way of shared memory --------------------------------------------------------------
+// Where rows of the output begin at multiples of 16 bytes and hold whole vectors, a warp takes its 32 features x 16 tokens from tensor
+// memory as fragments (a lane then has features g, g + 8, g + 16 and g + 24, g = lane / 4, of tokens 2 q, 2 q + 1, 2 q + 8 and 2 q + 9, q =
+// lane % 4), turns them in shared memory and stores 16 bytes per lane.  One store and one address per element and lane, as in the
+// general epilogue, took as long as the products of a tile (4680 x 5120 x 20480 into bf16: 42 of 290 us, GELU another 43).
+constexpr int kTurnBytes = 1024;                       // of a warp
+
+// Values of a lane: v[4 f + k] is feature g + 8 f of the lane's k-th token.
+struct Lane {
+  int n, m, q;                                         // first feature, first token (of the warp's block), lane % 4
+  __device__ __forceinline__ int token(int k) const { return m + 2 * q + (k & 1) + 8 * (k / 2); }
+};
+
+struct FragGate {
+  TileGate of[4];
+};
+
+template <int OutType>
+__device__ __forceinline__ void load_residual_frag(const Linear8Params& p, typename OutElem<OutType>::T (&res)[16], const Lane& l, int m_end) {
+  using T = typename OutElem<OutType>::T;
+  if (!p.residual) return;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    if (l.token(k) >= m_end) continue;
+    const T* r = static_cast<const T*>(p.residual) + l.token(k) * p.ld_res + l.n;
+#pragma unroll
+    for (int f = 0; f < 4; ++f)
+      if (l.n + 8 * f < p.cols) res[4 * f + k] = r[8 * f];
+  }
+}
+
+// activate16 in packed pairs, which is what an epilogue of 8-bit products has time for: the constants of an exponential's argument
+// are multiplied out (z is -u log2 e), a quotient is one reciprocal, whose limits are those of activate16: past 2^126 it is 0.
+__device__ __forceinline__ rows::Pair exp2_pair(rows::Pair z) {
+  const float2 f = rows::floats_of(z);
+  float2 e;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e.x) : "f"(f.x));
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e.y) : "f"(f.y));
+  return rows::pair_of(e.x, e.y);
+}
+__device__ __forceinline__ rows::Pair reciprocal_pair(rows::Pair d) {
+  const float2 f = rows::floats_of(d);
+  float2 r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r.x) : "f"(f.x));
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r.y) : "f"(f.y));
+  return rows::pair_of(r.x, r.y);
+}
+__device__ __forceinline__ void activate_pairs(float (&v)[16], int act) {
+  using namespace rows;
+  constexpr float kLog2e = 1.4426950408889634f;
+  auto each = [&](auto f) {
+#pragma unroll
+    for (int i = 0; i < 16; i += 2) {
+      const float2 y = floats_of(f(pair_of(v[i], v[i + 1])));
+      v[i] = y.x;
+      v[i + 1] = y.y;
+    }
+  };
+  const Pair one = pair_of(1.f, 1.f);
+  if (act == SDVG_ACT_SILU) {
+    const Pair c = pair_of(-kLog2e, -kLog2e);
+    each([&](Pair a) { return mul2(a, reciprocal_pair(add2(exp2_pair(mul2(a, c)), one))); });
+  } else if (act == SDVG_ACT_GELU_TANH) {
+    constexpr float k = -1.5957691216057308f * kLog2e;
+    const Pair c1 = pair_of(k, k), c3 = pair_of(k * 0.044715f, k * 0.044715f);
+    each([&](Pair a) { return mul2(a, reciprocal_pair(add2(exp2_pair(mul2(a, fma2(mul2(a, a), c3, c1))), one))); });
+  } else if (act == SDVG_ACT_GELU) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] = gelu_erf(v[i]);
+  }
+}
+
+// gate * act(acc + bias)
+__device__ __forceinline__ void gated_frag(const Linear8Params& p, float (&v)[16], const Lane& l, int m_end, const float (&bias)[4],
+                                           const FragGate& gate) {
+#pragma unroll
+  for (int i = 0; i < 16; ++i) v[i] += bias[i / 4];
+  activate_pairs(v, p.act);
+  if (!p.gate) return;
+#pragma unroll
+  for (int f = 0; f < 4; ++f) {
+    const TileGate& g = gate.of[f];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int m = l.token(k);
+      if (g.few) v[4 * f + k] *= m < g.border ? g.first : g.second;
+      else if (m < m_end && l.n + 8 * f < p.cols) v[4 * f + k] *= p.gate[(m / p.gate_rows) * p.ld_gate + l.n + 8 * f];
+    }
+  }
+}
+
+// 16-bit outputs.
+template <int OutType>
+__device__ __forceinline__ void store_frag(const Linear8Params& p, const float (&v)[16], const Lane& l, int m_end, uint32_t turn) {
+  const int lane = threadIdx.x % 32;
+  uint32_t h[8];                                       // of two neighbouring tokens: [feature block][tokens 0 and 1, or 8 and 9]
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    if constexpr (OutType == SDVG_BF16) {
+      const __nv_bfloat162 x = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+      h[i] = *reinterpret_cast<const uint32_t*>(&x);
+    } else {
+      const __half2 x = __floats2half2_rn(v[2 * i], v[2 * i + 1]);
+      h[i] = *reinterpret_cast<const uint32_t*>(&x);
+    }
+  }
+  // token t of the block: 64 bytes at 64 t, whose 16-byte pieces are moved round so that neither side meets a bank twice
+  auto at = [&](int t, int piece) { return turn + t * 64 + (piece ^ (t / 2 % 4)) * 16; };
+  st_frag_t4(at(lane % 8, lane / 8), h[0], h[2], h[4], h[6]);
+  st_frag_t4(at(8 + lane % 8, lane / 8), h[1], h[3], h[5], h[7]);
+  __syncwarp();
+  const int n = l.n - lane / 4 + lane % 4 * 8;         // this lane's vector
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int t = lane / 4 + 8 * i;
+    uint4 x;
+    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(x.x), "=r"(x.y), "=r"(x.z), "=r"(x.w) : "r"(at(t, lane % 4)) : "memory");
+    if (l.m + t < m_end && n < p.cols)
+      *reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.out) + (l.m + t) * p.ld_out + n) = x;
+  }
+  __syncwarp();
+}
+
+// 8-bit outputs.  Returns false when a wait gave up.
+__device__ __forceinline__ bool quantise_frag(const Linear8Params& p, Exchange& x, int& turns, const float (&v)[16], const Lane& l, int quad,
+                                              int m_end, uint32_t turn) {
+  const int lane = threadIdx.x % 32, g = lane / 4;
+  float top[4];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    float a[4];
+#pragma unroll
+    for (int f = 0; f < 4; ++f) a[f] = l.n + 8 * f < p.cols ? v[4 * f + k] : 0.f;
+    top[k] = sdvg::larger(sdvg::larger(0.f, a[0], a[1]), a[2], a[3]);
+#pragma unroll
+    for (int o = 4; o < 32; o *= 2) top[k] = fmaxf(top[k], __shfl_xor_sync(0xffffffffu, top[k], o));
+  }
+  const int buffer = turns & 1;
+  if (lane < 4) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      reinterpret_cast<float*>(&x.top[buffer][2 * lane + (k & 1) + 8 * (k / 2)])[quad] = top[k];
+  }
+  __syncwarp();
+  if (lane == 0) mbar_arrive(&x.bar);
+  const bool ok = __all_sync(0xffffffffu, wait_for(&x.bar, (uint32_t)buffer, p.status, kWaitLimitNs));
+  ++turns;
+  if (!ok) return false;
+  const uint4 t = x.top[buffer][lane % 16];
+  const int e = sdvg::scale_exponent(max(max(t.x, t.y), max(t.z, t.w)));
+  const int n0 = l.n - g, block = n0 / 128;            // the same for the warp
+  if (quad == 0 && lane < 16 && l.m + lane < m_end && block * 128 < p.cols)
+    p.out_scale[(long long)(l.m + lane) * p.ld_os + block] = (uint8_t)(e + 127);
+  const float mine = sdvg::power_of_two(-e);           // of token lane % 16
+  float inv[4];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) inv[k] = __shfl_sync(0xffffffffu, mine, 2 * l.q + (k & 1) + 8 * (k / 2));
+  // codes of a feature's four tokens; then lanes of neighbouring features trade tokens, so that each has both features of two
+  uint32_t c[4];
+#pragma unroll
+  for (int f = 0; f < 4; ++f) c[f] = pack_e4m3x4(v[4 * f] * inv[0], v[4 * f + 1] * inv[1], v[4 * f + 2] * inv[2], v[4 * f + 3] * inv[3]);
+  const bool odd = g & 1;
+  const uint32_t keep = odd ? 0x7531 : 0x6420, give = odd ? 0x6420 : 0x7531, lo = odd ? 0x1504 : 0x5140, hi = odd ? 0x3726 : 0x7362;
+  const int token = 2 * l.q + odd;                     // and 8 tokens on
+  // token t of the block: 32 bytes at 32 t, whose halves change places every four tokens, for the banks' sake
+  auto at = [&](int t, int half) { return turn + t * 32 + (half ^ (t / 4 % 2)) * 16; };
+#pragma unroll
+  for (int f = 0; f < 4; f += 2) {
+    const uint32_t k = __byte_perm(c[f], c[f + 1], keep);
+    const uint32_t r = __shfl_xor_sync(0xffffffffu, __byte_perm(c[f], c[f + 1], give), 4);
+    const uint32_t a = __byte_perm(k, r, lo), b = __byte_perm(k, r, hi);       // feature blocks f and f + 1: (token, token + 8)
+    const uint32_t to = at(token, f / 2) + g / 2 * 2, to8 = at(token + 8, f / 2) + g / 2 * 2;
+    asm volatile("st.shared.u16 [%0], %1;" ::"r"(to), "h"((uint16_t)a) : "memory");
+    asm volatile("st.shared.u16 [%0], %1;" ::"r"(to8), "h"((uint16_t)(a >> 16)) : "memory");
+    asm volatile("st.shared.u16 [%0], %1;" ::"r"(to + 8), "h"((uint16_t)b) : "memory");
+    asm volatile("st.shared.u16 [%0], %1;" ::"r"(to8 + 8), "h"((uint16_t)(b >> 16)) : "memory");
+  }
+  __syncwarp();
+  const int row = lane / 2, n = n0 + lane % 2 * 16;
+  uint4 w;
+  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w.x), "=r"(w.y), "=r"(w.z), "=r"(w.w) : "r"(at(row, lane % 2)) : "memory");
+  if (l.m + row < m_end && n < p.cols) *reinterpret_cast<uint4*>(static_cast<uint8_t*>(p.out) + (l.m + row) * p.ld_out + n) = w;
+  __syncwarp();
   return true;
 }
 
@@ -377,6 +564,10 @@ constexpr int kPairSlotBytes = SUBS * 512 + 1024;
 template <int SUBS>
 __host__ __device__ constexpr int pair_stage_bytes(int tile_t) { return SUBS * kTileF * 128 + tile_t * 64; }
 
+// What is not operand stages: the alignment, the scales, the space in which the epilogue warps turn outputs.
+template <int SUBS, bool TURNED>
+constexpr int pair_fixed_bytes = 1024 + kScaleSlots * kPairSlotBytes<SUBS> + (TURNED ? kEpiWarps * kTurnBytes : 0);
+
 struct PairSmem {
   uint64_t full[kMaxStages], empty[kMaxStages], sf_full[kScaleSlots], sf_empty[kScaleSlots], acc_full[kAccs], acc_empty[kAccs];
   Exchange exchange[kEpiWarps / 4];
@@ -384,7 +575,8 @@ struct PairSmem {
 };
 static_assert(sizeof(PairSmem) <= 3072 - 512);
 
-template <int OutType, int SUBS>
+// TURNED: the outputs go by way of shared memory.
+template <int OutType, int SUBS, bool TURNED>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
     linear8_pair_kernel(const __grid_constant__ Linear8Params p) {
   constexpr bool kChunked = OutType == SDVG_F32, kOut8 = OutType == SDVG_E4M3;
@@ -399,6 +591,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
   constexpr int kFeatures = SUBS * kTileF, w_bytes = kFeatures * 128;  // of a CTA
   const int stage_bytes = pair_stage_bytes<SUBS>(p.tile_t);
   uint8_t* slots = buf + p.stages * stage_bytes;
+  const uint32_t turn_space = smem_u32(slots + kScaleSlots * kPairSlotBytes<SUBS>) + (TURNED ? warp % kEpiWarps * kTurnBytes : 0);
   const int chunks = kChunked ? (p.k_iters + kPairChunkIters - 1) / kPairChunkIters : 1;
   const int words = (p.k_iters + kWordStages - 1) / kWordStages;
   sdvg::overlap_begin();
@@ -578,11 +771,23 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
       const int m0 = tt * p.tile_t, m_end = min(p.rows, m0 + p.tile_t);
 #pragma unroll 1
       for (int sub = 0; sub < SUBS; ++sub) {
-        const int n = (2 * ft + (int)rank) * kFeatures + sub * kTileF + quad * 32 + lane;
-        const float bias = p.bias && n < p.cols ? p.bias[n] : 0.f;
-        const TileGate gate = tile_gate(p, n, m0, m_end);
+        const int n0 = (2 * ft + (int)rank) * kFeatures + sub * kTileF + quad * 32, n = n0 + lane;
+        float bias[TURNED ? 4 : 1];
+        FragGate gate;
         T ahead[16];
-        if (!kOut8) load_residual16<OutType>(p, ahead, n, m0 + part * 16, m_end);
+        Lane at{n0 + lane / 4, m0 + part * 16, lane % 4};
+        if constexpr (TURNED) {
+#pragma unroll
+          for (int f = 0; f < 4; ++f) {
+            bias[f] = p.bias && at.n + 8 * f < p.cols ? p.bias[at.n + 8 * f] : 0.f;
+            gate.of[f] = tile_gate(p, at.n + 8 * f, m0, m_end);
+          }
+          if constexpr (!kOut8) load_residual_frag<OutType>(p, ahead, at, m_end);
+        } else {
+          bias[0] = p.bias && n < p.cols ? p.bias[n] : 0.f;
+          gate.of[0] = tile_gate(p, n, m0, m_end);
+          if constexpr (!kOut8) load_residual16<OutType>(p, ahead, n, m0 + part * 16, m_end);
+        }
         auto release = [&](int stage) {
           if (lane == 0) mbar_arrive_cluster(empty + 8 * stage);
         };
@@ -599,14 +804,40 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
 #pragma unroll 1
         for (int col = part * 16; m0 + col < m_end; col += 16 * kParts) {
           float acc[16];
-          tmem_ld16(sums + col, reinterpret_cast<uint32_t(&)[16]>(acc));
-          tmem_wait_ld();
-          if constexpr (kOut8) {
-            if (n < p.cols) gated16(p, acc, n, m0 + col, min(16, m_end - m0 - col), bias, gate);
-            if (!(ok = quantise16(p, sm.exchange[part], turn, acc, n, quad, m0 + col, m_end))) break;
+          if constexpr (TURNED) {
+            float lo[8], hi[8];
+            tmem_ld_frag16(sums + col, lo);
+            tmem_ld_frag16(sums + col + (16u << 16), hi);
+            tmem_wait_ld();
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {              // register i: feature block i / 2 % 2, token i % 2 + 2 (i / 4)
+              acc[4 * (i / 2 % 2) + i % 2 + 2 * (i / 4)] = lo[i];
+              acc[4 * (2 + i / 2 % 2) + i % 2 + 2 * (i / 4)] = hi[i];
+            }
+            at.m = m0 + col;
+            gated_frag(p, acc, at, m_end, bias, gate);
+            if constexpr (kOut8) {
+              if (!(ok = quantise_frag(p, sm.exchange[part], turn, acc, at, quad, m_end, turn_space))) break;
+            } else {
+              if (p.residual) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) acc[i] += OutElem<OutType>::get(ahead[i]);
+              }
+              at.m += 16 * kParts;
+              load_residual_frag<OutType>(p, ahead, at, m_end);
+              at.m = m0 + col;
+              store_frag<OutType>(p, acc, at, m_end, turn_space);
+            }
           } else {
-            epilogue16<OutType>(p, acc, ahead, n, m0 + col, m_end, bias, gate);
-            load_residual16<OutType>(p, ahead, n, m0 + col + 16 * kParts, m_end);
+            tmem_ld16(sums + col, reinterpret_cast<uint32_t(&)[16]>(acc));
+            tmem_wait_ld();
+            if constexpr (kOut8) {
+              if (n < p.cols) gated16(p, acc, n, m0 + col, min(16, m_end - m0 - col), bias[0], gate.of[0]);
+              if (!(ok = quantise16(p, sm.exchange[part], turn, acc, n, quad, m0 + col, m_end))) break;
+            } else {
+              epilogue16<OutType>(p, acc, ahead, n, m0 + col, m_end, bias[0], gate.of[0]);
+              load_residual16<OutType>(p, ahead, n, m0 + col + 16 * kParts, m_end);
+            }
           }
         }
         if (!ok) break;
@@ -678,9 +909,9 @@ int tile_split(long long tiles, int k_iters, int tile_t, int sms) {
 
 // One-time set-up per device and output type: the opt-in to the kernels' dynamic shared memory, and how many CTA pairs
 // the device runs at once.
-template <int OutType, int SUBS>
+template <int OutType, int SUBS, bool TURNED>
 cudaError_t set_up_pair(int* pairs) {
-  cudaError_t e = cudaFuncSetAttribute(linear8_pair_kernel<OutType, SUBS>, cudaFuncAttributeMaxDynamicSharedMemorySize, kPairSmem);
+  cudaError_t e = cudaFuncSetAttribute(linear8_pair_kernel<OutType, SUBS, TURNED>, cudaFuncAttributeMaxDynamicSharedMemorySize, kPairSmem);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(2);
@@ -692,7 +923,10 @@ cudaError_t set_up_pair(int* pairs) {
   attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
   cfg.attrs = &attr;
   cfg.numAttrs = 1;
-  return cudaOccupancyMaxActiveClusters(pairs, linear8_pair_kernel<OutType, SUBS>, &cfg);
+  int n = 0;
+  e = cudaOccupancyMaxActiveClusters(&n, linear8_pair_kernel<OutType, SUBS, TURNED>, &cfg);
+  *pairs = std::min(*pairs, n);
+  return e;
 }
 
 template <int OutType>
@@ -707,12 +941,12 @@ int set_up(int* pairs) {
     e = cudaFuncSetAttribute(linear8_tile_kernel<OutType>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                              std::max(tile_dynamic(32), tile_dynamic(kMaxTileFew)));
     if (e != cudaSuccess) return sdvg::cuda_status(e);
-    int n = 0;
-    e = set_up_pair<OutType, 1>(&n);
+    int n = 0x7fffffff;
+    e = set_up_pair<OutType, 1, false>(&n);
     if constexpr (OutType != SDVG_F32) {
-      int wide = 0;
-      if (e == cudaSuccess) e = set_up_pair<OutType, 2>(&wide);
-      n = std::min(n, wide);
+      if (e == cudaSuccess) e = set_up_pair<OutType, 2, false>(&n);
+      if (e == cudaSuccess) e = set_up_pair<OutType, 1, true>(&n);
+      if (e == cudaSuccess) e = set_up_pair<OutType, 2, true>(&n);
     }
     if (e != cudaSuccess || n < 1) return sdvg::cuda_status(e != cudaSuccess ? e : cudaErrorUnknown);
     pairs_of_device[dev] = n;
@@ -742,7 +976,7 @@ PairTile choose_tile(int rows, int cols, int k_iters, int pairs, bool chunked) {
   return best;
 }
 
-template <int OutType, int SUBS>
+template <int OutType, int SUBS, bool TURNED>
 int launch_pair(Linear8Params& p, const void* x, int64_t ld_x, const void* w, int64_t ld_w, int inner, int pairs, cudaStream_t stream) {
   p.tiles_f = (p.cols + 2 * SUBS * kTileF - 1) / (2 * SUBS * kTileF);
   p.tiles_t = (p.rows + p.tile_t - 1) / p.tile_t;
@@ -753,13 +987,13 @@ int launch_pair(Linear8Params& p, const void* x, int64_t ld_x, const void* w, in
   if (st != SDVG_OK) return st;
   if ((st = make_map(&p.x_map, x, inner, p.rows, ld_x, p.tile_t / 2)) != SDVG_OK) return st;
   p.group = 8 / SUBS;
-  p.stages = std::min(kMaxStages, (kPairSmem - 1024 - kScaleSlots * kPairSlotBytes<SUBS>) / pair_stage_bytes<SUBS>(p.tile_t));
+  p.stages = std::min(kMaxStages, (kPairSmem - pair_fixed_bytes<SUBS, TURNED>) / pair_stage_bytes<SUBS>(p.tile_t));
   const int grid = 2 * (int)std::min((long long)pairs, p.tiles);
   return sdvg::cuda_status(
-      sdvg::launch_overlapped(linear8_pair_kernel<OutType, SUBS>, grid, kPairThreads, kPairSmem, 0, stream, p));
+      sdvg::launch_overlapped(linear8_pair_kernel<OutType, SUBS, TURNED>, grid, kPairThreads, kPairSmem, 0, stream, p));
 }
 // The skewed stages of both ends are all in the ring at once.
-static_assert((kPairSmem - 1024 - kScaleSlots * kPairSlotBytes<2>) / pair_stage_bytes<2>(kMaxTileT) > kSkew);
+static_assert((kPairSmem - pair_fixed_bytes<2, true>) / pair_stage_bytes<2>(kMaxTileT) > kSkew);
 
 template <int OutType>
 int launch(Linear8Params& p, const void* x, int64_t ld_x, const void* w, int64_t ld_w, int inner, cudaStream_t stream) {
@@ -770,9 +1004,14 @@ int launch(Linear8Params& p, const void* x, int64_t ld_x, const void* w, int64_t
     const PairTile tile = choose_tile(p.rows, p.cols, p.k_iters, pairs, OutType == SDVG_F32);
     p.tile_t = tile.tile_t;
     if constexpr (OutType != SDVG_F32) {
-      if (tile.subs == 2) return launch_pair<OutType, 2>(p, x, ld_x, w, ld_w, inner, pairs, stream);
+      constexpr int kVec = OutType == SDVG_E4M3 ? 16 : 8;       // elements of 16 bytes
+      const bool turned = sdvg::aligned16(p.out) && p.cols % kVec == 0 && p.ld_out % kVec == 0;
+      if (tile.subs == 2)
+        return turned ? launch_pair<OutType, 2, true>(p, x, ld_x, w, ld_w, inner, pairs, stream)
+                      : launch_pair<OutType, 2, false>(p, x, ld_x, w, ld_w, inner, pairs, stream);
+      if (turned) return launch_pair<OutType, 1, true>(p, x, ld_x, w, ld_w, inner, pairs, stream);
     }
-    return launch_pair<OutType, 1>(p, x, ld_x, w, ld_w, inner, pairs, stream);
+    return launch_pair<OutType, 1, false>(p, x, ld_x, w, ld_w, inner, pairs, stream);
   }
   p.tile_t = (p.rows + 15) / 16 * 16;
   p.tiles_f = (p.cols + kTileF - 1) / kTileF;

@@ -108,9 +108,37 @@ def test_shapes(rows, cols, inner, out):
 
 @pytest.mark.parametrize("rows", [5, 100])
 @pytest.mark.parametrize("act", list(ACTS))
-@pytest.mark.parametrize("out", ["bf16", "fp32", "e4m3"])
+@pytest.mark.parametrize("out", ["bf16", "fp16", "fp32", "e4m3"])
 def test_activations(rows, act, out):
-    check(problem(rows, 200, 300, out, act, residual="" if out == "e4m3" else "broadcast", gate_rows=rows, seed=7))
+    for cols in (200, 201, 208):                               # whole vectors of 8, none, of 16
+        check(problem(rows, cols, 300, out, act, residual="" if out == "e4m3" else "broadcast", gate_rows=rows, seed=7))
+
+
+@pytest.mark.parametrize("out", ["bf16", "fp16", "e4m3"])
+@pytest.mark.parametrize("cols,ld_out,gate_rows", [(192, 192, 1), (192, 200, 7), (320, 336, 40), (16, 16, 100), (48, 64, 3), (176, 192, 100)])
+def test_outputs_of_whole_vectors(out, cols, ld_out, gate_rows):
+    """Gates that change within a block of tokens, strides wider than the rows, features that end inside a warp's 32."""
+    for rows in (65, 130, 333):
+        s = problem(rows, cols, 260, out, "silu", gate_rows=gate_rows, residual="" if out == "e4m3" else "rows", seed=rows + cols)
+        check(s, ld_out=ld_out)
+        if out != "e4m3":
+            check(s, ld_out=ld_out, in_place=True)
+
+
+@pytest.mark.parametrize("rows", [64, 65])
+@pytest.mark.parametrize("act", ["silu", "gelu_tanh", "gelu"])
+def test_infinite_sums_and_far_tails(rows, act):
+    """Through the bias: infinities, NaN and values whose activation underflows, next to ordinary ones."""
+    s = problem(rows, 128, 128, "bf16", act, seed=41)
+    s["bias"][:8] = torch.tensor([float("inf"), float("-inf"), float("nan"), -1e4, 1e4, -60.0, 60.0, 0.0])
+    out = torch.empty((rows, 128), device="cuda", dtype=torch.bfloat16)
+    call(s, out, api.attn_workspace())
+    torch.cuda.synchronize()
+    got = f64(out)
+    ref, tol = expected(s, torch.bfloat16)
+    assert np.isposinf(got[:, 0]).all() and np.isnan(got[:, 2]).all()
+    assert (np.isnan(got[:, 1]) | (got[:, 1] == 0)).all()      # -inf times 0, or 0 by its limit
+    assert (np.abs(got[:, 3:] - ref[:, 3:]) <= tol[:, 3:]).all()
 
 
 @pytest.mark.parametrize("rows,cols,inner", [(3, 300, 1400), (90, 300, 1400), (90, 1, 600)])
