@@ -14,6 +14,7 @@
 
 #include <algorithm>
 #include <mutex>
+#include <type_traits>
 
 #include "e4m3_scale.cuh"
 #include "elem_types.cuh"
@@ -45,6 +46,7 @@ struct alignas(64) Linear8Params : EpilogueParams {
   int tile_t, tiles_f, tiles_t, k_iters, stages;
   int split;                                         // CTAs (a cluster) that share a tile's sum; tiles only
   int group;                                         // feature tiles of a group of the tile order (pairs)
+  int whole;                                         // sums are not cut into chunks (pairs)
   long long tiles;
   uint32_t idesc;
   unsigned int* status;
@@ -79,7 +81,11 @@ __device__ __forceinline__ void stage_scales(uint4* to, const uint8_t* scale, lo
 
 // fp32 outputs: the tensor core adds products to the accumulator by truncation, so a long sum drifts; there it is cut into chunks
 // that are added with round-to-nearest, as in linear.cu.  A step of the 8-bit kind adds 32 products, twice those of the 16-bit
-// kind, so that chunks are twice as long for the same drift.
+// kind, and drifts half as much.  Relative errors at inner = 5120 and 20480 (the worst case, all terms positive, in brackets): in one go
+// 3.4e-7 and 2.0e-6 (1.9e-6 and 1.2e-5), in chunks of 1280 1e-7 (2.5e-7), fp32 sums of a library product 1e-7 (2.4e-7).
+// Sums of up to 6144 go in one: a chunked sum's total takes the room of larger tiles (4680 x 5120 x 5120: 152 us in two
+// chunks of 2560, 101 in one).  Few tokens have the time: chunks of 512.
+constexpr int kWholeIters = 6144 / kTileK;
 constexpr int kPairChunkIters = 2560 / kTileK;
 constexpr int kTileChunkIters = 512 / kTileK;
 
@@ -146,20 +152,6 @@ struct FragGate {
   TileGate of[4];
 };
 
-template <int OutType>
-__device__ __forceinline__ void load_residual_frag(const Linear8Params& p, typename OutElem<OutType>::T (&res)[16], const Lane& l, int m_end) {
-  using T = typename OutElem<OutType>::T;
-  if (!p.residual) return;
-#pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    if (l.token(k) >= m_end) continue;
-    const T* r = static_cast<const T*>(p.residual) + l.token(k) * p.ld_res + l.n;
-#pragma unroll
-    for (int f = 0; f < 4; ++f)
-      if (l.n + 8 * f < p.cols) res[4 * f + k] = r[8 * f];
-  }
-}
-
 // activate16 in packed pairs, which is what an epilogue of 8-bit products has time for: the constants of an exponential's argument
 // are multiplied out (z is -u log2 e), a quotient is one reciprocal, whose limits are those of activate16: past 2^126 it is 0.
 __device__ __forceinline__ rows::Pair exp2_pair(rows::Pair z) {
@@ -220,20 +212,97 @@ __device__ __forceinline__ void gated_frag(const Linear8Params& p, float (&v)[16
   }
 }
 
-// 16-bit outputs.
+template <int OutType>
+__device__ __forceinline__ uint32_t pack16(float a, float b) {
+  if constexpr (OutType == SDVG_BF16) {
+    const __nv_bfloat162 x = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&x);
+  } else {
+    const __half2 x = __floats2half2_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&x);
+  }
+}
+
+// Residual of the 16 tokens, requested a block ahead of its use: lane i takes four features from 4 (i % 8) on of tokens i / 8, + 4, + 8 and
+// + 12, as it will store them.
+template <int OutType>
+struct Residual {
+  using Vec = typename std::conditional<OutType == SDVG_F32, uint4, uint2>::type;
+  Vec v[4];
+  __device__ __forceinline__ void load(const Linear8Params& p, int n0, int m, int m_end) {
+    using T = typename OutElem<OutType>::T;
+    if (!p.residual) return;
+    const int lane = threadIdx.x % 32, n = n0 + lane % 8 * 4;
+    const T* r = static_cast<const T*>(p.residual) + (m + lane / 8) * p.ld_res + n;
+    const long long step = 4 * p.ld_res;
+#pragma unroll
+    for (int i = 0; i < 4; ++i, r += step)
+      if (m + lane / 8 + 4 * i < m_end && n < p.cols) v[i] = *reinterpret_cast<const Vec*>(r);
+  }
+  __device__ __forceinline__ void add(int i, float (&f)[4]) const {
+    if constexpr (OutType == SDVG_F32) {
+      const uint4 x = v[i];
+      f[0] += __uint_as_float(x.x), f[1] += __uint_as_float(x.y), f[2] += __uint_as_float(x.z), f[3] += __uint_as_float(x.w);
+    } else {
+      const uint32_t w[2] = {v[i].x, v[i].y};
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        float2 x;
+        if constexpr (OutType == SDVG_BF16) x = make_float2(rows::bf16_lo(w[k]), rows::bf16_hi(w[k]));
+        else x = __half22float2(*reinterpret_cast<const __half2*>(&w[k]));
+        f[2 * k] += x.x;
+        f[2 * k + 1] += x.y;
+      }
+    }
+  }
+};
+
+// fp32 outputs, and 16-bit ones with a residual, which is added before they are rounded: 8 tokens at a time are turned as fp32.
+template <int OutType>
+__device__ __forceinline__ void store_frag32(const Linear8Params& p, const float (&v)[16], const Residual<OutType>& res, const Lane& l,
+                                             int m_end, uint32_t turn) {
+  using T = typename OutElem<OutType>::T;
+  const int lane = threadIdx.x % 32, g = lane / 4, n = l.n - g + lane % 8 * 4;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    // token t of the eight: 128 bytes at 128 t, whose 16-byte pieces are moved round so that neither side meets a bank twice
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const int t = 2 * l.q + k;
+#pragma unroll
+      for (int f = 0; f < 4; ++f)
+        asm volatile("st.shared.f32 [%0], %1;" ::"r"(turn + t * 128 + ((g / 4 + 2 * f) ^ t) * 16 + g % 4 * 4), "f"(v[4 * f + 2 * h + k])
+                     : "memory");
+    }
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int t = lane / 8 + 4 * i, m = l.m + 8 * h + t;
+      float f[4];
+      asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(f[0]), "=f"(f[1]), "=f"(f[2]), "=f"(f[3])
+                   : "r"(turn + t * 128 + ((lane % 8) ^ t) * 16) : "memory");
+      if (p.residual) res.add(2 * h + i, f);
+      if (m < m_end && n < p.cols) {
+        T* o = static_cast<T*>(p.out) + m * p.ld_out + n;
+        if constexpr (OutType == SDVG_F32) {
+          *reinterpret_cast<float4*>(o) = make_float4(f[0], f[1], f[2], f[3]);
+        } else {
+          *reinterpret_cast<uint2*>(o) = make_uint2(pack16<OutType>(f[0], f[1]), pack16<OutType>(f[2], f[3]));
+        }
+      }
+    }
+    __syncwarp();
+  }
+}
+
+// 16-bit outputs without a residual.
 template <int OutType>
 __device__ __forceinline__ void store_frag(const Linear8Params& p, const float (&v)[16], const Lane& l, int m_end, uint32_t turn) {
   const int lane = threadIdx.x % 32;
   uint32_t h[8];                                       // of two neighbouring tokens: [feature block][tokens 0 and 1, or 8 and 9]
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    if constexpr (OutType == SDVG_BF16) {
-      const __nv_bfloat162 x = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
-      h[i] = *reinterpret_cast<const uint32_t*>(&x);
-    } else {
-      const __half2 x = __floats2half2_rn(v[2 * i], v[2 * i + 1]);
-      h[i] = *reinterpret_cast<const uint32_t*>(&x);
-    }
+    h[i] = pack16<OutType>(v[2 * i], v[2 * i + 1]);
   }
   // token t of the block: 64 bytes at 64 t, whose 16-byte pieces are moved round so that neither side meets a bank twice
   auto at = [&](int t, int piece) { return turn + t * 64 + (piece ^ (t / 2 % 4)) * 16; };
@@ -552,10 +621,8 @@ constexpr int kMaxTileT = 240, kMaxTileChunked = 160;
 constexpr int kScaleCol = 480, kPairScaleCols = 16;
 constexpr int kAccs = 2;
 constexpr int kSkew = 3;
-template <int OutType>
-constexpr int kAccStride = OutType == SDVG_F32 ? kMaxTileChunked : kMaxTileT;
 // A chunked sum has its total behind the accumulators.
-static_assert((kAccs + 1) * kAccStride<SDVG_F32> <= kScaleCol && kAccs * kAccStride<SDVG_BF16> <= kScaleCol);
+static_assert((kAccs + 1) * kMaxTileChunked <= kScaleCol && kAccs * kMaxTileT <= kScaleCol);
 static_assert(kScaleCol + 2 * kPairScaleCols <= 512);
 
 // A word of scales of the CTA's features, and of the tile's tokens.
@@ -579,8 +646,7 @@ static_assert(sizeof(PairSmem) <= 3072 - 512);
 template <int OutType, int SUBS, bool TURNED>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
     linear8_pair_kernel(const __grid_constant__ Linear8Params p) {
-  constexpr bool kChunked = OutType == SDVG_F32, kOut8 = OutType == SDVG_E4M3;
-  static_assert(!kChunked || SUBS == 1);
+  constexpr bool kChunked = OutType == SDVG_F32 && SUBS == 1, kOut8 = OutType == SDVG_E4M3;
   using T = typename OutElem<OutType>::T;
   extern __shared__ uint8_t raw[];
   __shared__ PairSmem sm;
@@ -592,7 +658,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
   const int stage_bytes = pair_stage_bytes<SUBS>(p.tile_t);
   uint8_t* slots = buf + p.stages * stage_bytes;
   const uint32_t turn_space = smem_u32(slots + kScaleSlots * kPairSlotBytes<SUBS>) + (TURNED ? warp % kEpiWarps * kTurnBytes : 0);
-  const int chunks = kChunked ? (p.k_iters + kPairChunkIters - 1) / kPairChunkIters : 1;
+  const int chunks = p.whole ? 1 : (p.k_iters + kPairChunkIters - 1) / kPairChunkIters;
   const int words = (p.k_iters + kWordStages - 1) / kWordStages;
   sdvg::overlap_begin();
   if (threadIdx.x == 0) {
@@ -623,6 +689,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
   cluster_wait();                                    // the other CTA's barriers are initialised as well
   tc_fence_after();
   const uint32_t tmem = sm.tmem;
+  const int acc_stride = kChunked && !p.whole ? kMaxTileChunked : kMaxTileT;
   sdvg::overlap_wait();
 
   if (warp == kEpiWarps) {
@@ -685,7 +752,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
         const uint32_t scales = tmem + kScaleCol + ((word_slot - 1 - behind) & 1) * kPairScaleCols;
 #pragma unroll
         for (int kk = 0; kk < 4; ++kk)
-          mma_ss_mx_pair(tmem + b * kAccStride<OutType>, da + 2 * kk, db + 2 * kk, idesc, scales + 4 * sub, scales + 4 * SUBS, onto || kk > 0);
+          mma_ss_mx_pair(tmem + b * acc_stride, da + 2 * kk, db + 2 * kk, idesc, scales + 4 * sub, scales + 4 * SUBS, onto || kk > 0);
       };
       RingPos r, acc;
       bool ok = true;
@@ -693,7 +760,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
         if constexpr (SUBS == 1) {
           for (int c = 0; ok && c < chunks; ++c, acc.next(kAccs)) {
             if (!(ok = wait_for(&sm.acc_empty[acc.stage], acc.phase ^ 1, p.status, kWaitLimitNs))) break;
-            const int i0 = c * kPairChunkIters, i1 = kChunked ? min(p.k_iters, i0 + kPairChunkIters) : p.k_iters;
+            const int i0 = c * kPairChunkIters, i1 = p.whole ? p.k_iters : min(p.k_iters, i0 + kPairChunkIters);
             for (int i = i0; i < i1; ++i, r.next(p.stages)) {
               if (!(ok = arrived(i, r))) break;
               multiply(i, r, 0, acc.stage, i > i0, 0);
@@ -775,6 +842,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
         float bias[TURNED ? 4 : 1];
         FragGate gate;
         T ahead[16];
+        Residual<OutType> vectors;
         Lane at{n0 + lane / 4, m0 + part * 16, lane % 4};
         if constexpr (TURNED) {
 #pragma unroll
@@ -782,7 +850,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
             bias[f] = p.bias && at.n + 8 * f < p.cols ? p.bias[at.n + 8 * f] : 0.f;
             gate.of[f] = tile_gate(p, at.n + 8 * f, m0, m_end);
           }
-          if constexpr (!kOut8) load_residual_frag<OutType>(p, ahead, at, m_end);
+          if constexpr (!kOut8 && !kChunked) vectors.load(p, n0, at.m, m_end);
         } else {
           bias[0] = p.bias && n < p.cols ? p.bias[n] : 0.f;
           gate.of[0] = tile_gate(p, n, m0, m_end);
@@ -794,13 +862,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
         const bool summed = kChunked && chunks > 1;
         if (summed)
           ok = add_chunks<kAccs, (kMaxTileChunked / 16 + kParts - 1) / kParts>(
-              chunks, lanes, kAccStride<OutType>, kAccs * kAccStride<OutType>, [&](int i) { return (i * kParts + part) * 16; }, m_end - m0, r,
+              chunks, lanes, acc_stride, kAccs * acc_stride, [&](int i) { return (i * kParts + part) * 16; }, m_end - m0, r,
               sm.acc_full, p.status, release);
         else
           ok = __all_sync(0xffffffffu, wait_for(&sm.acc_full[r.stage], r.phase, p.status, kWaitLimitNs));
         if (!ok) break;
         tc_fence_after();
-        const uint32_t sums = lanes + (summed ? kAccs : r.stage) * kAccStride<OutType>;
+        if constexpr (TURNED && kChunked) vectors.load(p, n0, at.m, m_end);        // not before: a chunked sum needs the registers
+        const uint32_t sums = lanes + (summed ? kAccs : r.stage) * acc_stride;
 #pragma unroll 1
         for (int col = part * 16; m0 + col < m_end; col += 16 * kParts) {
           float acc[16];
@@ -819,14 +888,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
             if constexpr (kOut8) {
               if (!(ok = quantise_frag(p, sm.exchange[part], turn, acc, at, quad, m_end, turn_space))) break;
             } else {
-              if (p.residual) {
-#pragma unroll
-                for (int i = 0; i < 16; ++i) acc[i] += OutElem<OutType>::get(ahead[i]);
+              if (OutType == SDVG_F32 || p.residual) {
+                store_frag32<OutType>(p, acc, vectors, at, m_end, turn_space);
+                vectors.load(p, n0, m0 + col + 16 * kParts, m_end);
+              } else if constexpr (OutType != SDVG_F32) {
+                store_frag<OutType>(p, acc, at, m_end, turn_space);
               }
-              at.m += 16 * kParts;
-              load_residual_frag<OutType>(p, ahead, at, m_end);
-              at.m = m0 + col;
-              store_frag<OutType>(p, acc, at, m_end, turn_space);
             }
           } else {
             tmem_ld16(sums + col, reinterpret_cast<uint32_t(&)[16]>(acc));
@@ -943,11 +1010,9 @@ int set_up(int* pairs) {
     if (e != cudaSuccess) return sdvg::cuda_status(e);
     int n = 0x7fffffff;
     e = set_up_pair<OutType, 1, false>(&n);
-    if constexpr (OutType != SDVG_F32) {
-      if (e == cudaSuccess) e = set_up_pair<OutType, 2, false>(&n);
-      if (e == cudaSuccess) e = set_up_pair<OutType, 1, true>(&n);
-      if (e == cudaSuccess) e = set_up_pair<OutType, 2, true>(&n);
-    }
+    if (e == cudaSuccess) e = set_up_pair<OutType, 2, false>(&n);
+    if (e == cudaSuccess) e = set_up_pair<OutType, 1, true>(&n);
+    if (e == cudaSuccess) e = set_up_pair<OutType, 2, true>(&n);
     if (e != cudaSuccess || n < 1) return sdvg::cuda_status(e != cudaSuccess ? e : cudaErrorUnknown);
     pairs_of_device[dev] = n;
   }
@@ -961,7 +1026,7 @@ constexpr int kTileEnd = 1500;
 struct PairTile {
   int subs, tile_t;
 };
-PairTile choose_tile(int rows, int cols, int k_iters, int pairs, bool chunked) {
+PairTile choose_tile(int rows, int cols, int k_iters, int pairs, bool chunked) {          // chunked: a sum in several chunks
   PairTile best{1, 0};
   long long best_cost = 0;
   for (int subs = 1; subs <= (chunked ? 1 : 2); ++subs)
@@ -1001,17 +1066,18 @@ int launch(Linear8Params& p, const void* x, int64_t ld_x, const void* w, int64_t
   int st = set_up<OutType>(&pairs);
   if (st != SDVG_OK) return st;
   if (p.rows > kPairRows) {
-    const PairTile tile = choose_tile(p.rows, p.cols, p.k_iters, pairs, OutType == SDVG_F32);
+    p.whole = OutType != SDVG_F32 || p.k_iters <= kWholeIters;
+    const PairTile tile = choose_tile(p.rows, p.cols, p.k_iters, pairs, !p.whole);
     p.tile_t = tile.tile_t;
-    if constexpr (OutType != SDVG_F32) {
-      constexpr int kVec = OutType == SDVG_E4M3 ? 16 : 8;       // elements of 16 bytes
-      const bool turned = sdvg::aligned16(p.out) && p.cols % kVec == 0 && p.ld_out % kVec == 0;
-      if (tile.subs == 2)
-        return turned ? launch_pair<OutType, 2, true>(p, x, ld_x, w, ld_w, inner, pairs, stream)
-                      : launch_pair<OutType, 2, false>(p, x, ld_x, w, ld_w, inner, pairs, stream);
-      if (turned) return launch_pair<OutType, 1, true>(p, x, ld_x, w, ld_w, inner, pairs, stream);
-    }
-    return launch_pair<OutType, 1, false>(p, x, ld_x, w, ld_w, inner, pairs, stream);
+    constexpr int kVec = OutType == SDVG_E4M3 ? 16 : OutType == SDVG_F32 ? 4 : 8;          // elements of 16 bytes
+    constexpr uintptr_t kResBytes = OutType == SDVG_F32 ? 16 : 8;                           // four of the residual's
+    const bool turned = sdvg::aligned16(p.out) && p.cols % kVec == 0 && p.ld_out % kVec == 0 &&
+                        (!p.residual || (reinterpret_cast<uintptr_t>(p.residual) % kResBytes == 0 && p.ld_res % 4 == 0));
+    if (tile.subs == 2)
+      return turned ? launch_pair<OutType, 2, true>(p, x, ld_x, w, ld_w, inner, pairs, stream)
+                    : launch_pair<OutType, 2, false>(p, x, ld_x, w, ld_w, inner, pairs, stream);
+    return turned ? launch_pair<OutType, 1, true>(p, x, ld_x, w, ld_w, inner, pairs, stream)
+                  : launch_pair<OutType, 1, false>(p, x, ld_x, w, ld_w, inner, pairs, stream);
   }
   p.tile_t = (p.rows + 15) / 16 * 16;
   p.tiles_f = (p.cols + kTileF - 1) / kTileF;
