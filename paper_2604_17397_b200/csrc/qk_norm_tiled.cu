@@ -128,8 +128,8 @@ __global__ void __launch_bounds__(kThreads, 1) qk_tiled_kernel(const __grid_cons
   const int t0 = tile * kTile, count = min(kTile, p.tokens - t0);
   const int group = threadIdx.x / kGroupThreads, id = threadIdx.x % kGroupThreads, j = id % 16, r0 = id / 16;
   uint4* ring = s_dynamic + kTurnBytes / 16 + group * kSlots * kItemVecs + id;
-  // The pass over the rows lets this kernel begin when all before it in the stream is done and seen: only its own factors are
-  // still to come.
+  // The pass over the rows lets this kernel begin when all before it in the stream is done and written: only its own factors are
+  // still to come.  What is read before they are goes past the L1 cache.
   if (HEAD) sdvg::overlap_wait();
 
   Walk asked{0, group};
@@ -175,7 +175,7 @@ __global__ void __launch_bounds__(kThreads, 1) qk_tiled_kernel(const __grid_cons
   const int per_place = axis == 0 ? p.pairs_f : axis == 1 ? p.pairs_h : pairs_w;
 #pragma unroll
   for (int t = threadIdx.x / 64; t < kTile; t += kThreads / 64)
-    reinterpret_cast<float2*>(s_turn)[t * 64 + pr % 4 / 2 * 32 + pr / 4 * 2 + pr % 2] = of_pair[(long long)s_place[axis][t] * per_place];
+    reinterpret_cast<float2*>(s_turn)[t * 64 + pr % 4 / 2 * 32 + pr / 4 * 2 + pr % 2] = __ldcg(of_pair + (long long)s_place[axis][t] * per_place);
   if (!HEAD) sdvg::overlap_wait();
   for (int i = threadIdx.x; i < p.jobs * kTile; i += kThreads) {
     const TileJob& job = p.job[i / kTile];

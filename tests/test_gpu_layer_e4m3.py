@@ -128,3 +128,79 @@ def test_time_modulation_in_8_bits(rows):
     ref = D.linear_ref(e, f64(tm.w_mod), f64(tm.b_mod))
     # three products of two operands each, off by at most 2^-4 of a value, on a path of gain about one; the offsets are exact
     assert np.linalg.norm(f64(got) - f64(tm.offsets) - ref) <= 6 * 2.0 ** -4 * np.linalg.norm(ref)
+
+
+@pytest.mark.parametrize("tiled", [False, True])
+@pytest.mark.parametrize("scope", ["row", "head"])
+def test_the_ring_write_sees_what_the_calls_before_it_wrote(tiled, scope):
+    """Rows, norm weights and rotary table rewritten in place just before each call; launches overlap, results are those of calls with a
+    wait between them."""
+    gen = torch.Generator(device="cuda").manual_seed(42)
+    heads, grid, ws = 6, (2, 10, 15), api.attn_workspace()
+    tokens, c = 300, 6 * 128
+    width = c if scope == "row" else 128
+    h, hs = api.e4m3_matrix(tokens, 256)
+    rows = [randn(gen, tokens, 256).bfloat16() for _ in range(4)]
+    w, wsc = api.e4m3_matrix(3 * c, 256, 128)
+    api.sdvg_quant_e4m3_blocks(randn(gen, 3 * c, 256, std=1 / 16), w, wsc)
+    feats, u = [randn(gen, 1, 64).bfloat16() for _ in range(4)], randn(gen, width, 64, std=1 / 8).bfloat16()
+    qkv, weight = torch.zeros((tokens, 3 * c), device="cuda", dtype=torch.bfloat16), torch.zeros((1, width), device="cuda")
+    q, k, v = (qkv[:, i * c:(i + 1) * c].view(tokens, heads, 128) for i in range(3))
+    tables = [api.sdvg_rope3d_table(128, n, 10, 15).cuda()[:api.lib().sdvg_rope3d_table_floats(128, 2, 10, 15)] for n in (2, 3, 4, 5)]
+    table = torch.zeros_like(tables[0])
+    cache = api.Cache(2, heads, tokens, 128, e4m3=True, tile_scales=tiled)
+    inv, space = torch.full((heads,), 30.0, device="cuda"), api.qk_norm_workspace(tokens)
+    sc = api.SDVG_SCOPE_ROW if scope == "row" else api.SDVG_SCOPE_HEAD
+
+    def chain(sync):
+        outs = torch.zeros((24, tokens, heads, 128), device="cuda", dtype=torch.uint8)
+        scales = torch.zeros((24, heads, 3), device="cuda")
+        pause = torch.cuda.synchronize if sync else lambda: None
+        pause()
+        for i, out in enumerate(outs):
+            table.copy_(tables[i % 4])
+            pause()
+            api.sdvg_linear(feats[i % 4], u, weight, ws)
+            pause()
+            api.sdvg_gated_norm_e4m3(rows[i % 4], h, hs, norm=api.SDVG_NORM_RMS)
+            pause()
+            api.sdvg_linear_e4m3(h, hs, w, wsc, qkv, ws)
+            pause()
+            args = (cache, q, k, v, weight[0], weight[0], sc, 1e-6, out)
+            at = (grid, 0, table, 2, 0, api.SDVG_STAGE)
+            if tiled:
+                api.sdvg_qk_norm_rope3d_commit_e4m3_tiled(*args, scales[i], *at, space)
+            else:
+                api.sdvg_qk_norm_rope3d_commit_e4m3(*args, inv, inv, inv, *at)
+            pause()
+        torch.cuda.synchronize()
+        return outs, scales, *cache.read_block(0)
+
+    want = chain(True)
+    assert not torch.equal(want[0][0], want[0][1]) and torch.equal(want[0][0], want[0][4])
+    for _ in range(5):
+        assert all(torch.equal(a, b) for a, b in zip(chain(False), want))
+
+
+def test_two_streams_with_workspaces_of_their_own():
+    """The same ring shapes written at once from two streams, each with its own cache and workspaces."""
+    made = []
+    for seed in (1, 2):
+        m = model(ODD, **RINGS["tiled"])
+        made.append((schedule.TransformerLayerE4M3(weights(ODD, seed), m), m, *stream(ODD, 40 + seed), torch.cuda.Stream()))
+    want = []
+    for layer, m, x, mod, _ in made:
+        out = torch.empty_like(x)
+        layer.step(x, mod, 0, out)
+        torch.cuda.synchronize()
+        want.append((out.clone(), m.q_roped.clone()))
+    for _ in range(10):
+        outs = []
+        for layer, m, x, mod, s in made:
+            with torch.cuda.stream(s):
+                out = torch.empty_like(x)
+                layer.step(x, mod, 0, out)
+                outs.append(out)
+        torch.cuda.synchronize()
+        for (o, q), got, (_, m, *_) in zip(want, outs, made):
+            assert torch.equal(got, o) and torch.equal(m.q_roped, q)
