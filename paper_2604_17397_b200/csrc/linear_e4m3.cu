@@ -983,7 +983,7 @@ int make_map(CUtensorMap* m, const void* base, int inner, int rows, int64_t ld, 
 
 std::mutex g_setup_mu;
 
-constexpr int kPairRows = kMaxTileFew;               // more tokens than this go to the pairs
+constexpr int kPairRows = kMaxTileFew;               // up to so many tokens pairs are not considered
 
 // As many stages as leave room for two CTAs on an SM: five up to 32 tokens (3% faster than four), four beyond.
 constexpr int tile_stages(int tile_t) { return tile_t <= 32 ? 5 : 4; }
@@ -1057,23 +1057,37 @@ int set_up(int* pairs) {
   return SDVG_OK;
 }
 
-// Features (SUBS x 256) and tokens of a pair's tile: the sizes whose waves of tiles cost least.  A stage costs the bytes it brings to an
-// SM, those of SUBS x 128 features and half the tokens; a tile's end costs about kTileEnd stages' worth of a token.
-constexpr int kTileEnd = 1500;
-struct PairTile {
-  int subs, tile_t;
+// How a product is cut: tiles of 128 features x tile_t tokens by clusters of `split` CTAs, or (subs > 0) tiles of subs x 256 features x tile_t
+// tokens by pairs.  The cheapest by these estimates, in clocks, whose constants were fitted to times of both kinds at 45 sizes:
+// a stage costs the bytes it brings to an SM, 56 of them a clock where CTAs come one or two to an SM, 36 and 43 for pairs, but not
+// less than its barriers and instructions; a split sum is joined; pairs take longer to begin and end.  Pairs against small
+// tiles, in us: 100 x 5120 x 1536 17.4 and 9.4, 333 x 5120 x 776 16.8 and 9.7, 1500 x 1536 x 1536 10.1 and 8.2, 300 x 5120 x 4000 18.3
+// and 15.2, 512 x 4096 x 5120 17.3 and 23.9.
+struct Cut {
+  int subs, tile_t, split;
+  double cost;
 };
-PairTile choose_tile(int rows, int cols, int k_iters, int pairs, bool chunked) {          // chunked: a sum in several chunks
-  PairTile best{1, 0};
-  long long best_cost = 0;
+Cut choose_cut(int rows, int cols, int k_iters, int pairs, bool chunked) {                // chunked: the pairs' sum in several chunks
+  auto ceil_div = [](long long a, long long b) { return (a + b - 1) / b; };
+  const int sms = 2 * pairs;
+  Cut best{0, 0, 0, 0};
+  auto offer = [&](const Cut& c) {
+    if (!best.tile_t || c.cost < best.cost) best = c;
+  };
+  const int most = (std::min(rows, kMaxTileFew) + 15) / 16 * 16;
+  for (int nt = most; nt >= std::min(most, 32); nt -= 16) {
+    const long long tiles = ceil_div(cols, kTileF) * ceil_div(rows, nt);
+    const int split = tile_split(tiles, k_iters, nt, sms);
+    const long long on_sm = std::min(2ll, ceil_div(tiles * split, sms)), waves = ceil_div(tiles * split, 2 * sms);
+    const double stage = std::max(250.0, on_sm * (kTileF + nt) * 128 / 56.0);
+    offer({0, nt, split, waves * ceil_div(k_iters, split) * stage + (split > 1 ? 1000 + 300 * split + 45 * nt : 0)});
+  }
+  if (rows <= kPairRows) return best;
   for (int subs = 1; subs <= (chunked ? 1 : 2); ++subs)
     for (int nt = chunked ? kMaxTileChunked : kMaxTileT; nt >= 64; nt -= 16) {
-      const long long tiles = (long long)((cols + 256 * subs - 1) / (256 * subs)) * ((rows + nt - 1) / nt);
-      const long long cost = (tiles + pairs - 1) / pairs * ((long long)k_iters * (nt + 256 * subs) + kTileEnd * subs);
-      if (!best_cost || cost < best_cost) {
-        best = PairTile{subs, nt};
-        best_cost = cost;
-      }
+      const long long waves = ceil_div(ceil_div(cols, 2 * kTileF * subs) * ceil_div(rows, nt), pairs);
+      const double stage = std::max(470.0, (kTileF * subs + nt / 2) * 128 / (subs == 2 ? 43.0 : 36.0));
+      offer({subs, nt, 1, 4500 + waves * (k_iters * stage + 2500 * subs)});
     }
   return best;
 }
@@ -1102,28 +1116,35 @@ int launch(Linear8Params& p, const void* x, int64_t ld_x, const void* w, int64_t
   int pairs = 0;
   int st = set_up<OutType>(&pairs);
   if (st != SDVG_OK) return st;
-  if (p.rows > kPairRows) {
-    p.whole = OutType != SDVG_F32 || p.k_iters <= kWholeIters;
-    const PairTile tile = choose_tile(p.rows, p.cols, p.k_iters, pairs, !p.whole);
-    p.tile_t = tile.tile_t;
+  p.whole = OutType != SDVG_F32 || p.k_iters <= kWholeIters;
+  // a program makes the same products over and over: the last answer is kept, which takes a third of a microsecond to find
+  static thread_local int known[5] = {};
+  static thread_local Cut cut = {};
+  const int asked[5] = {p.rows, p.cols, p.k_iters, pairs, p.whole};
+  if (!std::equal(asked, asked + 5, known)) {
+    cut = choose_cut(p.rows, p.cols, p.k_iters, pairs, !p.whole);
+    std::copy(asked, asked + 5, known);
+  }
+  p.tile_t = cut.tile_t;
+  if (cut.subs) {
     constexpr int kVec = OutType == SDVG_E4M3 ? 16 : OutType == SDVG_F32 ? 4 : 8;          // elements of 16 bytes
     constexpr uintptr_t kResBytes = OutType == SDVG_F32 ? 16 : 8;                           // four of the residual's
     const bool turned = sdvg::aligned16(p.out) && p.cols % kVec == 0 && p.ld_out % kVec == 0 &&
                         (!p.residual || (reinterpret_cast<uintptr_t>(p.residual) % kResBytes == 0 && p.ld_res % 4 == 0));
-    if (tile.subs == 2)
+    if (cut.subs == 2)
       return turned ? launch_pair<OutType, 2, true>(p, x, ld_x, w, ld_w, inner, pairs, stream)
                     : launch_pair<OutType, 2, false>(p, x, ld_x, w, ld_w, inner, pairs, stream);
     return turned ? launch_pair<OutType, 1, true>(p, x, ld_x, w, ld_w, inner, pairs, stream)
                   : launch_pair<OutType, 1, false>(p, x, ld_x, w, ld_w, inner, pairs, stream);
   }
-  p.tile_t = (p.rows + 15) / 16 * 16;
   p.tiles_f = (p.cols + kTileF - 1) / kTileF;
-  p.tiles_t = 1;
-  p.tiles = p.tiles_f;
+  p.tiles_t = (p.rows + p.tile_t - 1) / p.tile_t;
+  p.tiles = (long long)p.tiles_f * p.tiles_t;
+  if (p.tiles >= 1ll << 28) return SDVG_ERR_BAD_SHAPE;
   p.idesc = idesc_mx_e4m3(kTileF, p.tile_t);
   if ((st = make_map(&p.w_map, w, inner, p.cols, ld_w, kTileF)) != SDVG_OK) return st;
   if ((st = make_map(&p.x_map, x, inner, p.rows, ld_x, p.tile_t)) != SDVG_OK) return st;
-  p.split = tile_split(p.tiles, p.k_iters, p.tile_t, 2 * pairs);
+  p.split = cut.split;
   p.stages = tile_stages(p.tile_t);
   return sdvg::cuda_status(sdvg::launch_overlapped(linear8_tile_kernel<OutType>, (unsigned)p.tiles * p.split, kTileThreads,
                                                    tile_dynamic(p.tile_t), p.split > 1 ? p.split : 0, stream, p));

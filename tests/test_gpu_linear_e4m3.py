@@ -331,3 +331,76 @@ def test_many_tiles(rows, cols, inner, out):
         tol = err + (ref.abs() + err) * torch.finfo(OUTS[out]).eps / 2
     assert bool(((got - ref).abs() <= tol).all())
     assert bool((o[rows] == 77).all())
+
+
+def bound_on_gpu(x, w, bias, act, gate, residual, dtype):
+    """linear_tolerance and the reference, in 64 bits on the GPU, for sizes that only pairs of CTAs take; gate per row or None."""
+    u = 2.0 ** -24
+    v = x @ w.t() + bias
+    err = (x.shape[1] + 2) * 2 * u * (x.abs() @ w.abs().t() + bias.abs())
+    a = v * torch.sigmoid(v) if act == "silu" else v
+    if act == "silu":
+        err = 1.13 * err + 2.0 ** -14 * a.abs() + 1e-36
+    g = torch.ones_like(a[:1]) if gate is None else gate
+    r = torch.zeros_like(a[:1]) if residual is None else residual
+    ref = g * a + r
+    err = g.abs() * err + 4 * u * ((g * a).abs() + r.abs())
+    return ref, err if dtype is None else err + (ref.abs() + err) * torch.finfo(dtype).eps / 2
+
+
+@pytest.mark.parametrize("out", ["bf16", "fp16", "fp32", "e4m3"])
+@pytest.mark.parametrize("cols,more,gate_rows,residual", [(3008, 0, 1, "rows"), (3016, 8, 7, "rows"), (3012, 4, 100, "broadcast"), (3013, 0, 300, "rows"),
+                                                          (3024, 16, 0, ""), (2990, 0, 777, "broadcast")])
+def test_outputs_of_pairs(out, cols, more, gate_rows, residual):
+    """Rows of whole vectors and not, strides wider than the rows, gates that change within a block of tokens, in place."""
+    rows, inner = 777, 1200
+    gen = torch.Generator(device="cuda").manual_seed(cols)
+    x, w = api.e4m3_matrix(rows, inner), api.e4m3_matrix(cols, inner, 128)
+    api.sdvg_quant_e4m3_blocks(randn(gen, rows, inner), *x)
+    api.sdvg_quant_e4m3_blocks(randn(gen, cols, inner, std=inner ** -0.5), *w)
+    bias, ws = randn(gen, cols), api.attn_workspace()
+    gate = randn(gen, -(-rows // gate_rows), cols) if gate_rows else None
+    per_row = None if gate is None else gate.double().repeat_interleave(gate_rows, 0)[:rows]
+    act = "silu" if gate_rows % 2 else "none"
+    dtype = OUTS[out]
+    res = None
+    if residual and out != "e4m3":
+        res = randn(gen, rows if residual == "rows" else 1, cols, std=2.0).to(dtype).expand(rows, cols)
+    buf = torch.full((rows + 2, cols + more), 77, device="cuda", dtype=dtype)
+    o = buf[1:-1, :cols]
+    ref, tol = bound_on_gpu(values_on_gpu(*x, 1), values_on_gpu(*w, 128), bias.double(), act, per_row, None if res is None else res.double(),
+                            None if out == "e4m3" else dtype)
+    for in_place in (False, residual == "rows" and res is not None):
+        if in_place:
+            o.copy_(res)
+        scale = torch.zeros((rows, -(-cols // 128)), device="cuda", dtype=torch.uint8) if out == "e4m3" else None
+        api.sdvg_linear_e4m3(*x, *w, o, ws, bias=bias, act=ACTS[act], gate=gate, gate_rows=gate_rows, residual=o if in_place else res,
+                             out_scale=scale)
+        assert api.sdvg_block_attn_status(ws) == api.SDVG_OK
+        if out == "e4m3":
+            f = torch.exp2(scale.double() - 127).repeat_interleave(128, 1)[:, :cols]
+            top = lambda a: torch.nn.functional.pad(a, (0, -cols % 128)).unflatten(1, (-1, 128)).amax(2)
+            assert bool((top(ref.abs() - tol) <= 448 * f[:, ::128]).all()) and bool((top(ref.abs() + tol) > 224 * f[:, ::128]).all())
+            got, within = o.view(torch.float8_e4m3fn).double() * f, tol + torch.maximum((ref.abs() + tol) / 16, f / 1024)
+        else:
+            got, within = o.double(), tol
+        assert bool(((got - ref).abs() <= within).all())
+        assert bool((buf[0] == 77).all()) and bool((buf[-1] == 77).all()) and bool((buf[:, cols:] == 77).all())
+
+
+@pytest.mark.parametrize("cols", [3000, 3001])
+@pytest.mark.parametrize("rows,inner", [(777, 6144), (777, 6272), (700, 7800)])
+def test_long_fp32_sums_of_pairs(rows, inner, cols):
+    gen = torch.Generator(device="cuda").manual_seed(inner)
+    x, w = api.e4m3_matrix(rows, inner), api.e4m3_matrix(cols, inner, 128)
+    api.sdvg_quant_e4m3_blocks(randn(gen, rows, inner).abs(), *x)                    # all terms of one sign: the drift adds up
+    api.sdvg_quant_e4m3_blocks(randn(gen, cols, inner, std=inner ** -0.5).abs(), *w)
+    res, bias, ws = randn(gen, rows, cols), randn(gen, cols), api.attn_workspace()
+    o = torch.full((rows, cols), float("nan"), device="cuda")
+    api.sdvg_linear_e4m3(*x, *w, o, ws, bias=bias, residual=res)
+    assert api.sdvg_block_attn_status(ws) == api.SDVG_OK
+    ref, tol = bound_on_gpu(values_on_gpu(*x, 1), values_on_gpu(*w, 128), bias.double(), "none", None, res.double(), torch.float32)
+    assert bool(((o.double() - ref).abs() <= tol).all())
+    # the truncation of the tensor core, 32 products at a time, off by at most half a step of the sum each on average: 2^-25 per step
+    # of a sum of up to 6144; later chunks are added to nearest
+    assert float((o.double() - ref).norm() / ref.norm()) <= 6144 / 32 * 2.0 ** -25
