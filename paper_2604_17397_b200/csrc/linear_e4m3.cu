@@ -36,7 +36,7 @@ constexpr int kWorkspaceBytes = 256;
 constexpr int kMaxDevices = 64;
 
 struct alignas(64) Linear8Params : EpilogueParams {
-  CUtensorMap w_map;                                 // box 128 x 128 features
+  CUtensorMap w_map;                                 // box 128 x the features of a CTA: 128, or 256 (pairs with SUBS = 2)
   CUtensorMap x_map;                                 // box 128 x tile_t tokens (tiles), or half of them (pairs)
   const uint8_t *x_scale, *w_scale;                  // exponent bytes: of row r and 128-element block b at scale[(r >> shift) * ld + b]
   long long ld_xs, ld_ws;
@@ -102,8 +102,8 @@ struct ScaleWords {
 // that are added with round-to-nearest, as in linear.cu.  A step of the 8-bit kind adds 32 products, twice those of the 16-bit
 // kind, and drifts half as much.  Relative errors at inner = 5120 and 20480 (the worst case, all terms positive, in brackets): in one go
 // 3.4e-7 and 2.0e-6 (1.9e-6 and 1.2e-5), in chunks of 1280 1e-7 (2.5e-7), fp32 sums of a library product 1e-7 (2.4e-7).
-// Sums of up to 6144 go in one: a chunked sum's total takes the room of larger tiles (4680 x 5120 x 5120: 152 us in two
-// chunks of 2560, 101 in one).  Few tokens have the time: chunks of 512.
+// Sums of up to 6144 go in one: a chunked sum's total is kept in registers, which hold a tile of 256 features and not one of 512
+// (4680 x 8192 x 5120 with gate and residual 230 us in chunks, 4680 x 5120 x 5120 131 in one).  Small tiles have the room: chunks of 512.
 constexpr int kWholeIters = 6144 / kTileK;
 constexpr int kPairChunkIters = 2560 / kTileK;
 constexpr int kTileChunkIters = 512 / kTileK;
@@ -403,9 +403,12 @@ __device__ __forceinline__ bool quantise_frag(const Linear8Params& p, Exchange& 
   return true;
 }
 
-// ---- few tokens: a cluster per tile, which splits `inner` ---------------------------------------
+// ---- small tiles: 128 features x 16 to 64 tokens, by a cluster that splits `inner` ------------------
+//
+// For few tokens, whose time is that of the weights' way from memory, and for small products of many, which would not give every
+// pair a tile (choose_cut).  Two CTAs share an SM: one multiplies while the other begins or ends.
 constexpr int kTileThreads = 224;                    // four epilogue warps, producer, issuer, scales
-constexpr int kMaxTileFew = 64;                      // tokens per tile
+constexpr int kMaxTileFew = 64;                      // tokens per tile, at most
 constexpr int kMaxSplit = 8;                         // portable cluster size
 constexpr int kTileSlotBytes = 1024;                 // a word of scales of the tile's features, and of its tokens
 constexpr int kTileScaleCols = 8;                    // and its columns in tensor memory
@@ -628,7 +631,7 @@ __global__ void __launch_bounds__(kTileThreads) linear8_tile_kernel(const __grid
   if (warp == 0) tmem_dealloc(tmem, tmem_cols);
 }
 
-// ---- many tokens: CTA pairs, persistent ---------------------------------------------------------
+// ---- large tiles: CTA pairs, persistent ---------------------------------------------------------
 //
 // A pair of CTAs (two SMs) works on a tile of SUBS x 256 features x tile_t tokens: each CTA holds SUBS x 128 of the features and fetches half
 // of the token tile, and one tcgen05.mma of the even CTA reads the operands of both.  Each CTA's tensor memory holds the
@@ -645,12 +648,11 @@ __global__ void __launch_bounds__(kTileThreads) linear8_tile_kernel(const __grid
 constexpr int kEpiWarps = 16;
 constexpr int kPairThreads = 32 * (kEpiWarps + 3);
 constexpr int kPairSmem = 227 * 1024 - 3072;         // dynamic shared memory of a CTA; the barriers and exchanges are static
-constexpr int kMaxTileT = 240, kMaxTileChunked = 160;
+constexpr int kMaxTileT = 240;
 constexpr int kScaleCol = 480, kPairScaleCols = 16;
 constexpr int kAccs = 2;
 constexpr int kSkew = 3;
-// A chunked sum has its total behind the accumulators.
-static_assert((kAccs + 1) * kMaxTileChunked <= kScaleCol && kAccs * kMaxTileT <= kScaleCol);
+static_assert(kAccs * kMaxTileT <= kScaleCol);
 static_assert(kScaleCol + 2 * kPairScaleCols <= 512);
 
 // A word of scales of the CTA's features, and of the tile's tokens.
@@ -669,6 +671,46 @@ struct PairSmem {
   uint32_t tmem;
 };
 static_assert(sizeof(PairSmem) <= 3072 - 512);
+
+// Adds the chunks of a sum in registers, round-to-nearest, 16 columns from `col`, col + 64, .. each, and leaves the total in the accumulator
+// of the last, which stays the caller's to release.  (A place of its own for the total left room for tiles of 160 tokens:
+// 4680 x 20480 x 5120 with gate and residual 638 us against 516, 4680 x 8192 x 5120 274 against 230.)
+template <class Release>
+__device__ __forceinline__ bool total_in_last(int chunks, uint32_t lanes, int col, int cols, RingPos& r, uint64_t* acc_full,
+                                              unsigned int* status, Release release) {
+  constexpr int kStep = 16 * kEpiWarps / 4, kSets = (kMaxTileT + kStep - 1) / kStep;
+  float sum[kSets][16];
+#pragma unroll
+  for (int i = 0; i < kSets; ++i)
+#pragma unroll
+    for (int j = 0; j < 16; ++j) sum[i][j] = 0.f;
+#pragma unroll 1
+  for (int c = 0;; ++c) {
+    if (!__all_sync(0xffffffffu, wait_for(&acc_full[r.stage], r.phase, status, kWaitLimitNs))) return false;
+    tc_fence_after();
+    const uint32_t part = lanes + r.stage * kMaxTileT + col;
+#pragma unroll
+    for (int i = 0; i < kSets; ++i)
+      if (col + i * kStep < cols) {
+        float v[16];
+        tmem_ld16(part + i * kStep, reinterpret_cast<uint32_t(&)[16]>(v));
+        tmem_wait_ld();
+#pragma unroll
+        for (int j = 0; j < 16; ++j) sum[i][j] += v[j];
+      }
+    if (c == chunks - 1) break;
+    tc_fence_before();
+    __syncwarp();
+    release(r.stage);
+    r.next(kAccs);
+  }
+#pragma unroll
+  for (int i = 0; i < kSets; ++i)
+    if (col + i * kStep < cols)
+      tmem_st16(lanes + r.stage * kMaxTileT + col + i * kStep, reinterpret_cast<uint32_t(&)[16]>(sum[i]));
+  tmem_wait_st();
+  return true;
+}
 
 // TURNED: the outputs go by way of shared memory.
 template <int OutType, int SUBS, bool TURNED>
@@ -717,7 +759,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
   cluster_wait();                                    // the other CTA's barriers are initialised as well
   tc_fence_after();
   const uint32_t tmem = sm.tmem;
-  const int acc_stride = kChunked && !p.whole ? kMaxTileChunked : kMaxTileT;
   sdvg::overlap_wait();
 
   if (warp == kEpiWarps) {
@@ -780,7 +821,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
         const uint32_t scales = tmem + kScaleCol + ((word_slot - 1 - behind) & 1) * kPairScaleCols;
 #pragma unroll
         for (int kk = 0; kk < 4; ++kk)
-          mma_ss_mx_pair(tmem + b * acc_stride, da + 2 * kk, db + 2 * kk, idesc, scales + 4 * sub, scales + 4 * SUBS, onto || kk > 0);
+          mma_ss_mx_pair(tmem + b * kMaxTileT, da + 2 * kk, db + 2 * kk, idesc, scales + 4 * sub, scales + 4 * SUBS, onto || kk > 0);
       };
       RingPos r, acc;
       bool ok = true;
@@ -881,32 +922,32 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
         T ahead[16];
         Residual<OutType> vectors;
         Lane at{n0 + lane / 4, m0 + part * 16, lane % 4};
-        if constexpr (TURNED) {
+        auto request = [&] {
+          if constexpr (TURNED) {
 #pragma unroll
-          for (int f = 0; f < 4; ++f) {
-            bias[f] = p.bias && at.n + 8 * f < p.cols ? p.bias[at.n + 8 * f] : 0.f;
-            gate.of[f] = tile_gate(p, at.n + 8 * f, m0, m_end);
+            for (int f = 0; f < 4; ++f) {
+              bias[f] = p.bias && at.n + 8 * f < p.cols ? p.bias[at.n + 8 * f] : 0.f;
+              gate.of[f] = tile_gate(p, at.n + 8 * f, m0, m_end);
+            }
+            if constexpr (!kOut8) vectors.load(p, n0, at.m, m_end);
+          } else {
+            bias[0] = p.bias && n < p.cols ? p.bias[n] : 0.f;
+            gate.of[0] = tile_gate(p, n, m0, m_end);
+            if constexpr (!kOut8) load_residual16<OutType>(p, ahead, n, m0 + part * 16, m_end);
           }
-          if constexpr (!kOut8 && !kChunked) vectors.load(p, n0, at.m, m_end);
-        } else {
-          bias[0] = p.bias && n < p.cols ? p.bias[n] : 0.f;
-          gate.of[0] = tile_gate(p, n, m0, m_end);
-          if constexpr (!kOut8) load_residual16<OutType>(p, ahead, n, m0 + part * 16, m_end);
-        }
+        };
+        if constexpr (!kChunked) request();          // a chunked sum needs the registers until its total is back in tensor memory
         auto release = [&](int stage) {
           if (lane == 0) mbar_arrive_cluster(empty + 8 * stage);
         };
-        const bool summed = kChunked && chunks > 1;
-        if (summed)
-          ok = add_chunks<kAccs, (kMaxTileChunked / 16 + kParts - 1) / kParts>(
-              chunks, lanes, acc_stride, kAccs * acc_stride, [&](int i) { return (i * kParts + part) * 16; }, m_end - m0, r,
-              sm.acc_full, p.status, release);
+        if (kChunked && chunks > 1)
+          ok = total_in_last(chunks, lanes, part * 16, m_end - m0, r, sm.acc_full, p.status, release);
         else
           ok = __all_sync(0xffffffffu, wait_for(&sm.acc_full[r.stage], r.phase, p.status, kWaitLimitNs));
         if (!ok) break;
         tc_fence_after();
-        if constexpr (TURNED && kChunked) vectors.load(p, n0, at.m, m_end);        // not before: a chunked sum needs the registers
-        const uint32_t sums = lanes + (summed ? kAccs : r.stage) * acc_stride;
+        if constexpr (kChunked) request();
+        const uint32_t sums = lanes + r.stage * kMaxTileT;
 #pragma unroll 1
         for (int col = part * 16; m0 + col < m_end; col += 16 * kParts) {
           float acc[16];
@@ -945,12 +986,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
           }
         }
         if (!ok) break;
-        if (!summed) {
-          tc_fence_before();
-          __syncwarp();
-          release(r.stage);
-          r.next(kAccs);
-        }
+        tc_fence_before();
+        __syncwarp();
+        release(r.stage);
+        r.next(kAccs);
       }
     }
   }
@@ -1084,7 +1123,7 @@ Cut choose_cut(int rows, int cols, int k_iters, int pairs, bool chunked) {      
   }
   if (rows <= kPairRows) return best;
   for (int subs = 1; subs <= (chunked ? 1 : 2); ++subs)
-    for (int nt = chunked ? kMaxTileChunked : kMaxTileT; nt >= 64; nt -= 16) {
+    for (int nt = kMaxTileT; nt >= 64; nt -= 16) {
       const long long waves = ceil_div(ceil_div(cols, 2 * kTileF * subs) * ceil_div(rows, nt), pairs);
       const double stage = std::max(470.0, (kTileF * subs + nt / 2) * 128 / (subs == 2 ? 43.0 : 36.0));
       offer({subs, nt, 1, 4500 + waves * (k_iters * stage + 2500 * subs)});

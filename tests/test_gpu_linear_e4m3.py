@@ -389,7 +389,7 @@ def test_outputs_of_pairs(out, cols, more, gate_rows, residual):
 
 
 @pytest.mark.parametrize("cols", [3000, 3001])
-@pytest.mark.parametrize("rows,inner", [(777, 6144), (777, 6272), (700, 7800)])
+@pytest.mark.parametrize("rows,inner", [(777, 6144), (777, 6272), (700, 7800), (2555, 6400)])
 def test_long_fp32_sums_of_pairs(rows, inner, cols):
     gen = torch.Generator(device="cuda").manual_seed(inner)
     x, w = api.e4m3_matrix(rows, inner), api.e4m3_matrix(cols, inner, 128)
