@@ -140,11 +140,12 @@ __device__ __forceinline__ TileGate tile_gate(const EpilogueParams& p, int n, in
 }
 
 // gate * act(acc + bias) of the first `count` tokens from m0 on.
+template <auto ACTIVATE = activate16>
 __device__ __forceinline__ void gated16(const EpilogueParams& p, float (&acc)[16], int n, int m0, int count, float b,
                                         const TileGate& gate) {
 #pragma unroll
   for (int j = 0; j < 16; ++j) acc[j] += b;
-  activate16(acc, p.act);
+  ACTIVATE(acc, p.act);
   if (p.gate) {
     if (gate.few) {
 #pragma unroll
@@ -168,7 +169,7 @@ __device__ __forceinline__ void gated16(const EpilogueParams& p, float (&acc)[16
 }
 
 // Epilogue of these tokens: `acc` holds the sums; tokens from `m_end` on are not touched.
-template <int OutType>
+template <int OutType, auto ACTIVATE = activate16>
 __device__ __forceinline__ void epilogue16(const EpilogueParams& p, float (&acc)[16], typename OutElem<OutType>::T (&res)[16],
                                            int n, int m0, int m_end, float b, const TileGate& gate) {
   using E = OutElem<OutType>;
@@ -177,7 +178,7 @@ __device__ __forceinline__ void epilogue16(const EpilogueParams& p, float (&acc)
   const int count = min(16, m_end - m0);
   const long long ld = stride_here(p.ld_out);
   T* o = static_cast<T*>(p.out) + m0 * ld + n;
-  gated16(p, acc, n, m0, count, b, gate);
+  gated16<ACTIVATE>(p, acc, n, m0, count, b, gate);
   if (p.residual) {
 #pragma unroll
     for (int j = 0; j < 16; ++j) acc[j] += E::get(res[j]);
