@@ -267,8 +267,8 @@ PyObject* gated_norm(PyObject*, PyObject* const* args, Py_ssize_t n) {
   else
     st = sdvg_gated_norm(mx.p, mx.ld, mx.type, my.p, my.ld, my.type, post, post_weight, static_cast<const float*>(gate.p), gate.ld,
                          gate_rows, xo.p, xo.ld, norm, weight, bias, static_cast<const float*>(scale.p),
-                       static_cast<const float*>(shift.p), scale.p ? scale.ld : shift.ld, mod_rows, eps, mo.p, mo.ld, mo.type,
-                       (int)rows, (int)cols, stream);
+                         static_cast<const float*>(shift.p), scale.p ? scale.ld : shift.ld, mod_rows, eps, mo.p, mo.ld, mo.type,
+                         (int)rows, (int)cols, stream);
   Py_END_ALLOW_THREADS
   return PyLong_FromLong(st);
 }
@@ -402,7 +402,8 @@ PyMethodDef method(const char* name) {
 
 PyMethodDef methods[] = {method<linear>("linear"), method<gated_norm<false>>("gated_norm"), method<qk_norm<kBf16>>("qk_norm"),
                          method<qk_norm<kStatic>>("qk_norm_e4m3"), method<qk_norm<kTiled>>("qk_norm_e4m3_tiled"),
-                         method<linear_e4m3>("linear_e4m3"), method<gated_norm<true>>("gated_norm_e4m3"), method<e4m3_blocks>("e4m3_blocks"), method<read_block_e4m3>("read_block_e4m3"),
+                         method<linear_e4m3>("linear_e4m3"), method<gated_norm<true>>("gated_norm_e4m3"),
+                         method<e4m3_blocks>("e4m3_blocks"), method<read_block_e4m3>("read_block_e4m3"),
                          {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

@@ -631,10 +631,10 @@ bool aligned_to(const void* p, int bytes) { return (reinterpret_cast<uintptr_t>(
 
 // Both entry points: out_type SDVG_E4M3 with out_scale, or another type without.
 int gated_norm(const void* x, int64_t ld_x, int x_type, const void* y, int64_t ld_y, int y_type, int post_norm,
-                    const float* post_weight, const float* gate, int64_t ld_gate, int gate_rows, void* x_out,
-                    int64_t ld_x_out, int norm, const float* weight, const float* bias, const float* scale,
-                    const float* shift, int64_t ld_mod, int mod_rows, float eps, void* out, int64_t ld_out, int out_type,
-                    void* out_scale, int64_t ld_out_scale, int rows, int cols, void* stream) {
+               const float* post_weight, const float* gate, int64_t ld_gate, int gate_rows, void* x_out,
+               int64_t ld_x_out, int norm, const float* weight, const float* bias, const float* scale,
+               const float* shift, int64_t ld_mod, int mod_rows, float eps, void* out, int64_t ld_out, int out_type,
+               void* out_scale, int64_t ld_out_scale, int rows, int cols, void* stream) {
   const bool out8 = out_type == SDVG_E4M3;
   constexpr int kMaxExtent = 0x7fffffff - 1024;                  // a column one step of a CTA further on is still an int
   if (rows < 0 || cols < 1 || rows > kMaxExtent || cols > kMaxExtent) return SDVG_ERR_BAD_SHAPE;
@@ -698,8 +698,9 @@ int gated_norm(const void* x, int64_t ld_x, int x_type, const void* y, int64_t l
     return !base || (sdvg::aligned16(base) && (rows <= group_rows || ld % 4 == 0));
   };
   const bool vec = cols % 8 == 0 && rows_ok(x, ld_x, x_type) && rows_ok(y, ld_y, y_type) && rows_ok(x_out, ld_x_out, x_type) &&
-                   (out8 ? aligned_to(out, 8) && (rows == 1 || ld_out % 8 == 0) : rows_ok(out, ld_out, out_type)) && groups_ok(gate, ld_gate, gate_rows) && groups_ok(scale, ld_mod, mod_rows) &&
-                   groups_ok(shift, ld_mod, mod_rows) && sdvg::aligned16(post_weight) && sdvg::aligned16(weight) &&
+                   (out8 ? aligned_to(out, 8) && (rows == 1 || ld_out % 8 == 0) : rows_ok(out, ld_out, out_type)) &&
+                   groups_ok(gate, ld_gate, gate_rows) && groups_ok(scale, ld_mod, mod_rows) && groups_ok(shift, ld_mod, mod_rows) &&
+                   sdvg::aligned16(post_weight) && sdvg::aligned16(weight) &&
                    sdvg::aligned16(bias);
   return out8 ? launch<true>(p, vec, (cudaStream_t)stream) : launch<false>(p, vec, (cudaStream_t)stream);
 }

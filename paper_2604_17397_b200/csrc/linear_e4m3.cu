@@ -661,7 +661,7 @@ __global__ void __launch_bounds__(kTileThreads) linear8_tile_kernel(const __grid
 // The last 32 columns of tensor memory are the scales' (two words in turn).
 constexpr int kEpiWarps = 16;
 constexpr int kPairThreads = 32 * (kEpiWarps + 3);
-constexpr int kPairSmem = 227 * 1024 - 3072;         // dynamic shared memory of a CTA; the barriers and exchanges are static
+constexpr int kPairSmem = 224 * 1024;                // dynamic shared memory of a CTA; the barriers and exchanges are static
 constexpr int kMaxTileT = 240;
 constexpr int kScaleCol = 480, kPairScaleCols = 16;
 constexpr int kAccs = 2;
@@ -684,7 +684,7 @@ struct PairSmem {
   Exchange exchange[kEpiWarps / 4];
   uint32_t tmem;
 };
-static_assert(sizeof(PairSmem) <= 3072 - 512);
+static_assert(sizeof(PairSmem) + kPairSmem <= 227 * 1024 - 512);
 
 // Adds the chunks of a sum in registers, round-to-nearest, 16 columns from `col`, col + 64, .. each, and leaves the total in the accumulator
 // of the last, which stays the caller's to release.  (A place of its own for the total left room for tiles of 160 tokens:
