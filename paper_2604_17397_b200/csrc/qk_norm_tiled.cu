@@ -111,6 +111,10 @@ struct Walk {
   }
 };
 
+// Smallest scale (its exponent) whose inverse makes one finite number with any factor of a norm, which is at most 2^75: the inverse
+// square root of the smallest float.  In tiles of smaller scales, those of zeros above all, the values take the norm's factor first.
+constexpr int kFoldedScale = -52;
+
 // HEAD: a norm per head.  A token's factor of the norm meets a value only where it is quantised, as one factor with the scale's
 // inverse (a power of two, so that this rounds as the product with the norm's factor alone), and the largest magnitude of its row
 // before that: rounding keeps the order of magnitudes.
@@ -253,11 +257,21 @@ __global__ void __launch_bounds__(kThreads, 1) qk_tiled_kernel(const __grid_cons
     turn ^= 1;
     const int e = sdvg::scale_exponent(top);
     const float inv = sdvg::power_of_two(-e);
+    const bool apart = e < kFoldedScale;                // the same for the group
+    if (apart) {
+#pragma unroll
+      for (int i = 0; i < kRows; ++i) {
+        const float n = HEAD ? of_row[HEAD ? i : 0] : rstd[kStep * i];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[i][k] *= n;
+        if constexpr (HEAD) of_row[i] = 1.f;
+      }
+    }
     if (id == 0) job.scale[h * job.scale_head_stride + tile] = sdvg::power_of_two(e);
     uint2* dst = job.dst + (t0 + r0) * job.token_stride + h * job.head_stride + j;
     const long long step = kStep * job.token_stride;
     auto codes = [&](int i) {
-      const float f = (HEAD ? of_row[HEAD ? i : 0] : rstd[kStep * i]) * inv;
+      const float f = (HEAD ? of_row[HEAD ? i : 0] : apart ? 1.f : rstd[kStep * i]) * inv;
       const float(&a)[8] = v[i];
       return make_uint2(sm100::pack_e4m3x4(a[0] * f, a[1] * f, a[2] * f, a[3] * f), sm100::pack_e4m3x4(a[4] * f, a[5] * f, a[6] * f, a[7] * f));
     };
