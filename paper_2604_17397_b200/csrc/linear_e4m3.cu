@@ -18,6 +18,7 @@
 
 #include "e4m3_scale.cuh"
 #include "elem_types.cuh"
+#include "linear_e4m3_cut.h"
 #include "linear_epilogue.cuh"
 #include "overlap.cuh"
 #include "row_team.cuh"
@@ -27,11 +28,12 @@
 namespace {
 
 using namespace linear;
+using namespace linear8;
 
-constexpr int kTileK = 128;                          // elements of `inner` per stage: one 128-byte swizzled row, one scale
+static_assert(kTileFeatures == kTileF);
+
 constexpr int kWordStages = 4;                       // stages that a 32-bit word of scales serves
 constexpr int kMaxStages = 8;
-constexpr int kScaleSlots = 4;                       // words of scales on their way
 constexpr int kWorkspaceBytes = 256;
 constexpr int kMaxDevices = 64;
 
@@ -97,16 +99,6 @@ struct ScaleWords {
     for (int g = 0; g < GROUPS; ++g) to[32 * g + lane] = make_uint4(w[4 * g][j], w[4 * g + 1][j], w[4 * g + 2][j], w[4 * g + 3][j]);
   }
 };
-
-// fp32 outputs: the tensor core adds products to the accumulator by truncation, so a long sum drifts; there it is cut into chunks
-// that are added with round-to-nearest, as in linear.cu.  A step of the 8-bit kind adds 32 products, twice those of the 16-bit
-// kind, and drifts half as much.  Relative errors at inner = 5120 and 20480 (the worst case, all terms positive, in brackets): in one go
-// 3.4e-7 and 2.0e-6 (1.9e-6 and 1.2e-5), in chunks of 1280 1e-7 (2.5e-7), fp32 sums of a library product 1e-7 (2.4e-7).
-// Sums of up to 6144 go in one: a chunked sum's total is kept in registers, which hold a tile of 256 features and not one of 512
-// (4680 x 8192 x 5120 with gate and residual 230 us in chunks, 4680 x 5120 x 5120 131 in one).  Small tiles have the room: chunks of 512.
-constexpr int kWholeIters = 6144 / kTileK;
-constexpr int kPairChunkIters = 2560 / kTileK;
-constexpr int kTileChunkIters = 512 / kTileK;
 
 // ---- 8-bit outputs ------------------------------------------------------------------------------
 // The four warps that hold the 128 features of a block exchange their largest magnitudes per token through shared memory: 16 tokens
@@ -422,9 +414,6 @@ __device__ __forceinline__ bool quantise_frag(const Linear8Params& p, Exchange& 
 // For few tokens, whose time is that of the weights' way from memory, and for small products of many, which would not give every
 // pair a tile (choose_cut).  Two CTAs share an SM: one multiplies while the other begins or ends.
 constexpr int kTileThreads = 224;                    // four epilogue warps, producer, issuer, scales
-constexpr int kMaxTileFew = 64;                      // tokens per tile, at most
-constexpr int kMaxSplit = 8;                         // portable cluster size
-constexpr int kTileSlotBytes = 1024;                 // a word of scales of the tile's features, and of its tokens
 constexpr int kTileScaleCols = 8;                    // and its columns in tensor memory
 
 struct TileSmem {
@@ -662,7 +651,6 @@ __global__ void __launch_bounds__(kTileThreads) linear8_tile_kernel(const __grid
 constexpr int kEpiWarps = 16;
 constexpr int kPairThreads = 32 * (kEpiWarps + 3);
 constexpr int kPairSmem = 224 * 1024;                // dynamic shared memory of a CTA; the barriers and exchanges are static
-constexpr int kMaxTileT = 240;
 constexpr int kScaleCol = 480, kPairScaleCols = 16;
 constexpr int kAccs = 2;
 constexpr int kSkew = 3;
@@ -1036,13 +1024,6 @@ int make_map(CUtensorMap* m, const void* base, int inner, int rows, int64_t ld, 
 
 std::mutex g_setup_mu;
 
-constexpr int kPairRows = kMaxTileFew;               // up to so many tokens pairs are not considered
-
-// As many stages as leave room for two CTAs on an SM: five up to 32 tokens (3% faster than four), four beyond.
-constexpr int tile_stages(int tile_t) { return tile_t <= 32 ? 5 : 4; }
-constexpr int tile_dynamic(int tile_t) {
-  return tile_stages(tile_t) * (kTileF + tile_t) * 128 + kScaleSlots * kTileSlotBytes + 1024;
-}
 static_assert(2 * (tile_dynamic(32) + 3 * 1024) <= 228 * 1024 && 2 * (tile_dynamic(64) + 3 * 1024) <= 228 * 1024);
 
 // As in linear.cu: no tile takes a larger share of an SM's tensor memory columns than of its shared memory, so that a CTA that an
@@ -1052,17 +1033,6 @@ constexpr bool columns_within_share(int tile_t) {
 }
 static_assert(columns_within_share(16) && columns_within_share(32) && columns_within_share(48) && columns_within_share(64));
 static_assert(kMaxTileFew == 64, "the sizes checked above");
-
-// CTAs per tile: as many as it takes to give every SM work, while all of them run at once and each keeps four stages of the sum,
-// or eight where the SMs have more than one CTA then.
-int tile_split(long long tiles, int k_iters, int tile_t, int sms) {
-  const int per_sm = 228 * 1024 / (tile_dynamic(tile_t) + 2 * 1024);
-  int split = 1;
-  while (split < kMaxSplit && tiles * split < sms && tiles * 2 * split <= (long long)sms * per_sm &&
-         k_iters >= (tiles * 2 * split <= sms ? 8 : 16) * split)
-    split *= 2;
-  return split;
-}
 
 // One-time set-up per device and output type: the opt-in to the kernels' dynamic shared memory, and how many CTA pairs
 // the device runs at once.
@@ -1110,41 +1080,6 @@ int set_up(int* pairs) {
   return SDVG_OK;
 }
 
-// How a product is cut: tiles of 128 features x tile_t tokens by clusters of `split` CTAs, or (subs > 0) tiles of subs x 256 features x tile_t
-// tokens by pairs.  The cheapest by these estimates, in clocks, whose constants were fitted to times of both kinds at 45 sizes:
-// a stage costs the bytes it brings to an SM, 56 of them a clock where CTAs come one or two to an SM, 36 and 43 for pairs, but not
-// less than its barriers and instructions; a split sum is joined; pairs take longer to begin and end.  Pairs against small
-// tiles, in us: 100 x 5120 x 1536 17.4 and 9.4, 333 x 5120 x 776 16.8 and 9.7, 1500 x 1536 x 1536 10.1 and 8.2, 300 x 5120 x 4000 18.3
-// and 15.2, 512 x 4096 x 5120 17.3 and 23.9.
-struct Cut {
-  int subs, tile_t, split;
-  double cost;
-};
-Cut choose_cut(int rows, int cols, int k_iters, int pairs, bool chunked) {                // chunked: the pairs' sum in several chunks
-  auto ceil_div = [](long long a, long long b) { return (a + b - 1) / b; };
-  const int sms = 2 * pairs;
-  Cut best{0, 0, 0, 0};
-  auto offer = [&](const Cut& c) {
-    if (!best.tile_t || c.cost < best.cost) best = c;
-  };
-  const int most = (std::min(rows, kMaxTileFew) + 15) / 16 * 16;
-  for (int nt = most; nt >= std::min(most, 32); nt -= 16) {
-    const long long tiles = ceil_div(cols, kTileF) * ceil_div(rows, nt);
-    const int split = tile_split(tiles, k_iters, nt, sms);
-    const long long on_sm = std::min(2ll, ceil_div(tiles * split, sms)), waves = ceil_div(tiles * split, 2 * sms);
-    const double stage = std::max(250.0, on_sm * (kTileF + nt) * 128 / 56.0);
-    offer({0, nt, split, waves * ceil_div(k_iters, split) * stage + (split > 1 ? 1000 + 300 * split + 45 * nt : 0)});
-  }
-  if (rows <= kPairRows) return best;
-  for (int subs = 1; subs <= (chunked ? 1 : 2); ++subs)
-    for (int nt = kMaxTileT; nt >= 64; nt -= 16) {
-      const long long waves = ceil_div(ceil_div(cols, 2 * kTileF * subs) * ceil_div(rows, nt), pairs);
-      const double stage = std::max(470.0, (kTileF * subs + nt / 2) * 128 / (subs == 2 ? 43.0 : 36.0));
-      offer({subs, nt, 1, 4500 + waves * (k_iters * stage + 2500 * subs)});
-    }
-  return best;
-}
-
 template <int OutType, int SUBS, bool TURNED>
 int launch_pair(Linear8Params& p, const void* x, int64_t ld_x, const void* w, int64_t ld_w, int inner, int pairs, cudaStream_t stream) {
   p.tiles_f = (p.cols + 2 * SUBS * kTileF - 1) / (2 * SUBS * kTileF);
@@ -1169,7 +1104,7 @@ int launch(Linear8Params& p, const void* x, int64_t ld_x, const void* w, int64_t
   int pairs = 0;
   int st = set_up<OutType>(&pairs);
   if (st != SDVG_OK) return st;
-  p.whole = OutType != SDVG_F32 || p.k_iters <= kWholeIters;
+  p.whole = whole_sums(p.k_iters, OutType == SDVG_F32);
   // a program makes the same products over and over: the last answer is kept, which takes a third of a microsecond to find
   static thread_local int known[5] = {};
   static thread_local Cut cut = {};
