@@ -733,8 +733,8 @@ int sdvg_gated_norm_e4m3(const void* x, int64_t ld_x, int x_type, const void* y,
  * bits, but a row may get other bits among another number of rows.  Up to 64 rows, and in products too small for the large tiles, a
  * cluster of up to eight CTAs works on 128 columns by up to 64 rows and may share the sum; else pairs of CTAs walk tiles of 256 or 512
  * columns by up to 240 rows.  16- and 8-bit outputs are summed over `inner` in one go (by each CTA that shares the sum); fp32 ones in chunks of 512 in
- * the small tiles, and in the large ones in one go up to 6144 and in chunks of 2560 beyond (the tensor core's truncation drifts by
- * about 4e-10 of the sum per element of inner, where all terms have one sign).  Outputs whose rows begin at multiples of 16
+ * the small tiles and of 1792 in the large ones (the tensor core's truncation drifts by about 2e-10 of a chunk's sum per element, where all
+ * terms have one sign; chunks are added with round-to-nearest).  Outputs whose rows begin at multiples of 16
  * bytes and are whole vectors are stored as such by the large tiles; others take up to a third longer there.
  * Strides and alignment: x8 and w8 16-byte aligned, ld_x and ld_w multiples of 16 and >= inner; x_scale and w_scale 4-byte aligned,
  * ld_x_scale and ld_w_scale multiples of 4 (a single row's stride is not read; bytes behind a row's scales are not either).

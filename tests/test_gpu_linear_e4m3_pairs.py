@@ -203,6 +203,20 @@ def test_long_sums(size, w_rows, layout):
     check(make(size, "fp32", "gelu", gate_rows=50, residual="rows", seed=5, w_rows=w_rows, layout=layout), in_place=True)
 
 
+@pytest.mark.parametrize("rows,cols,inner", [(1560, 5120, 1792), (1560, 5120, 1793), (777, 3008, 2560), (1560, 5120, 5120), (777, 3013, 6144)])
+def test_fp32_sums_keep_their_digits(rows, cols, inner):
+    """Terms of one sign, whose truncations add up: a chunk of 1792 has 56 steps of 32 products, each off by half a step (2^-24 of the sum
+    so far) on average, the sum so far being half the chunk's on average; the chunks are added to nearest."""
+    gen = torch.Generator(device="cuda").manual_seed(inner)
+    x, w = operand(randn(gen, rows, inner).abs(), 1), operand(randn(gen, cols, inner, std=inner ** -0.5).abs(), 128)
+    out, ws = torch.full((rows, cols), math.nan, device="cuda"), api.attn_workspace()
+    api.sdvg_linear_e4m3(*x, *w, out, ws)
+    assert api.sdvg_block_attn_status(ws) == api.SDVG_OK
+    ref = values(*x, 1) @ values(*w, 128).t()
+    chunks = -(-inner // 1792)
+    assert float((out.double() - ref).norm() / ref.norm()) <= 56 * 2.0 ** -25 + chunks * 2.0 ** -24
+
+
 @pytest.mark.parametrize("tile", [256, 512])
 @pytest.mark.parametrize("sizes", [SIZES, ODD], ids=["vectors", "odd"])
 @pytest.mark.parametrize("out", ["fp32", "bf16", "e4m3"])
