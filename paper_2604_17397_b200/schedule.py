@@ -20,7 +20,7 @@ function drives synthetic traces and a real model.
 from __future__ import annotations
 
 import functools
-from dataclasses import dataclass, field
+from dataclasses import dataclass, field, replace
 from typing import Callable, Optional
 
 import numpy as np
@@ -308,12 +308,13 @@ class TransformerLayerE4M3(TransformerLayer):
     """The same layer with its matrices in E4M3, quantised here once, and 8-bit rows between its operators: both norms, the attention's
     output and the hidden rows of the feed-forward pair are written (or quantised) with a scale per 128 elements, and all
     four products run on the 8-bit tensor cores.  Over an 8-bit ring q, k and v go from the product's rows into the ring in one
-    call, rounded once.  The residual stream, the modulation and the sums stay what they are.
+    call, rounded once.  The residual stream, the modulation and the sums stay what they are.  The 16-bit matrices are not kept.
     """
 
     def __init__(self, weights: LayerWeights, m: ModelState, x_dtype: torch.dtype = torch.bfloat16):
         c = m.cache
-        self.w, self.m, self.width, self.tokens = weights, m, c.heads * c.head_dim, c.block_tokens
+        self.w = replace(weights, w_qkv=None, w_out=None, w_up=None, w_down=None)
+        self.m, self.width, self.tokens = m, c.heads * c.head_dim, c.block_tokens
         hidden, dev = weights.w_up.shape[0], m.table.device
         new = lambda cols, dtype=torch.bfloat16: torch.empty((self.tokens, cols), dtype=dtype, device=dev)
         rows = lambda cols: E4M3Matrix.empty(self.tokens, cols, device=dev)
@@ -400,10 +401,11 @@ class TimeModulation:
 
 
 class TimeModulationE4M3:
-    """TimeModulation with its matrices in E4M3, quantised here once: half the bytes, which is what a few rows pay for."""
+    """TimeModulation with its matrices in E4M3, quantised here once: half the bytes, which is what a few rows pay for.  The 16-bit
+    matrices are not kept."""
 
     def __init__(self, tm: TimeModulation):
-        self.tm = tm
+        self.tm = replace(tm, w1=None, w2=None, w_mod=None)
         self.w1, self.w2, self.w_mod = (E4M3Matrix.of_weight(w) for w in (tm.w1, tm.w2, tm.w_mod))
 
     def __call__(self, features, workspace, out=None) -> torch.Tensor:
