@@ -80,7 +80,10 @@ int sdvg_cache_read_block_e4m3(const sdvg_cache* c, int slot, const float* k_des
   for (int i = 0; i < 2; ++i)
     if (outs[i]) p.job[jobs++] = ReadJob{(const uint4*)bufs[i] + sdvg::slot_offset(c, 0, slot) / 16, (uint4*)outs[i], scales[i]};
   const long long total = (long long)p.tokens * p.heads * 8, want = (total + kThreads - 1) / kThreads;
-  const dim3 grid((unsigned)(want < 148 * 32 ? want : 148 * 32), jobs);
+  int dev = 0, sms = 148;
+  cudaGetDevice(&dev);
+  cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+  const dim3 grid((unsigned)(want < sms * 32ll ? want : sms * 32ll), jobs);
   return sdvg::cuda_status(sdvg::launch_overlapped(ring_read_e4m3_kernel, grid, kThreads, 0, 0, (cudaStream_t)stream, p));
 }
 
