@@ -634,7 +634,9 @@ __global__ void __launch_bounds__(WsCfg<D, F8>::kThreads, 1) attn_fwd_ws_kernel(
           // the largest V exponent met so far (O is rescaled, exactly, when it rises; the row sum never carries it).
           // d stops at 64: beyond that the tile's values are below 2^-64 of what O holds and P may vanish, but
           // the row sum still gets the tile's weights, scaled back by 2^d.
-          c2 = c2_item * k_sc;
+          // Two scales of 2^-126 (tiles of zeros) multiply to 0, which a masked logit, -inf, must not meet: the smallest
+          // normal number in its place moves no logit (|S| < 2^25) by more than 2^-101.
+          c2 = fmaxf(c2_item * k_sc, 1.17549435e-38f);
           c2x2 = pack2(c2, c2);
           const int lv = (__float_as_int(v_sc) >> 23) - 127;
           const float mx_s = mxa * c2;
