@@ -679,7 +679,8 @@ int sdvg_qk_norm_rope3d_commit_e4m3_tiled(sdvg_cache* cache, const void* q, int6
 
 /*
  * A slot of an 8-bit ring read back as values: k_out and v_out (either may be NULL), device bf16 [block_tokens, heads, 128], receive
- * code * scale, rounded once.  k_descale, v_descale: device fp32 [heads], the scales of a ring with static ones (of what is read);
+ * code * scale, the product in fp32 (exact where the scale is a power of two) and rounded to bf16.  k_descale, v_descale: device fp32
+ * [heads], the scales of a ring with static ones (of what is read);
  * both NULL: the ring's tile scales.  Like sdvg_cache_read_block it reads whatever the slot holds.
  * Errors: INVALID_ARG (slot, missing scales), BAD_SHAPE (bf16 ring), BAD_STATE (no scales given and no scale arrays attached),
  * MISALIGNED, UNSUPPORTED_ARCH, CUDA.
@@ -737,7 +738,8 @@ int sdvg_gated_norm_e4m3(const void* x, int64_t ld_x, int x_type, const void* y,
  * terms have one sign; chunks are added with round-to-nearest).  Outputs whose rows begin at multiples of 16
  * bytes and are whole vectors are stored as such by the large tiles; others take up to a third longer there.
  * Strides and alignment: x8 and w8 16-byte aligned, ld_x and ld_w multiples of 16 and >= inner; x_scale and w_scale 4-byte aligned,
- * ld_x_scale and ld_w_scale multiples of 4 (a single row's stride is not read; bytes behind a row's scales are not either).
+ * ld_x_scale and ld_w_scale multiples of 4 (a single row's stride is not read).  Bytes between a row's scales and the next row's may be read and
+ * never count; behind the last row's nothing is read.
  * out, out_scale, residual, bias and gate need the alignment of their element type only.
  * Errors: those of sdvg_linear; INVALID_ARG also for another w_scale_rows.
  */

@@ -38,8 +38,8 @@ inline int tile_split(long long tiles, int k_iters, int tile_t, int sms) {
 // of 1280 0.8e-7 (2.5e-7), 1792 1.0e-7 (3.3e-7), 2048 1.1e-7 (4.3e-7), 2560 1.4e-7 (7.1e-7), in one go 2.8e-7 (2.0e-6); fp32 sums of a
 // library product 1e-7 (2.4e-7).  Longer chunks than 1792 gain little time and lose digits; no chunks at all gain more, since a chunked sum's
 // total is kept in registers, which hold a tile of 256 features and not one of 512: 4680 x 5120 x 5120 with gate and residual 145 us in
-// chunks of 1792, 149 of 1280, 141 of 2560, 129 in one go; 4680 x 20480 x 5120 495, 504 and 486 in chunks.  So only what is one chunk goes in
-// one: the drafter's inner axis of 1536, 4680 x 1536 x 1536 26 us (34 in chunks of 1280).  Small tiles have the room: chunks of 512.
+// chunks of 1792, 149 of 1280, 141 of 2560, 129 in one go (20 launches from cold); 4680 x 20480 x 5120 495, 504 and 486 in chunks (400 launches).
+// So only what is one chunk goes in one: the drafter's inner axis of 1536, 4680 x 1536 x 1536 26 us (34 in chunks of 1280).  Small tiles have the room: chunks of 512.
 constexpr int kPairChunkIters = 1792 / kTileK;
 constexpr int kWholeIters = kPairChunkIters;
 constexpr int kTileChunkIters = 512 / kTileK;

@@ -117,7 +117,8 @@ constexpr int kFoldedScale = -52;
 
 // HEAD: a norm per head.  A token's factor of the norm meets a value only where it is quantised, as one factor with the scale's
 // inverse (a power of two, so that this rounds as the product with the norm's factor alone), and the largest magnitude of its row
-// before that: rounding keeps the order of magnitudes.
+// before that: rounding keeps the order of magnitudes.  A row's values meet their weights before either, in fp32's range for weights from
+// 2^-60 to 2^60.
 template <bool HEAD>
 __global__ void __launch_bounds__(kThreads, 1) qk_tiled_kernel(const __grid_constant__ TiledParams p) {
   extern __shared__ uint4 s_dynamic[];

@@ -1,4 +1,4 @@
-// A slot of an 8-bit ring as bf16 tensors: code times scale, rounded once.  A thread turns 16 codes of a (token, head) row (one 16-byte
+// A slot of an 8-bit ring as bf16 tensors: code times scale in fp32, rounded to bf16.  A thread turns 16 codes of a (token, head) row (one 16-byte
 // load) into two 16-byte stores.  Bound by HBM: 1 byte read and 2 written per element.
 #include <cuda_bf16.h>
 
